@@ -22,7 +22,7 @@
  *   - Workspaces are scratch: contents are undefined before and after a call;
  *     base must be 256-byte aligned.  Two calls that share a workspace or an
  *     output buffer must be ordered on the stream.
- *   - Shape limits of this library: n_clients <= 256, batch_cap <= 256,
+ *   - Shape limits of the scheduling calls: n_clients <= 256, batch_cap <= 256,
  *     n_req <= 24384, kv_budget < 2^31, estimated times T_i < 2^32; for the lower bounds
  *     also n_req * R^2 / 2 < 2^63, R = the most KV tokens one request may need
  *     (kv_reserve_tokens if set, else kv_budget).
@@ -315,6 +315,88 @@ int hos_lower_bound_static(const hos_batch* batch, const hos_cost_model* cm, hos
  * Experiment section. */
 int hos_trace_offsets(const hos_client_result* cres, int64_t n_units, int64_t* trace_off,
                       void* stream);
+
+/*
+ * The KV side of the iterations that are scheduled above.  A client keeps the keys and values of its
+ * running requests in pages of page_size tokens (the paper's client: 1,024 blocks of 128 tokens);
+ * a prefill iteration appends its prompts' keys and values and lets every new token attend to its
+ * own sequence, a decode iteration does the same with one token per request.
+ *
+ * Element types: queries, new keys and values, and outputs are all HOS_TYPE_BF16 or all
+ * HOS_TYPE_FP16.  The cache holds that type (HOS_KV_SAME) or 8-bit codes with one 32-bit scale per
+ * token and KV head (HOS_KV_E4M3: floating point, 4 exponent and 3 mantissa bits; HOS_KV_INT8):
+ *   a = max(max_d |x_d|, 1e-30), scale = a / Q, code_d = round_to_nearest_even(x_d * (Q / a)),
+ *   Q = 448 or 127, each operation rounded to 32 bits;  the value of a code is code * scale.
+ * A vector that holds a NaN or an infinity reads back as NaN.
+ */
+enum { HOS_TYPE_BF16 = 0, HOS_TYPE_FP16 = 1 };
+enum { HOS_KV_SAME = 0, HOS_KV_E4M3 = 1, HOS_KV_INT8 = 2 };
+
+/* HOST struct; DEVICE arrays.  k, v: [n_pages][n_kv_heads][page_size][head_dim], pages page_stride
+ * elements apart (0: densely packed); k_scale, v_scale (8-bit formats only, else NULL):
+ * [n_pages][n_kv_heads][page_size], pages scale_page_stride elements apart (0: densely packed).
+ * head_dim 64 or 128; page_size 16, 32, 64, 128 or 256; all bases and page strides multiples of 16 bytes. */
+typedef struct hos_kv_cache {
+    int32_t n_pages, page_size, n_kv_heads, head_dim, type, format;
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t page_stride, scale_page_stride;
+} hos_kv_cache;
+
+/* HOST struct; DEVICE arrays.  Sequence s owns the n_s = tok_off[s+1] - tok_off[s] packed tokens from
+ * tok_off[s] on.  They are the last n_s of its kv_len[s] tokens: token i is at position
+ * kv_len[s] - n_s + i.  Token j of the sequence lies in row j % page_size of page
+ * page_table[s * table_stride + j / page_size]; entries past the last token are not read.
+ * max_new: no n_s is larger (it chooses kernels, a larger n_s costs time only). */
+typedef struct hos_kv_batch {
+    int32_t n_seq, n_tokens, max_new, max_pages;
+    const int32_t* tok_off;      /* [n_seq + 1] */
+    const int32_t* kv_len;       /* [n_seq] */
+    const int32_t* page_table;   /* [n_seq][table_stride], max_pages entries of a row are its own */
+    int64_t table_stride;
+} hos_kv_batch;
+
+/*
+ * Writes the new tokens' keys and values to their places in the cache, in the cache's format.
+ * k, v: element (token, head, d) at token * tok_stride + head * head_stride + d (elements; bases
+ * and strides multiples of 16 bytes), so that slices of one projection's output need no copy.
+ * A token at a negative position (n_s > kv_len[s]) has no place and is skipped.  Two tokens of one
+ * call must not share a place.
+ *   status [n_seq], nullable, OR-ed into: HOS_ST_INVALID where offsets, length or a page number
+ *   are out of range; tokens without a valid place are skipped, nothing else is written.
+ */
+int hos_kv_append(const hos_kv_cache* cache, const hos_kv_batch* batch, const void* k, const void* v,
+                  int64_t k_tok_stride, int64_t k_head_stride, int64_t v_tok_stride, int64_t v_head_stride,
+                  int32_t* status, void* stream);
+
+/*
+ * The inverse: the batch's tokens are read from the cache, k and v [n_tokens][n_kv_heads][head_dim]
+ * (dense) in the cache's `type`: code * scale in 32 bits, rounded once.  With n_s = kv_len[s] that is
+ * everything a sequence holds.  Tokens without a valid place read as zero; status as above.
+ */
+int hos_kv_read(const hos_kv_cache* cache, const hos_kv_batch* batch, void* k, void* v, int32_t* status,
+                void* stream);
+
+/*
+ * Attention of the batch's new tokens to the cache (which already holds their own keys and values).
+ * Query head h reads KV head h / (n_heads / n_kv_heads).  Token at position pos sees token j of its
+ * sequence if j < kv_len, with `causal` j <= pos, and with window > 0 j > pos - window:
+ *   x_j = sm_scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = ln sum_j exp(x_j).
+ * A row that sees nothing gets out = 0, lse = -inf.  Sums, maxima and normalisers are held in 32
+ * bits; the weights are rounded to 16 bits (of the output's type, fp16 with an 8-bit cache) for their
+ * product with the values.  Memory past a sequence's last token may hold anything, NaN included; a
+ * non-finite value that some new token of a sequence sees may also reach other new tokens of that sequence.
+ *   q    element (token, head, d) at token * q_tok_stride + head * q_head_stride + d (16-byte multiples)
+ *   out  likewise with its own strides;  lse [n_tokens][n_heads], nullable
+ *   status [n_seq], nullable, OR-ed into: HOS_ST_INVALID (offsets, length or page number out of
+ *   range: the sequence's rows are undefined, nothing outside the given arrays is touched),
+ *   HOS_ST_LIMIT (a bounded wait inside a kernel ran out; cannot happen on a working device)
+ */
+int hos_paged_attention(const hos_kv_cache* cache, const hos_kv_batch* batch, const void* q,
+                        int64_t q_tok_stride, int64_t q_head_stride, int n_heads, float sm_scale, int causal,
+                        int window, void* out, int64_t out_tok_stride, int64_t out_head_stride, float* lse,
+                        int32_t* status, void* ws, size_t ws_bytes, void* stream);
+size_t hos_paged_attention_workspace_bytes(const hos_kv_cache* cache, const hos_kv_batch* batch, int n_heads);
 
 size_t hos_offline_workspace_bytes(const hos_batch* batch, int n_copies, int ls_rounds);
 size_t hos_offline_multifit_workspace_bytes(const hos_batch* batch, int ls_rounds);

@@ -12,3 +12,6 @@ from .binding import (  # noqa: F401
     HosError, exported_symbols, hos_debug_bounds_violations, hos_local_search, hos_lower_bound, hos_lower_bound_static, hos_offline_pack,
     hos_online_simulate, hos_online_simulate_steal, hos_set_launch_hook, hos_strerror, hos_trace_fill, hos_trace_offsets, lib, lib_path,
 )
+from .kv_cache import (  # noqa: F401
+    HOS_KV_E4M3, HOS_KV_INT8, HOS_KV_SAME, KvCache, hos_kv_append, hos_kv_cache, hos_kv_read, hos_paged_attention,
+)

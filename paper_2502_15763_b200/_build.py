@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(_PKG, "libhos.so")
 DEBUG_LIB_PATH = os.path.join(_PKG, "libhos_debug.so")   # the bounds-checked build (-DHOS_DEBUG_BOUNDS)
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
+              "-shared", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "-t", "0"]
 
 
 def _sources():

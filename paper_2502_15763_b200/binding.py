@@ -32,7 +32,8 @@ _SYMBOLS = ("hos_offline_pack", "hos_local_search", "hos_lower_bound", "hos_onli
             "hos_trace_offsets", "hos_offline_workspace_bytes", "hos_lower_bound_workspace_bytes",
             "hos_online_workspace_bytes", "hos_strerror", "hos_set_launch_hook",
             "hos_lower_bound_static", "hos_trace_fill", "hos_online_simulate_steal",
-            "hos_offline_pack_multifit", "hos_debug_bounds_violations", "hos_offline_multifit_workspace_bytes")
+            "hos_offline_pack_multifit", "hos_debug_bounds_violations", "hos_offline_multifit_workspace_bytes",
+            "hos_kv_append", "hos_kv_read", "hos_paged_attention", "hos_paged_attention_workspace_bytes")
 
 LAUNCH_HOOK = C.CFUNCTYPE(None, C.c_char_p, C.c_int, C.c_void_p, C.c_void_p)
 
@@ -76,13 +77,20 @@ def lib():
         L = C.CDLL(path)
         L.hos_debug_bounds_violations.restype = C.c_longlong
         for name in ("hos_offline_workspace_bytes", "hos_lower_bound_workspace_bytes",
-                     "hos_online_workspace_bytes", "hos_offline_multifit_workspace_bytes"):
+                     "hos_online_workspace_bytes", "hos_offline_multifit_workspace_bytes",
+                     "hos_paged_attention_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.hos_strerror.restype = C.c_char_p
         for name in ("hos_offline_pack", "hos_local_search", "hos_lower_bound",
                      "hos_online_simulate", "hos_trace_offsets", "hos_lower_bound_static", "hos_trace_fill",
-                     "hos_online_simulate_steal", "hos_offline_pack_multifit"):
+                     "hos_online_simulate_steal", "hos_offline_pack_multifit", "hos_kv_append", "hos_kv_read",
+                     "hos_paged_attention"):
             getattr(L, name).restype = C.c_int
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        L.hos_kv_append.argtypes = [p, p, p, p, i64, i64, i64, i64, p, p]
+        L.hos_kv_read.argtypes = [p, p, p, p, p, p]
+        L.hos_paged_attention.argtypes = [p, p, p, i64, i64, i32, C.c_float, i32, i32, p, i64, i64, p, p, p, C.c_size_t, p]
+        L.hos_paged_attention_workspace_bytes.argtypes = [p, p, i32]
         _lib = L
     return _lib
 

@@ -87,4 +87,16 @@ cudaError_t launch_finalize(const hos_batch& b, int n_lambda, const unsigned lon
 cudaError_t launch_trace_offsets(const hos_client_result* cres, long long n_units, long long* trace_off,
                                  cudaStream_t st);
 
+// KV cache and attention over it (hos_kv_cache.cu, hos_attn_rows.cu).
+struct KvView;
+struct AttnView;
+struct RowState;
+struct Partial;
+cudaError_t launch_kv_append(const KvView& c, int type, int format, const void* k, const void* v,
+                             const long long (&strides)[4], cudaStream_t st);
+cudaError_t launch_kv_read(const KvView& c, int type, int format, void* k, void* v, cudaStream_t st);
+int attn_rows_workers();
+cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int max_rows, Partial* meta, RowState* state,
+                             float* part, cudaStream_t st);
+
 }  // namespace hos

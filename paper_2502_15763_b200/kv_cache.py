@@ -1,0 +1,174 @@
+"""Binding of the KV-cache calls: keys and values in pages, written, read back and attended to.
+
+`hos_kv_cache` checks a cache's tensors once and returns the handle that the other calls take.  The
+batch is the same three device tensors everywhere (int32): `tok_off` [n_seq + 1], the packed new
+tokens of every sequence; `kv_len` [n_seq], its tokens in the cache, the new ones included;
+`page_table` [n_seq][>= pages], its pages in order.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+from .binding import _check, _torch, lib
+
+HOS_KV_SAME, HOS_KV_E4M3, HOS_KV_INT8 = 0, 1, 2
+
+
+class _KvCache(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("type", C.c_int32), ("format", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("page_stride", C.c_int64),
+                ("scale_page_stride", C.c_int64)]
+
+
+class _KvBatch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("max_pages", C.c_int32),
+                ("tok_off", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64)]
+
+
+class KvCache:
+    """Handle of a paged cache: its tensors, checked, and the C description of them.
+
+    `status` (int32, one word per sequence of the largest batch so far) collects the HOS_ST_* bits of the
+    calls made with this handle until `status.zero_()`."""
+
+    def __init__(self, k, v, k_scale, v_scale, dtype):
+        torch = _torch()
+        formats = {torch.float8_e4m3fn: HOS_KV_E4M3, torch.int8: HOS_KV_INT8}
+        types = {torch.bfloat16: 0, torch.float16: 1}
+        for t, what in ((k, "k"), (v, "v")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4):
+                raise TypeError(f"{what}: expected a CUDA tensor [n_pages][n_kv_heads][page_size][head_dim]")
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride() != k.stride():
+            raise ValueError("k and v must agree in shape, type, device and strides")
+        self.format = formats.get(k.dtype, HOS_KV_SAME)
+        dtype = dtype if dtype is not None else k.dtype
+        if dtype not in types:
+            raise TypeError("dtype: bfloat16 or float16 (give it for an 8-bit cache)")
+        if self.format == HOS_KV_SAME and k.dtype != dtype:
+            raise TypeError(f"k, v: expected {dtype}, float8_e4m3fn or int8")
+        n_pages, n_kv, page, dim = k.shape
+        if tuple(k.stride()[1:]) != (page * dim, dim, 1):
+            raise ValueError("k, v: only the pages may be strided")
+        scale_stride = 0
+        if self.format != HOS_KV_SAME:
+            for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+                if not (isinstance(t, torch.Tensor) and t.device == k.device and t.dtype == torch.float32):
+                    raise TypeError(f"{what}: expected a CUDA tensor of float32")
+                if tuple(t.shape) != (n_pages, n_kv, page) or tuple(t.stride()[1:]) != (page, 1):
+                    raise ValueError(f"{what}: expected [n_pages][n_kv_heads][page_size], strided by pages only")
+            if k_scale.stride(0) != v_scale.stride(0):
+                raise ValueError("k_scale and v_scale must have the same strides")
+            scale_stride = k_scale.stride(0)
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to an 8-bit cache")
+        self.k, self.v, self.k_scale, self.v_scale, self.dtype = k, v, k_scale, v_scale, dtype
+        self.n_kv_heads, self.page_size, self.head_dim, self.device = n_kv, page, dim, k.device
+        self.status = torch.zeros((256,), dtype=torch.int32, device=k.device)
+        # a page's stride means nothing where there is one page
+        dense = n_kv * page * dim
+        self._c = _KvCache(n_pages, page, n_kv, dim, types[dtype], self.format, k.data_ptr(), v.data_ptr(),
+                           k_scale.data_ptr() if k_scale is not None else None,
+                           v_scale.data_ptr() if v_scale is not None else None,
+                           k.stride(0) if n_pages > 1 else dense, scale_stride if n_pages > 1 else 0)
+        self._ref = C.byref(self._c)
+        self._ws_bytes = 0
+
+    def _batch(self, tok_off, kv_len, page_table, n_tokens, max_new):
+        torch = _torch()
+        for t, what, dims in ((tok_off, "tok_off", 1), (kv_len, "kv_len", 1), (page_table, "page_table", 2)):
+            if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == torch.int32 and t.dim() == dims
+                    and (t.shape[-1] < 2 or t.stride(-1) == 1)):
+                raise TypeError(f"{what}: expected a {dims}-dimensional int32 tensor on the cache's device, dense rows")
+        n_seq = kv_len.shape[0]
+        if tok_off.shape[0] != n_seq + 1 or page_table.shape[0] != n_seq:
+            raise ValueError("tok_off must have n_seq + 1 entries, page_table n_seq rows")
+        if n_seq > self.status.shape[0]:
+            old = self.status
+            self.status = torch.zeros((2 * n_seq,), dtype=torch.int32, device=self.device)
+            self.status[:old.shape[0]] = old
+        width = page_table.shape[1]
+        return _KvBatch(n_seq, n_tokens, max_new, width, tok_off.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                        page_table.stride(0) if n_seq > 1 else width)
+
+    def _rows(self, t, what, heads=None):
+        torch = _torch()
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == self.dtype and t.dim() == 3
+                and t.stride(2) == 1):
+            raise TypeError(f"{what}: expected a [tokens][heads][head_dim] tensor of {self.dtype} on the cache's device, "
+                            "elements of a head dense")
+        if t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{what}: heads or head_dim do not match the cache")
+        return t
+
+
+def _raw_stream(device):
+    return _torch().cuda.current_stream(device).cuda_stream
+
+
+def hos_kv_cache(k, v, k_scale=None, v_scale=None, dtype=None) -> KvCache:
+    """Handle of the cache in tensors k, v [n_pages][n_kv_heads][page_size][head_dim]: bfloat16 or float16, or
+    float8_e4m3fn or int8 with float32 scales [n_pages][n_kv_heads][page_size] and the `dtype` of the
+    queries and outputs.  The tensors stay the caller's; the handle keeps them alive."""
+    return KvCache(k, v, k_scale, v_scale, dtype)
+
+
+def hos_kv_append(cache: KvCache, k, v, tok_off, kv_len, page_table):
+    """Writes the new tokens' k and v [n_tokens][n_kv_heads][head_dim] (strided views are fine) to their
+    places, quantised to the cache's format.  Returns {'status': the handle's words}."""
+    cache._rows(k, "k", cache.n_kv_heads)
+    cache._rows(v, "v", cache.n_kv_heads)
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    b = cache._batch(tok_off, kv_len, page_table, k.shape[0], k.shape[0])
+    _check(lib().hos_kv_append(cache._ref, C.byref(b), k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0),
+                               v.stride(1), cache.status.data_ptr(), _raw_stream(cache.device)), "hos_kv_append")
+    return dict(status=cache.status)
+
+
+def hos_kv_read(cache: KvCache, tok_off, kv_len, page_table, n_tokens: int, out=None):
+    """The batch's tokens (the last tok_off[s+1] - tok_off[s] of sequence s; n_tokens in all) from the cache,
+    dequantised: {'k', 'v': [n_tokens][n_kv_heads][head_dim], 'status'}.  out: optional dense (k, v) to write into."""
+    torch = _torch()
+    shape = (int(n_tokens), cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        k = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+        v = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+    else:
+        k, v = (cache._rows(t, "out") for t in out)
+        if tuple(k.shape) != shape or tuple(v.shape) != shape or not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("out tensors must be dense [n_tokens][n_kv_heads][head_dim]")
+    b = cache._batch(tok_off, kv_len, page_table, shape[0], shape[0])
+    _check(lib().hos_kv_read(cache._ref, C.byref(b), k.data_ptr(), v.data_ptr(), cache.status.data_ptr(),
+                             _raw_stream(cache.device)), "hos_kv_read")
+    return dict(k=k, v=v, status=cache.status)
+
+
+def hos_paged_attention(q, cache: KvCache, tok_off, kv_len, page_table, max_new: int, sm_scale=None, causal: bool = True,
+                        window: int = 0, want_lse: bool = False, out=None, ws=None):
+    """Attention of the batch's new tokens, q [n_tokens][n_heads][head_dim], to their sequences in the cache (which
+    already holds the new tokens' own keys and values): {'out': like q, dense, 'lse': float32 [n_tokens][n_heads]
+    or None, 'status'}.
+
+    max_new: no sequence has more new tokens.  sm_scale: default 1 / sqrt(head_dim).  window > 0: a token sees
+    the last `window` tokens up to itself.  out, ws: optional output tensor and workspace."""
+    torch = _torch()
+    cache._rows(q, "q")
+    n_tok, heads = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((n_tok, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    elif cache._rows(out, "out", heads).shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    lse = torch.empty((n_tok, heads), dtype=torch.float32, device=cache.device) if want_lse else None
+    b = cache._batch(tok_off, kv_len, page_table, n_tok, int(max_new))
+    L = lib()
+    need = L.hos_paged_attention_workspace_bytes(cache._ref, C.byref(b), heads)
+    if ws is None or ws.numel() < need:
+        ws = torch.empty((max(need, 256),), dtype=torch.uint8, device=cache.device)
+    scale = 1.0 / math.sqrt(cache.head_dim) if sm_scale is None else float(sm_scale)
+    _check(L.hos_paged_attention(cache._ref, C.byref(b), q.data_ptr(), q.stride(0), q.stride(1), heads, scale, int(causal),
+                                 int(window), out.data_ptr(), out.stride(0), out.stride(1),
+                                 lse.data_ptr() if lse is not None else None, cache.status.data_ptr(), ws.data_ptr(),
+                                 ws.numel(), _raw_stream(cache.device)), "hos_paged_attention")
+    return dict(out=out, lse=lse, status=cache.status)
