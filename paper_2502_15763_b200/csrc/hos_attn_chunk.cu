@@ -1,0 +1,743 @@
+// Attention of many query rows per sequence and KV head (prompts, chunks of new tokens) to the paged cache.
+//
+// The mathematics: with x = scale * log2(e) * q.k, a row keeps a reference m near its running maximum, l = sum 2^(x - m)
+// and O = sum 2^(x - m) v; m moves (and O and l are rescaled) only when the maximum has grown by more than 2^8 -- the
+// quotient O / l does not depend on m, and 2^8 is far inside every type's range -- so O is rescaled in the first few
+// steps of a tile and hardly ever after.
+//
+// One CTA of 12 (16-bit cache) or 16 warps (8-bit cache) an SM works through an equal, contiguous share of the batch's
+// steps of 128 tokens; a tile is two halves of 128 rows.  Both products run on tcgen05: S = Q K^T from shared memory
+// into tensor memory (128 columns a half), O += P V with P from tensor memory, where it takes the place of S.
+// While one half's S is turned into P by its four warps (one thread a row, no shuffles), the tensor cores have the other
+// half's products.
+//   warps 0-3, 4-7   softmax, output of half 0, 1
+//   warp 8           K and V of a 16-bit cache into a ring of shared memory by TMA, page by page
+//   warp 9           issues the products
+//   warps 10, 11     the rows of the next tile's queries, half 0, 1
+//   warps 12-15      (8-bit cache) codes to fp16 on their way from global to shared memory
+// An 8-bit cache's K scale multiplies the score, its V scale joins the exponent: y_j = x_j + log2 vs_j, the weights 2^(y_j - m)
+// meet the bare codes and are safe in fp16 whatever the scales are, and l = sum 2^(y_j - m) / vs_j.
+//
+// All waits are bounded: one that runs out sets HOS_ST_LIMIT and the CTA drains and returns.
+#include <cuda.h>
+
+#include "hos_attn_list.cuh"
+#include "hos_kernels.h"
+#include "hos_kv.cuh"
+
+namespace hos {
+namespace {
+
+constexpr int ROWS = 256, STEP = 128, HALF = 128;
+using List = AttnList<ROWS, STEP>;
+using Cursor = List::Cursor;
+constexpr float GROWTH = 8.0f;                // log2 of how far a row's maximum may pass the one its reference was taken from
+// The reference is the maximum - LIFT: fp16 weights start at 2^7 and end below 2^15, so that small ones keep their bits.
+template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 7.0f : 0.0f;
+
+template <typename T, int FMT, int D> struct Cfg {
+    static constexpr bool Q8 = FMT != HOS_KV_SAME;
+    static constexpr int THREADS = Q8 ? 512 : 384;
+    static constexpr int TILE_BYTES = STEP * D * 2;            // K or V of a step, 16-bit
+    static constexpr int Q_BYTES = HALF * D * 2;               // one half's queries
+    static constexpr int STAGES = D == 128 ? (Q8 ? 4 : 5) : 8;
+    static constexpr int SCALE_BUFS = STAGES / 2 + 1;
+    static constexpr int SCALES = Q8 ? SCALE_BUFS * 3 * STEP * 4 : 0;
+    static constexpr bool Q_RANGE = Q8 && !std::is_same<T, __half>::value;   // bf16 queries become fp16
+    static constexpr int Q_SCALES = Q_RANGE ? 2 * ROWS * 4 : 0;
+    static constexpr int HEAD = 1024;                          // barriers, the cursor, the tensor memory address
+    static constexpr int SMEM = 1024 /*alignment*/ + HEAD + 2 * Q_BYTES + STAGES * TILE_BYTES + SCALES + Q_SCALES;
+};
+template <typename T, int FMT> struct MatType { using type = __half; };
+template <typename T> struct MatType<T, HOS_KV_SAME> { using type = T; };
+
+// --- barriers ---------------------------------------------------------------------------------
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+constexpr unsigned long long WAIT_NS = 2000000000ull;
+// The whole warp waits for the phase; false (for all lanes) after two seconds or once another role has given up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (__all_sync(FULL, bar_try(bar, parity))) return true;
+    const unsigned long long t0 = now_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (__all_sync(FULL, bar_try(bar, parity))) return true;
+        if (now_ns() - t0 > WAIT_NS) *gave_up = 1;
+        if (__any_sync(FULL, *gave_up != 0)) return false;
+    }
+}
+
+// --- tcgen05 ----------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+// D[128][N] (+)= A[128][16] B[N][16]^T, both in shared memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// The same with A in tensor memory.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+#define HOS_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
+#define HOS_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+// 32 columns of this thread's row of tensor memory.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : HOS_R8(x, 0), HOS_R8(x, 8), HOS_R8(x, 16), HOS_R8(x, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+                 :: HOS_W8(x, 0), HOS_W8(x, 8), HOS_W8(x, 16), HOS_W8(x, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 :: HOS_W8(x, 0), HOS_W8(x, 8), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory operands: rows of 128 bytes (64 elements along head_dim), the 16-byte chunk c of row r at c ^ (r & 7);
+// a tile of head_dim 128 is two such blocks of 128 rows, one after the other.
+constexpr int BLOCK_BYTES = 128 * 128;
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead_bytes) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(lead_bytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+constexpr uint32_t instr_desc(bool bf16, bool b_along_n, int n) {
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_along_n ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+struct Shared {                                // in the first HEAD bytes
+    uint64_t bars[32];
+    Cursor first;
+    long long lo, hi, total, active;
+    uint32_t tmem;
+    int gave_up;
+};
+static_assert(sizeof(Shared) <= 1024, "");
+
+struct Segment { int blocks; bool starts, ends; };   // steps of the current tile that are this CTA's; whether it has the first, the last
+
+template <typename T, int FMT, int D>
+__global__ void __launch_bounds__(Cfg<T, FMT, D>::THREADS, 1)
+k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+             const int min_rows, Partial* __restrict__ meta, RowState* __restrict__ state, float* __restrict__ part) {
+    using C = Cfg<T, FMT, D>;
+    using M = typename MatType<T, FMT>::type;
+    constexpr bool BF16 = std::is_same<M, __nv_bfloat16>::value;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    Shared& sh = *reinterpret_cast<Shared*>(base);
+    volatile int* gave_up = &sh.gave_up;
+    const uint32_t q_smem = smem_u32(base) + C::HEAD, ring = q_smem + 2 * C::Q_BYTES;
+    const uint32_t scales = ring + C::STAGES * C::TILE_BYTES;          // [buffer][scale log2(e) ks | log2 vs | 1 / vs][token]
+    const uint32_t q_scales = scales + C::SCALES;                      // [tile parity][row]: what a row of queries was divided by
+    const uint32_t bar0 = smem_u32(sh.bars);
+    auto kv_full = [&](int i) { return bar0 + 8 * i; };
+    auto kv_free = [&](int i) { return bar0 + 8 * (C::STAGES + i); };
+    const uint32_t bar1 = bar0 + 16 * C::STAGES;
+    auto q_full = [&](int h) { return bar1 + 8 * h; };
+    auto q_free = [&](int h) { return bar1 + 16 + 8 * h; };
+    auto s_full = [&](int h) { return bar1 + 32 + 8 * h; };
+    auto p_ready = [&](int h) { return bar1 + 48 + 8 * h; };
+    auto o_done = [&](int h) { return bar1 + 64 + 8 * h; };
+    const uint32_t drain = bar1 + 80;
+    const int warp = warp_id(), lane = lane_id(), w = (int)blockIdx.x;
+    const List list{a, min_rows, 0x7FFFFFFF};
+    pdl_launch_dependents();
+
+    if (warp == 0) {
+        const long long total = list.total(w == 0);
+        const int active = (int)min((long long)gridDim.x, total);
+        const long long lo = w < active ? total * w / active : 0, hi = w < active ? total * (w + 1) / active : 0;
+        Cursor c = {};
+        if (hi > lo) c = list.locate(lo);
+        if (lane == 0) {
+            sh.first = c;
+            sh.lo = lo;
+            sh.hi = hi;
+            sh.total = total;
+            sh.active = active;
+            sh.gave_up = 0;
+            meta[w].last = -1;                 // until the softmax warps find a tile that begins here and ends in a later share
+        }
+    } else if (warp == 1 && lane == 0) {
+        for (int i = 0; i < C::STAGES; ++i) {
+            bar_init(kv_full(i), C::Q8 ? 4 : 1);
+            bar_init(kv_free(i), 1);
+        }
+        for (int h = 0; h < 2; ++h) {
+            bar_init(q_full(h), 1);
+            bar_init(q_free(h), 1);
+            bar_init(s_full(h), 1);
+            bar_init(p_ready(h), 4);
+            bar_init(o_done(h), 1);
+        }
+        bar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    const long long lo = sh.lo, hi = sh.hi;
+    Cursor cur = sh.first;
+    // the steps from `at` to the end of the tile or the share
+    auto segment = [&](long long at) {
+        Segment s;
+        const long long left = hi - at;
+        const int rest = cur.t.steps - cur.step;
+        s.blocks = left < rest ? (int)left : rest;
+        s.starts = cur.step == 0;
+        s.ends = s.blocks == rest;
+        return s;
+    };
+
+    if (warp < 8) {
+        // ================================ softmax and output ================================
+        if (C::Q8) more_registers<168>(); else more_registers<216>();
+        const int h = warp >> 2, row = (warp & 3) * 32 + lane;         // row of this half
+        const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_tm = tmem + lane_at + h * 128, o_tm = tmem + lane_at + 256 + h * D;
+        const float c = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);   // positive, so that masked scores stay -inf
+        uint32_t s_phase = 0, o_phase = 0;
+        long long block = 0;                                           // steps this CTA has begun: ring item 2 * block is K
+        uint32_t q_buf = 1;
+        bool ok = true;
+        for (long long at = lo; at < hi && ok;) {
+            const Segment seg = segment(at);
+            const bool active = cur.t.rows > h * HALF;
+            q_buf ^= 1;
+            if (!active) {
+                at += seg.blocks; block += seg.blocks;
+                if (at < hi) list.next(cur);
+                continue;
+            }
+            const int r = cur.tile * ROWS + h * HALF + row;
+            const bool there = h * HALF + row < cur.t.rows;
+            const int tok = r / a.group, hd = cur.head * a.group + r - tok * a.group;
+            const int pos = cur.q.len - cur.q.n + tok;
+            // rows past the tile see everything: no masking, and they are not written
+            const int see_hi = !there ? 0x7FFFFFFF : a.causal ? min(cur.q.len, pos + 1) : cur.q.len;
+            const int see_lo = there && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+            for (int b = 0; b < seg.blocks; ++b, ++block) {
+                const int j0 = cur.t.k0 + (cur.step + b) * STEP;
+                const int buf = C::Q8 ? (int)(block % C::SCALE_BUFS) : 0;
+                if (C::Q8) {
+                    const long long item = 2 * block;
+                    if (!bar_wait(kv_full((int)(item % C::STAGES)), (uint32_t)(item / C::STAGES) & 1, gave_up)) { ok = false; break; }
+                }
+                if (!bar_wait(s_full(h), s_phase, gave_up)) { ok = false; break; }
+                s_phase ^= 1;
+                tc_fence_after();
+                uint32_t s[128];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_load32(s_tm + 32 * i, s + 32 * i);
+                tmem_wait_load();
+                float* x = reinterpret_cast<float*>(s);
+                const uint32_t f_at = scales + buf * (3 * STEP * 4), lv_at = f_at + STEP * 4, iv_at = lv_at + STEP * 4;
+                if (C::Q_RANGE) {
+                    const float up = lds32f(q_scales + (q_buf * ROWS + h * HALF + row) * 4);
+                    if (__any_sync(FULL, up != 1.0f)) {
+#pragma unroll
+                        for (int i = 0; i < 128; ++i) x[i] *= up;
+                    }
+                }
+                if (C::Q8) {
+                    // y = x * (scale log2(e) ks) + log2 vs
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const uint4 f = lds128(f_at + 16 * i), lv = lds128(lv_at + 16 * i);
+                        x[4 * i] = fmaf(x[4 * i], __uint_as_float(f.x), __uint_as_float(lv.x));
+                        x[4 * i + 1] = fmaf(x[4 * i + 1], __uint_as_float(f.y), __uint_as_float(lv.y));
+                        x[4 * i + 2] = fmaf(x[4 * i + 2], __uint_as_float(f.z), __uint_as_float(lv.z));
+                        x[4 * i + 3] = fmaf(x[4 * i + 3], __uint_as_float(f.w), __uint_as_float(lv.w));
+                    }
+                }
+                if (__any_sync(FULL, j0 < see_lo || j0 + STEP > see_hi)) {
+                    const int first = see_lo - j0, end = see_hi - j0;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i < first || i >= end) x[i] = -INFINITY;
+                }
+                float top = fmaxf(x[0], x[1]);
+#pragma unroll
+                for (int i = 2; i < 128; i += 2) top = max3(top, x[i], x[i + 1]);
+                if (!C::Q8) top *= c;
+                if (b == 0) {
+                    m = top - LIFT<M>;
+                } else if (__any_sync(FULL, top > m + (GROWTH + LIFT<M>))) {
+                    // the products up to the previous step are complete (this step's score was issued after them)
+                    const float mn = fmaxf(m, top - LIFT<M>);
+                    const float by = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
+                    m = mn;
+                    l *= by;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint32_t o[32];
+                        tmem_load32(o_tm + 32 * i, o);
+                        tmem_wait_load();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                        tmem_store32(o_tm + 32 * i, o);
+                    }
+                }
+                const float ms = m == -INFINITY ? 0.0f : m;
+                float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float e[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float v = x[32 * q + 2 * i + k];
+                            e[k] = exp2_fast(C::Q8 ? v - ms : fmaf(v, c, -ms));
+                        }
+                        if (C::Q8) {
+                            const uint4 iv = lds128(iv_at + (32 * q + 2 * i) * 4);
+                            sum0 = fmaf(e[0], __uint_as_float(iv.x), sum0);
+                            sum1 = fmaf(e[1], __uint_as_float(iv.y), sum1);
+                            sum0 = fmaf(e[2], __uint_as_float(iv.z), sum0);
+                            sum1 = fmaf(e[3], __uint_as_float(iv.w), sum1);
+                        } else {
+                            sum0 += e[0]; sum1 += e[1]; sum0 += e[2]; sum1 += e[3];
+                        }
+                        p[i] = Pair<M>::pack(e[0], e[1]);
+                        p[i + 1] = Pair<M>::pack(e[2], e[3]);
+                    }
+                    tmem_store16(s_tm + 16 * q, p);
+                }
+                l += sum0 + sum1;
+                tmem_wait_store();
+                if (!C::Q8 && h == 0 && (j0 < cur.t.kb || j0 + STEP > cur.t.ke)) {
+                    // rows of V outside the visible tokens may hold anything, and 0 * NaN is NaN: clear them
+                    const long long item = 2 * block + 1;
+                    const int stage = (int)(item % C::STAGES);
+                    if (!bar_wait(kv_full(stage), (uint32_t)(item / C::STAGES) & 1, gave_up)) { ok = false; break; }
+                    if (j0 + row < cur.t.kb || j0 + row >= cur.t.ke) {
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                st_shared16(ring + stage * C::TILE_BYTES + half * BLOCK_BYTES + row * 128 + i * 16, make_uint4(0, 0, 0, 0));
+                    }
+                    fence_async_smem();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_ready(h));
+            }
+            if (!ok) break;
+            // --- output ---
+            if (!bar_wait(o_done(h), o_phase, gave_up)) { ok = false; break; }
+            o_phase ^= 1;
+            tc_fence_after();
+            const bool whole = seg.starts && seg.ends;
+            const int slot = 2 * w + (seg.starts ? 1 : 0);
+            const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+            T* dst = reinterpret_cast<T*>(a.out) + (long long)(cur.q.off + tok) * a.o_tok + (long long)hd * a.o_head;
+            const long long prow = (long long)slot * ROWS + h * HALF + row;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                uint32_t o[32];
+                tmem_load32(o_tm + 32 * i, o);
+                tmem_wait_load();
+                if (!there) continue;
+                if (whole) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint4 v;
+                        uint32_t* vw = &v.x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            vw[e] = Pair<T>::pack(__uint_as_float(o[8 * k + 2 * e]) * by, __uint_as_float(o[8 * k + 2 * e + 1]) * by);
+                        *reinterpret_cast<uint4*>(dst + 32 * i + 8 * k) = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *reinterpret_cast<uint4*>(part + prow * D + 32 * i + 4 * k) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                }
+            }
+            if (there) {
+                if (whole) {
+                    if (a.lse)
+                        a.lse[(long long)(cur.q.off + tok) * a.n_heads + hd] =
+                            l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+                } else {
+                    state[prow] = RowState{m, l, m, 0.0f};
+                }
+            }
+            if (!whole && seg.starts && h == 0 && row == 0) {
+                const long long end = at + (cur.t.steps - cur.step);
+                meta[w] = Partial{cur.seq, cur.head, cur.tile, (int)((end * sh.active - 1) / sh.total)};
+            }
+            tc_fence_before();
+            at += seg.blocks;
+            if (at < hi) list.next(cur);
+        }
+        if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
+    } else {
+        if (C::Q8) {
+            if (warp >= 12) fewer_registers<104>(); else fewer_registers<72>();
+        } else {
+            fewer_registers<72>();
+        }
+        if (warp == 8 && !C::Q8) {
+            // ================================ K and V by TMA ================================
+            const int box = min(STEP, 1 << a.kv.page_shift), pieces = STEP / box;
+            long long item = 0;
+            for (long long at = lo; at < hi;) {
+                const Segment seg = segment(at);
+                bool ok = true;
+                for (int b = 0; b < seg.blocks && ok; ++b) {
+                    const int j0 = cur.t.k0 + (cur.step + b) * STEP, j = j0 + lane * box;
+                    int page = a.kv.n_pages;                            // past the pool: TMA fills with zeros
+                    if (lane < pieces && j < cur.t.ke && j + box > cur.t.kb) {
+                        const int p = __ldg(a.kv.table + (long long)cur.seq * a.kv.table_stride + (j >> a.kv.page_shift));
+                        if ((unsigned)p < (unsigned)a.kv.n_pages) page = p;
+                        else if (a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_INVALID);
+                    }
+                    for (int kv = 0; kv < 2; ++kv, ++item) {
+                        const int stage = (int)(item % C::STAGES);
+                        const uint32_t round = (uint32_t)(item / C::STAGES);
+                        if (!bar_wait(kv_free(stage), (round & 1) ^ 1, gave_up)) { ok = false; break; }
+                        if (lane == 0) bar_expect(kv_full(stage), C::TILE_BYTES);
+                        __syncwarp();
+                        if (lane < pieces) {
+#pragma unroll
+                            for (int half = 0; half < D / 64; ++half)
+                                asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                                             :: "r"(ring + stage * C::TILE_BYTES + half * BLOCK_BYTES + lane * box * 128),
+                                                "l"(kv ? &v_map : &k_map), "r"(half * 64), "r"(j & ((1 << a.kv.page_shift) - 1)), "r"(cur.head), "r"(page),
+                                                "r"(kv_full(stage)) : "memory");
+                        }
+                    }
+                }
+                if (!ok) break;
+                at += seg.blocks;
+                if (at < hi) list.next(cur);
+            }
+            // leave only when every copy has landed
+            for (long long i = item > C::STAGES ? item - C::STAGES : 0; i < item; ++i) {
+                const unsigned long long t0 = now_ns();
+                while (!bar_try(kv_full((int)(i % C::STAGES)), (uint32_t)(i / C::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
+            }
+        } else if (warp == 9) {
+            // ================================ the products ================================
+            constexpr uint32_t QK = instr_desc(BF16, false, STEP), PV = instr_desc(BF16, true, D);
+            uint32_t q_phase = 0, p_phase[2] = {0, 0};
+            long long item = 0;                                         // ring items consumed
+            bool ok = true, issued = false;
+            auto product_qk = [&](int h, int stage) {
+                const uint64_t qa = smem_desc(q_smem + h * C::Q_BYTES, 16), kb = smem_desc(ring + stage * C::TILE_BYTES, 16);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint64_t step = (uint64_t)(((k >> 2) * BLOCK_BYTES + (k & 3) * 32) >> 4);
+                    mma_ss(tmem + h * 128, qa + step, kb + step, QK, k > 0);
+                }
+                tc_commit(s_full(h));
+            };
+            auto product_pv = [&](int h, int stage, bool add) {
+                const uint64_t vb = smem_desc(ring + stage * C::TILE_BYTES, BLOCK_BYTES);
+#pragma unroll
+                for (int k = 0; k < STEP / 16; ++k)
+                    mma_ts(tmem + 256 + h * D, tmem + h * 128 + 8 * k, vb + (uint64_t)((k * 16 * 128) >> 4), PV, add || k > 0);
+            };
+            for (long long at = lo; at < hi && ok;) {
+                const Segment seg = segment(at);
+                const int halves = cur.t.rows > HALF ? 2 : 1;
+                for (int h = 0; h < 2 && ok; ++h) ok = bar_wait(q_full(h), q_phase, gave_up);
+                q_phase ^= 1;
+                if (ok) ok = bar_wait(kv_full((int)(item % C::STAGES)), (uint32_t)(item / C::STAGES) & 1, gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                if (lane == 0) {
+                    issued = true;
+                    for (int h = 0; h < halves; ++h) product_qk(h, (int)(item % C::STAGES));
+                    tc_commit(kv_free((int)(item % C::STAGES)));
+                    if (seg.blocks == 1) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
+                }
+                __syncwarp();
+                for (int b = 0; b < seg.blocks; ++b) {
+                    const long long vi = item + 1, ki = item + 2;
+                    const bool more = b + 1 < seg.blocks;
+                    ok = bar_wait(kv_full((int)(vi % C::STAGES)), (uint32_t)(vi / C::STAGES) & 1, gave_up);
+                    if (ok && more) ok = bar_wait(kv_full((int)(ki % C::STAGES)), (uint32_t)(ki / C::STAGES) & 1, gave_up);
+                    if (!ok) break;
+                    for (int h = 0; h < halves; ++h) {
+                        ok = bar_wait(p_ready(h), p_phase[h], gave_up);
+                        if (!ok) break;
+                        p_phase[h] ^= 1;
+                        tc_fence_after();
+                        if (lane == 0) {
+                            product_pv(h, (int)(vi % C::STAGES), b > 0);
+                            if (more) product_qk(h, (int)(ki % C::STAGES)); else tc_commit(o_done(h));
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (lane == 0) {
+                        tc_commit(kv_free((int)(vi % C::STAGES)));
+                        if (more) tc_commit(kv_free((int)(ki % C::STAGES)));
+                        if (b + 2 == seg.blocks) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
+                    }
+                    __syncwarp();
+                    item += 2;
+                }
+                at += seg.blocks;
+                if (at < hi) list.next(cur);
+            }
+            // nothing of this warp's is in flight when the tensor memory is given back
+            if (issued && lane == 0) {
+                tc_commit(drain);
+                const unsigned long long t0 = now_ns();
+                while (!bar_try(drain, 0) && now_ns() - t0 < WAIT_NS) {}
+            }
+            __syncwarp();
+        } else if (warp == 10 || warp == 11) {
+            // ================================ queries ================================
+            constexpr int CH = D / 8;                                   // 16-byte chunks of a row
+            const int h = warp - 10;
+            const uint32_t dst = q_smem + h * C::Q_BYTES;
+            const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;   // the softmax works with |scale|
+            uint32_t phase = 1, q_buf = 0;                              // the first wait falls through
+            for (long long at = lo; at < hi;) {
+                const Segment seg = segment(at);
+                if (!bar_wait(q_free(h), phase, gave_up)) break;
+                phase ^= 1;
+#pragma unroll 8
+                for (int i = 0; i < HALF * CH / 32; ++i) {
+                    const int id = i * 32 + lane, r = id / CH, ch = id % CH;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (h * HALF + r < cur.t.rows) {
+                        const int pr = cur.tile * ROWS + h * HALF + r, tok = pr / a.group, hd = cur.head * a.group + pr - tok * a.group;
+                        v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + (long long)(cur.q.off + tok) * a.q_tok +
+                                                                 (long long)hd * a.q_head + ch * 8));
+                    }
+                    uint32_t x[4] = {v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
+                    if (C::Q_RANGE) {
+                        // a row whose largest element is outside [2^-6, 2^15) is brought to [2^13, 2^14) by a power of two
+                        float2 f[4];
+                        float top = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            f[k] = Pair<T>::unpack(x[k]);
+                            top = fmaxf(top, fmaxf(fabsf(f[k].x), fabsf(f[k].y)));
+                        }
+#pragma unroll
+                        for (int d = CH / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
+                        const int ex = (int)(__float_as_uint(top) >> 23);
+                        const int sh = ex >= 27 && ex < 254 && (ex < 121 || ex >= 142) ? 140 - ex : 0;
+                        const float up = __uint_as_float((uint32_t)(127 + sh) << 23);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[k] = Pair<__half>::pack(f[k].x * up, f[k].y * up);
+                        if (ch == 0)
+                            asm volatile("st.shared.f32 [%0], %1;" :: "r"(q_scales + (q_buf * ROWS + h * HALF + r) * 4),
+                                         "f"(__uint_as_float((uint32_t)(127 - sh) << 23)) : "memory");
+                    }
+                    st_shared16(dst + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16, make_uint4(x[0], x[1], x[2], x[3]));
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(q_full(h));
+                q_buf ^= 1;
+                at += seg.blocks;
+                if (at < hi) list.next(cur);
+            }
+        } else if (C::Q8 && warp >= 12) {
+            // ================================ K and V of an 8-bit cache ================================
+            // A thread has 16 codes (one 16-byte load) of LANES-th of the rows; the next K or V is on its way from
+            // global memory while this one is turned into fp16.
+            constexpr int LANES = D / 16, PASSES = LANES, PER_PASS = 128 / LANES;
+            const int tid = (int)threadIdx.x - 384, sub = tid % LANES, row0 = tid / LANES;
+            const float c = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
+            uint4 kc[PASSES], vc[PASSES];
+            float ks = 0.0f, vs = 0.0f;
+            bool seen = false;
+            auto page_of = [&](int j) {                                 // -1: no such token, or no such page
+                if (j < cur.t.kb || j >= cur.t.ke) return -1;
+                const int p = __ldg(a.kv.table + (long long)cur.seq * a.kv.table_stride + (j >> a.kv.page_shift));
+                if ((unsigned)p < (unsigned)a.kv.n_pages) return p;
+                if (a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_INVALID);
+                return -1;
+            };
+            const int in_page = (1 << a.kv.page_shift) - 1;
+            auto fetch = [&](const unsigned char* src, int step, uint4 (&x)[PASSES]) {
+                const int j0 = cur.t.k0 + step * STEP;
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) {
+                    const int j = j0 + i * PER_PASS + row0, p = page_of(j);
+                    x[i] = make_uint4(0, 0, 0, 0);
+                    if (p >= 0) x[i] = __ldg(reinterpret_cast<const uint4*>(src + page_elem(a.kv, p, cur.head, j & in_page) + sub * 16));
+                }
+            };
+            auto fetch_scales = [&](int step) {
+                const int j = cur.t.k0 + step * STEP + tid, p = page_of(j);
+                seen = p >= 0;
+                if (seen) {
+                    const long long e = scale_elem(a.kv, p, cur.head, j & in_page);
+                    ks = __ldg(a.kv.k_scale + e);
+                    vs = __ldg(a.kv.v_scale + e);
+                }
+            };
+            auto convert = [&](int stage, const uint4 (&x)[PASSES]) {
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) {
+                    const int r = i * PER_PASS + row0;
+                    const uint4 lo4 = make_uint4(codes_to_half2<FMT>(x[i].x), codes_to_half2<FMT>(x[i].x >> 16),
+                                                 codes_to_half2<FMT>(x[i].y), codes_to_half2<FMT>(x[i].y >> 16));
+                    const uint4 hi4 = make_uint4(codes_to_half2<FMT>(x[i].z), codes_to_half2<FMT>(x[i].z >> 16),
+                                                 codes_to_half2<FMT>(x[i].w), codes_to_half2<FMT>(x[i].w >> 16));
+                    // lanes 4-7 of a row go to the other block of the tile: they store their chunks the other way
+                    // round, so that eight lanes always fill eight different chunk positions
+                    const bool swap = sub & 4;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int ch = sub * 2 + (swap ? 1 - e : e);
+                        st_shared16(ring + stage * C::TILE_BYTES + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16,
+                                    (e == 0) != swap ? lo4 : hi4);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(kv_full(stage));
+            };
+            long long item = 0, block = 0;
+            long long at = lo;
+            if (at < hi) {
+                fetch_scales(cur.step);
+                fetch(a.kv.k, cur.step, kc);
+            }
+            while (at < hi) {
+                const int step = cur.step;
+                fetch(a.kv.v, step, vc);
+                int stage = (int)(item % C::STAGES);
+                if (!bar_wait(kv_free(stage), ((uint32_t)(item / C::STAGES) & 1) ^ 1, gave_up)) break;
+                const uint32_t sc = scales + (uint32_t)(block % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
+                // a V scale below 2^-80 counts as 2^-80 (of a vector of zeros, whose scale does not matter, or of values below 1e-21)
+                const float v1 = fmaxf(vs, 8.2718061e-25f);
+                const float f = seen ? c * ks : 0.0f, lv = seen ? (vs != vs ? vs : __log2f(v1)) : -INFINITY, iv = seen ? 1.0f / v1 : 0.0f;
+                asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc), "f"(f) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + STEP * 4), "f"(lv) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + 2 * STEP * 4), "f"(iv) : "memory");
+                convert(stage, kc);
+                ++item; ++block; ++at;
+                if (++cur.step == cur.t.steps && at < hi) list.next(cur);
+                if (at < hi) {
+                    fetch_scales(cur.step);
+                    fetch(a.kv.k, cur.step, kc);
+                }
+                stage = (int)(item % C::STAGES);
+                if (!bar_wait(kv_free(stage), ((uint32_t)(item / C::STAGES) & 1) ^ 1, gave_up)) break;
+                convert(stage, vc);
+                ++item;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
+}
+
+// Tensor map of k or v: {head_dim, row in page, KV head, page}, boxes of 64 elements by (part of) a page.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+    static EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+bool make_map(CUtensorMap* map, const KvView& c, void* base) {
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const int page = 1 << c.page_shift;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)page, (cuuint64_t)c.n_kv, (cuuint64_t)c.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.head_dim * 2, (cuuint64_t)page * c.head_dim * 2, (cuuint64_t)c.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(page < STEP ? page : STEP), 1, 1}, one[4] = {1, 1, 1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int FMT, int D>
+cudaError_t run(const AttnView& a, int min_rows, Partial* meta, RowState* state, float* part, cudaStream_t st) {
+    using C = Cfg<T, FMT, D>;
+    cudaError_t e = allow_max_dynamic_smem(reinterpret_cast<const void*>(&k_attn_chunk<T, FMT, D>));
+    if (e != cudaSuccess) return e;
+    CUtensorMap km = {}, vm = {};
+    if (!C::Q8 && (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v))) return cudaErrorInvalidValue;
+    launch_hook("k_attn_chunk", 0, st);
+    k_attn_chunk<T, FMT, D><<<attn_chunk_workers(), C::THREADS, C::SMEM, st>>>(a, km, vm, min_rows, meta, state, part);
+    launch_hook("k_attn_chunk", 1, st);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, attn_chunk_workers(), meta, state,
+                               part, st);
+}
+
+}  // namespace
+
+int attn_chunk_workers() { return 148; }
+
+cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state, float* part,
+                              cudaStream_t st) {
+    return kv_dispatch(type, format, a.kv.head_dim, [&](auto t, auto f, auto d) {
+        return run<typename decltype(t)::type, decltype(f)::value, decltype(d)::value>(a, min_rows, meta, state, part, st);
+    });
+}
+
+}  // namespace hos

@@ -16,6 +16,7 @@
 //   - 8-bit codes become fp16 exactly; K's scale multiplies the score, V's scale joins the exponent of
 //     the weight (w_j = exp2(x_j + log2 vs_j - max of that)), so no weight under- or overflows fp16
 //     whatever the scales are.
+#include "hos_attn_list.cuh"
 #include "hos_kernels.h"
 #include "hos_kv.cuh"
 
@@ -23,6 +24,8 @@ namespace hos {
 namespace {
 
 constexpr int ROWS = 16, STEP = 16, WARPS = 4;
+using List = AttnList<ROWS, STEP>;
+using Cursor = List::Cursor;
 constexpr int MIN_STEPS = 2;                  // a worker's smallest share; fewer and the joining costs more than it saves
 
 template <typename T, int FMT, int D> struct Cfg {
@@ -35,6 +38,9 @@ template <typename T, int FMT, int D> struct Cfg {
     static constexpr int CTAS = Q8 ? 2 : 2;
     static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
+// A row's weights are 2^(x - (maximum - LIFT)): in fp16 the largest is 2^14, so that small ones keep their bits
+// down to 2^-28 of it.
+template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 14.0f : 0.0f;
 template <typename T, int FMT> struct MatType { using type = __half; };
 template <typename T> struct MatType<T, HOS_KV_SAME> { using type = T; };
 
@@ -42,98 +48,6 @@ template <typename T> struct MatType<T, HOS_KV_SAME> { using type = T; };
 // chunks of two neighbouring rows; the same chunk pair of every second row) over the banks.
 template <int CHUNKS> __device__ __forceinline__ int swizzle(int r) {
     return CHUNKS == 4 ? (r >> 1) & 3 : (((r >> 1) & 1) << 1) | ((((r >> 2) ^ r) & 1) << 2);
-}
-
-struct Tile { int k0, kb, ke, steps, rows; };  // steps of 16 tokens from k0; tokens [kb, ke) are seen by some row
-
-__device__ __forceinline__ Tile tile_of(const AttnView& a, const SeqInfo& q, int tile) {
-    Tile t;
-    const int first = tile * ROWS, total = q.n * a.group;
-    t.rows = min(ROWS, total - first);
-    const int base = q.len - q.n;
-    t.ke = a.causal ? min(q.len, base + (first + t.rows - 1) / a.group + 1) : q.len;
-    t.ke = max(t.ke, 0);
-    t.kb = a.window > 0 ? max(0, min(base + first / a.group - a.window + 1, t.ke)) : 0;
-    t.k0 = t.kb & ~(STEP - 1);
-    t.steps = max(1, (t.ke - t.k0 + STEP - 1) / STEP);
-    return t;
-}
-__device__ __forceinline__ int tiles_of(const AttnView& a, const SeqInfo& q) { return (q.n * a.group + ROWS - 1) / ROWS; }
-
-__device__ __forceinline__ bool mine(const AttnView& a, const SeqInfo& q, int max_rows) {
-    return q.n > 0 && (long long)q.n * a.group <= max_rows;
-}
-// Steps of one KV head of a sequence.
-__device__ __forceinline__ long long seq_steps(const AttnView& a, const SeqInfo& q, int max_rows) {
-    if (!mine(a, q, max_rows)) return 0;
-    long long sum = 0;
-    const int nt = tiles_of(a, q);
-    for (int t = 0; t < nt; ++t) sum += tile_of(a, q, t).steps;
-    return sum;
-}
-__device__ __forceinline__ long long warp_scan(long long v) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long w = __shfl_up_sync(FULL, v, d);
-        if (lane_id() >= d) v += w;
-    }
-    return v;
-}
-
-struct Cursor {
-    int seq, head, tile, tiles, step;
-    SeqInfo q;
-    Tile t;
-};
-// To the next tile of the list (the caller knows that there is one).
-__device__ __forceinline__ void next_tile(const AttnView& a, int max_rows, Cursor& c) {
-    c.step = 0;
-    if (++c.tile == c.tiles) {
-        c.tile = 0;
-        if (++c.head == a.kv.n_kv) {
-            c.head = 0;
-            do {
-                if (++c.seq >= a.kv.n_seq) { c.seq = a.kv.n_seq - 1; break; }
-                c.q = load_seq(a.kv, c.seq, false);
-            } while (!mine(a, c.q, max_rows));
-            c.tiles = tiles_of(a, c.q);
-        }
-    }
-    c.t = tile_of(a, c.q, c.tile);
-}
-
-// Finds step number `at` of the list.
-__device__ __forceinline__ Cursor locate(const AttnView& a, int max_rows, long long at) {
-    Cursor c;
-    long long before = 0;
-    c.seq = 0;
-    for (int s0 = 0; s0 < a.kv.n_seq; s0 += 32) {
-        const int s = s0 + lane_id();
-        const long long cost = s < a.kv.n_seq ? seq_steps(a, load_seq(a.kv, s, false), max_rows) * a.kv.n_kv : 0;
-        const long long scan = warp_scan(cost);
-        const unsigned hit = __ballot_sync(FULL, before + scan > at);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            c.seq = s0 + l;
-            before += __shfl_sync(FULL, scan - cost, l);
-            break;
-        }
-        before += __shfl_sync(FULL, scan, 31);
-    }
-    c.q = load_seq(a.kv, c.seq, false);
-    c.tiles = tiles_of(a, c.q);
-    const long long per_head = seq_steps(a, c.q, max_rows);
-    long long rest = at - before;
-    c.head = (int)(rest / per_head);
-    rest -= (long long)c.head * per_head;
-    c.tile = 0;
-    c.t = tile_of(a, c.q, 0);
-    while (rest >= c.t.steps) {
-        rest -= c.t.steps;
-        c.t = tile_of(a, c.q, ++c.tile);
-    }
-    c.step = (int)rest;
-    return c;
 }
 
 template <typename T, int FMT, int D>
@@ -151,17 +65,15 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     pdl_launch_dependents();
 
     // this warp's share of the list
-    long long total = 0;
-    for (int s = lane; s < a.kv.n_seq; s += 32)
-        total += seq_steps(a, load_seq(a.kv, s, w == 0), max_rows) * a.kv.n_kv;
-    total = (long long)warp_sum_u64((unsigned long long)total);
+    const List list{a, 0, max_rows};
+    const long long total = list.total(w == 0);
     const int active = (int)min((long long)workers, (total + MIN_STEPS - 1) / MIN_STEPS);
     if (w >= active) {
         if (lane == 0) meta[w].last = -1;
         return;
     }
     const long long lo = total * w / active, hi = total * (w + 1) / active;
-    Cursor cons = locate(a, max_rows, lo);
+    Cursor cons = list.locate(lo);
     Cursor prod = cons;
     int to_issue = (int)(hi - lo);
     const uint32_t ring = smem_u32(smem) + warp_id() * C::STAGES * C::STAGE;
@@ -203,7 +115,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 cp_async16(vd + C::KV_BYTES + lane * 16, (lane < 4 ? a.kv.k_scale : a.kv.v_scale) + se, page >= 0);
             }
             if (++prod.step == prod.t.steps && to_issue > 0) {
-                next_tile(a, max_rows, prod);
+                list.next(prod);
                 pages_at = -1;
             }
         }
@@ -391,7 +303,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
             float top = fmaxf(fmaxf(x[0][2 * h], x[0][2 * h + 1]), fmaxf(x[1][2 * h], x[1][2 * h + 1]));
             top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
             top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
-            const float mn = fmaxf(m[h], top), ms = mn == -INFINITY ? 0.0f : mn;
+            const float mn = fmaxf(m[h], C::Q8 ? top : top - LIFT<M>), ms = mn == -INFINITY ? 0.0f : mn;
             shrink[h] = exp2_fast(m[h] - ms);
             m[h] = mn;
             float p[4], sum = 0.0f;
@@ -408,7 +320,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 }
                 ty = fmaxf(ty, __shfl_xor_sync(FULL, ty, 1));
                 ty = fmaxf(ty, __shfl_xor_sync(FULL, ty, 2));
-                const float yn = fmaxf(mt[h], ty), ys = yn == -INFINITY ? 0.0f : yn;
+                const float yn = fmaxf(mt[h], ty - LIFT<M>), ys = yn == -INFINITY ? 0.0f : yn;
                 shrink[h] = exp2_fast(mt[h] - ys);
                 mt[h] = yn;
 #pragma unroll
@@ -471,7 +383,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
         if (tile_done || unit + 1 == hi) {
             finish(unit);
             if (unit + 1 < hi) {
-                next_tile(a, max_rows, cons);
+                list.next(cons);
                 seg_first = 0;
                 begin();
             }
@@ -481,67 +393,6 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     }
     if (!open_end && lane == 0) meta[w].last = -1;
     cp_async_wait<0>();
-}
-
-// Joins the pieces of the tiles that k_attn_rows' shares cut: block w has the tile that begins in worker
-// w's share and ends in a later one's; the pieces are slot 1 of w and slot 0 of the workers up to `last`.
-constexpr int COMBINE_WARPS = 8;
-template <typename T, int D>
-__global__ void __launch_bounds__(COMBINE_WARPS * 32) k_attn_combine(const __grid_constant__ AttnView a, const Partial* __restrict__ meta,
-                                                                    const RowState* __restrict__ state,
-                                                                    const float* __restrict__ part) {
-    pdl_wait();
-    const int w = (int)blockIdx.x;
-    const Partial p = meta[w];
-    if (p.last < 0) return;
-    constexpr int PER = D / 32;                // elements a lane
-    const SeqInfo q = load_seq(a.kv, p.seq, false);
-    const int rows = min(ROWS, q.n * a.group - p.tile * ROWS);
-    for (int r = warp_id(); r < rows; r += COMBINE_WARPS) {
-        // row state i of the pieces: slot 2w + 1, then 2(w + 1), 2(w + 2), ...
-        auto slot = [&](int i) { return (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * ROWS + r; };
-        const int n = p.last - w + 1;
-        float m = -INFINITY;
-        for (int i = lane_id(); i < n; i += 32) m = fmaxf(m, state[slot(i)].m);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, d));
-        const float ms = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f, o[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            float by = 0.0f;
-            if (i0 + lane_id() < n) {
-                const RowState st = state[slot(i0 + lane_id())];
-                l += st.l * exp2f(st.m - ms);
-                by = st.mt == -INFINITY ? 0.0f : exp2f(st.mt - ms);
-            }
-            const int some = min(32, n - i0);
-#pragma unroll 8
-            for (int i = 0; i < some; ++i) {
-                const float b = __shfl_sync(FULL, by, i);
-                const float* src = part + slot(i0 + i) * D + lane_id() * PER;
-                if (PER == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(src);
-                    o[0] += b * v.x; o[1] += b * v.y; o[PER - 2] += b * v.z; o[PER - 1] += b * v.w;
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
-                    o[0] += b * v.x; o[1] += b * v.y;
-                }
-            }
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(FULL, l, d);
-        const float by = l == 0.0f ? 0.0f : 1.0f / l;
-        const int row = p.tile * ROWS + r, tok = q.off + row / a.group, hd = p.head * a.group + row % a.group;
-        T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head + lane_id() * PER;
-        if (PER == 4)
-            *reinterpret_cast<uint2*>(dst) = make_uint2(Pair<T>::pack(o[0] * by, o[1] * by), Pair<T>::pack(o[PER - 2] * by, o[PER - 1] * by));
-        else
-            *reinterpret_cast<uint32_t*>(dst) = Pair<T>::pack(o[0] * by, o[1] * by);
-        if (a.lse && lane_id() == 0)
-            a.lse[(long long)tok * a.n_heads + hd] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
-    }
 }
 
 template <typename T, int FMT, int D>
@@ -555,19 +406,8 @@ cudaError_t run(const AttnView& a, int max_rows, Partial* meta, RowState* state,
     k_attn_rows<T, FMT, D><<<ctas, WARPS * 32, C::SMEM, st>>>(a, max_rows, meta, state, part);
     launch_hook("k_attn_rows", 1, st);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)attn_rows_workers());
-    cfg.blockDim = dim3(COMBINE_WARPS * 32);
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    launch_hook("k_attn_combine", 0, st);
-    e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D>, a, (const Partial*)meta, (const RowState*)state, (const float*)part);
-    launch_hook("k_attn_combine", 1, st);
-    return e;
+    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, attn_rows_workers(), meta,
+                               state, part, st);
 }
 
 }  // namespace

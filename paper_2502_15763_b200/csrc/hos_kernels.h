@@ -98,5 +98,10 @@ cudaError_t launch_kv_read(const KvView& c, int type, int format, void* k, void*
 int attn_rows_workers();
 cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int max_rows, Partial* meta, RowState* state,
                              float* part, cudaStream_t st);
+int attn_chunk_workers();
+cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state,
+                              float* part, cudaStream_t st);
+cudaError_t launch_attn_combine(const AttnView& a, int type, int rows, int workers, const Partial* meta, const RowState* state,
+                                const float* part, cudaStream_t st);
 
 }  // namespace hos

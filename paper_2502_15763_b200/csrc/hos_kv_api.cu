@@ -1,4 +1,5 @@
 // C-ABI layer of the KV-cache calls: argument validation, workspace carving, kernel sequencing.
+#include <algorithm>
 #include <cmath>
 
 #include "hos_kernels.h"
@@ -66,6 +67,8 @@ KvView view(const hos_kv_cache* c, const hos_kv_batch* b, int32_t* status) {
 
 inline int cuda_rc(cudaError_t e) { return e == cudaSuccess ? HOS_OK : HOS_E_CUDA; }
 
+constexpr int ROW_TILE = 16;                 // rows of a tile of the row kernel
+
 struct AttnWs {
     Partial* meta;
     RowState* state;
@@ -76,11 +79,13 @@ AttnWs carve_attention(int head_dim, void* ws) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     AttnWs w;
     unsigned char* base = static_cast<unsigned char*>(ws);
-    const size_t n = (size_t)attn_rows_workers();
+    // the two kernels follow one another on the stream and share the space
+    const size_t n = (size_t)std::max(attn_rows_workers(), attn_chunk_workers());
+    const size_t rows = 2 * (size_t)std::max(attn_rows_workers() * 16, attn_chunk_workers() * 256);
     size_t off = 0;
     w.meta = reinterpret_cast<Partial*>(base + off);   off += up(n * sizeof(Partial));
-    w.state = reinterpret_cast<RowState*>(base + off); off += up(n * 2 * 16 * sizeof(RowState));
-    w.part = reinterpret_cast<float*>(base + off);     off += up(n * 2 * 16 * (size_t)head_dim * 4);
+    w.state = reinterpret_cast<RowState*>(base + off); off += up(rows * sizeof(RowState));
+    w.part = reinterpret_cast<float*>(base + off);     off += up(rows * (size_t)head_dim * 4);
     w.bytes = off;
     return w;
 }
@@ -145,8 +150,12 @@ int hos_paged_attention(const hos_kv_cache* c, const hos_kv_batch* b, const void
     a.scale_log2 = sm_scale * 1.44269504088896340736f;
     a.causal = causal != 0;
     a.window = window;
-    return cuda_rc(launch_attn_rows(a, c->type, c->format, 0x7FFFFFFF, w.meta, w.state, w.part,
-                                    static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // Sequences of more rows than one tile of the row kernel go to the chunk kernel (all, if there is but one).
+    const bool chunks = (long long)b->max_new * a.group > ROW_TILE, alone = b->n_seq == 1;
+    if (chunks && (rc = cuda_rc(launch_attn_chunk(a, c->type, c->format, alone ? 0 : ROW_TILE, w.meta, w.state, w.part, st)))) return rc;
+    if (chunks && alone) return HOS_OK;
+    return cuda_rc(launch_attn_rows(a, c->type, c->format, chunks ? ROW_TILE : 0x7FFFFFFF, w.meta, w.state, w.part, st));
 }
 
 }  // extern "C"
