@@ -11,10 +11,10 @@
 // While one half's S is turned into P by its four warps (one thread a row, no shuffles), the tensor cores have the other
 // half's products.
 //   warps 0-3, 4-7   softmax, output of half 0, 1
-//   warp 8           K and V of a 16-bit cache into a ring of shared memory by TMA, page by page
+//   warp 8           K and V into a ring of shared memory by TMA, page by page
 //   warp 9           issues the products
 //   warps 10, 11     the rows of the next tile's queries, half 0, 1
-//   warps 12-15      (8-bit cache) codes to fp16 on their way from global to shared memory
+//   warps 12-15      (8-bit cache) turn the codes of a stage into fp16, in place
 // An 8-bit cache's K scale multiplies the score, its V scale joins the exponent: y_j = x_j + log2 vs_j, the weights 2^(y_j - m)
 // meet the bare codes and are safe in fp16 whatever the scales are, and l = sum 2^(y_j - m) / vs_j.
 //
@@ -67,23 +67,22 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-constexpr unsigned long long WAIT_NS = 2000000000ull;
+constexpr long long WAIT_CYCLES = 4000000000ll;        // about two seconds
 // The whole warp waits for the phase; false (for all lanes) after two seconds or once another role has given up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
     if (__all_sync(FULL, bar_try(bar, parity))) return true;
-    const unsigned long long t0 = now_ns();
-    for (;;) {
+    const uint32_t t0 = (uint32_t)(clock64() >> 16);
 #pragma unroll 1
-        for (int i = 0; i < 64; ++i)
-            if (__all_sync(FULL, bar_try(bar, parity))) return true;
-        if (now_ns() - t0 > WAIT_NS) *gave_up = 1;
+    for (;;) {
+        if (__all_sync(FULL, bar_try(bar, parity))) return true;
+        if ((uint32_t)(clock64() >> 16) - t0 > (uint32_t)(WAIT_CYCLES >> 16)) *gave_up = 1;
         if (__any_sync(FULL, *gave_up != 0)) return false;
     }
+}
+// The same for one wait at the end of a role, whatever the others do.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!bar_try(bar, parity) && clock64() - t0 < WAIT_CYCLES) {}
 }
 
 // --- tcgen05 ----------------------------------------------------------------------------------
@@ -110,10 +109,9 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* x) {
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : HOS_R8(x, 0), HOS_R8(x, 8), HOS_R8(x, 16), HOS_R8(x, 24) : "r"(addr));
 }
-__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* x) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-                 :: HOS_W8(x, 0), HOS_W8(x, 8), HOS_W8(x, 16), HOS_W8(x, 24), "r"(addr) : "memory");
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : HOS_R8(x, 0), HOS_R8(x, 8) : "r"(addr));
 }
 __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* x) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
@@ -134,6 +132,15 @@ constexpr uint32_t instr_desc(bool bf16, bool b_along_n, int n) {
            ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
+// One lane of the (converged) warp; the compiler knows that it is one, so the operands of the matrix
+// instructions stay in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(FULL, x, 0); }
+
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
 
@@ -142,15 +149,41 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// Two 32-bit floats in one instruction.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 f2_split(F2 x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void lds_f2x2(uint32_t addr, F2& a, F2& b) {
+    asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
+}
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 struct Shared {                                // in the first HEAD bytes
-    uint64_t bars[32];
+    uint64_t bars[40];
     Cursor first;
-    long long lo, hi, total, active;
+    long long lo, total, active;
+    int share;                                 // steps of this CTA
     uint32_t tmem;
     int gave_up;
 };
@@ -161,7 +194,7 @@ struct Segment { int blocks; bool starts, ends; };   // steps of the current til
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(Cfg<T, FMT, D>::THREADS, 1)
 k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-             const int min_rows, Partial* __restrict__ meta, RowState* __restrict__ state, float* __restrict__ part) {
+             const __grid_constant__ CUtensorMap q_map, const bool q_tma, const int min_rows, Partial* __restrict__ meta, RowState* __restrict__ state, float* __restrict__ part) {
     using C = Cfg<T, FMT, D>;
     using M = typename MatType<T, FMT>::type;
     constexpr bool BF16 = std::is_same<M, __nv_bfloat16>::value;
@@ -173,16 +206,18 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     const uint32_t scales = ring + C::STAGES * C::TILE_BYTES;          // [buffer][scale log2(e) ks | log2 vs | 1 / vs][token]
     const uint32_t q_scales = scales + C::SCALES;                      // [tile parity][row]: what a row of queries was divided by
     const uint32_t bar0 = smem_u32(sh.bars);
-    auto kv_full = [&](int i) { return bar0 + 8 * i; };
-    auto kv_free = [&](int i) { return bar0 + 8 * (C::STAGES + i); };
+    auto kv_full = [&](uint32_t i) { return bar0 + 8 * i; };
+    auto kv_free = [&](uint32_t i) { return bar0 + 8 * (C::STAGES + i); };
     const uint32_t bar1 = bar0 + 16 * C::STAGES;
     auto q_full = [&](int h) { return bar1 + 8 * h; };
     auto q_free = [&](int h) { return bar1 + 16 + 8 * h; };
     auto s_full = [&](int h) { return bar1 + 32 + 8 * h; };
     auto p_ready = [&](int h) { return bar1 + 48 + 8 * h; };
     auto o_done = [&](int h) { return bar1 + 64 + 8 * h; };
-    const uint32_t drain = bar1 + 80;
-    const int warp = warp_id(), lane = lane_id(), w = (int)blockIdx.x;
+    auto p_half = [&](int h) { return bar1 + 80 + 8 * h; };
+    const uint32_t drain = bar1 + 96;
+    auto raw_full = [&](uint32_t i) { return C::Q8 ? bar1 + 104 + 8 * i : kv_full(i); };   // what the copies report to
+    const int warp = uniform(warp_id()), lane = lane_id(), w = (int)blockIdx.x;
     const List list{a, min_rows, 0x7FFFFFFF};
     pdl_launch_dependents();
 
@@ -195,7 +230,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
         if (lane == 0) {
             sh.first = c;
             sh.lo = lo;
-            sh.hi = hi;
+            sh.share = (int)(hi - lo);
             sh.total = total;
             sh.active = active;
             sh.gave_up = 0;
@@ -205,11 +240,13 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
         for (int i = 0; i < C::STAGES; ++i) {
             bar_init(kv_full(i), C::Q8 ? 4 : 1);
             bar_init(kv_free(i), 1);
+            if (C::Q8) bar_init(raw_full(i), 1);
         }
         for (int h = 0; h < 2; ++h) {
             bar_init(q_full(h), 1);
             bar_init(q_free(h), 1);
             bar_init(s_full(h), 1);
+            bar_init(p_half(h), 4);
             bar_init(p_ready(h), 4);
             bar_init(o_done(h), 1);
         }
@@ -222,15 +259,14 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     }
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
-    const long long lo = sh.lo, hi = sh.hi;
+    const uint32_t tmem = (uint32_t)uniform((int)sh.tmem);
+    const int share = sh.share;
     Cursor cur = sh.first;
-    // the steps from `at` to the end of the tile or the share
-    auto segment = [&](long long at) {
+    // the steps from number `at` of the share to the end of the tile or the share
+    auto segment = [&](int at) {
         Segment s;
-        const long long left = hi - at;
-        const int rest = cur.t.steps - cur.step;
-        s.blocks = left < rest ? (int)left : rest;
+        const int left = share - at, rest = cur.t.steps - cur.step;
+        s.blocks = min(left, rest);
         s.starts = cur.step == 0;
         s.ends = s.blocks == rest;
         return s;
@@ -238,22 +274,35 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 
     if (warp < 8) {
         // ================================ softmax and output ================================
-        if (C::Q8) more_registers<168>(); else more_registers<216>();
+        if (C::Q8) more_registers<176>(); else more_registers<216>();
         const int h = warp >> 2, row = (warp & 3) * 32 + lane;         // row of this half
         const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_tm = tmem + lane_at + h * 128, o_tm = tmem + lane_at + 256 + h * D;
         const float c = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);   // positive, so that masked scores stay -inf
         uint32_t s_phase = 0, o_phase = 0;
-        long long block = 0;                                           // steps this CTA has begun: ring item 2 * block is K
+        uint32_t block = 0;                                           // steps this CTA has begun: ring item 2 * block is K
         uint32_t q_buf = 1;
         bool ok = true;
-        for (long long at = lo; at < hi && ok;) {
+        // Rows of V outside the visible tokens may hold anything, and 0 * NaN is NaN: half 0's threads clear them before
+        // either half's product (half 1's is issued later).
+        auto clear_v = [&](int j0, uint32_t item) {
+            const uint32_t stage = item % C::STAGES;
+            if (!bar_wait(kv_full(stage), (item / C::STAGES) & 1, gave_up)) return false;
+            if (j0 + row < cur.t.kb || j0 + row >= cur.t.ke) {
+#pragma unroll 1
+                for (int i = 0; i < D / 8; ++i)
+                    st_shared16(ring + stage * C::TILE_BYTES + (i >> 3) * BLOCK_BYTES + row * 128 + (i & 7) * 16, make_uint4(0, 0, 0, 0));
+            }
+            fence_async_smem();
+            return true;
+        };
+        for (int at = 0; at < share && ok;) {
             const Segment seg = segment(at);
             const bool active = cur.t.rows > h * HALF;
             q_buf ^= 1;
             if (!active) {
                 at += seg.blocks; block += seg.blocks;
-                if (at < hi) list.next(cur);
+                if (at < share) list.next(cur);
                 continue;
             }
             const int r = cur.tile * ROWS + h * HALF + row;
@@ -269,8 +318,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 const int j0 = cur.t.k0 + (cur.step + b) * STEP;
                 const int buf = C::Q8 ? (int)(block % C::SCALE_BUFS) : 0;
                 if (C::Q8) {
-                    const long long item = 2 * block;
-                    if (!bar_wait(kv_full((int)(item % C::STAGES)), (uint32_t)(item / C::STAGES) & 1, gave_up)) { ok = false; break; }
+                    const uint32_t item = 2 * block;
+                    if (!bar_wait(kv_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up)) { ok = false; break; }
                 }
                 if (!bar_wait(s_full(h), s_phase, gave_up)) { ok = false; break; }
                 s_phase ^= 1;
@@ -291,12 +340,12 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 if (C::Q8) {
                     // y = x * (scale log2(e) ks) + log2 vs
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const uint4 f = lds128(f_at + 16 * i), lv = lds128(lv_at + 16 * i);
-                        x[4 * i] = fmaf(x[4 * i], __uint_as_float(f.x), __uint_as_float(lv.x));
-                        x[4 * i + 1] = fmaf(x[4 * i + 1], __uint_as_float(f.y), __uint_as_float(lv.y));
-                        x[4 * i + 2] = fmaf(x[4 * i + 2], __uint_as_float(f.z), __uint_as_float(lv.z));
-                        x[4 * i + 3] = fmaf(x[4 * i + 3], __uint_as_float(f.w), __uint_as_float(lv.w));
+                    for (int i = 0; i < 128; i += 4) {
+                        F2 f0, f1, l0, l1;
+                        lds_f2x2(f_at + 4 * i, f0, f1);
+                        lds_f2x2(lv_at + 4 * i, l0, l1);
+                        const float2 y0 = f2_split(f2_fma(f2(x[i], x[i + 1]), f0, l0)), y1 = f2_split(f2_fma(f2(x[i + 2], x[i + 3]), f1, l1));
+                        x[i] = y0.x; x[i + 1] = y0.y; x[i + 2] = y1.x; x[i + 3] = y1.y;
                     }
                 }
                 if (__any_sync(FULL, j0 < see_lo || j0 + STEP > see_hi)) {
@@ -305,9 +354,12 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     for (int i = 0; i < 128; ++i)
                         if (i < first || i >= end) x[i] = -INFINITY;
                 }
-                float top = fmaxf(x[0], x[1]);
+                float tops[4];
 #pragma unroll
-                for (int i = 2; i < 128; i += 2) top = max3(top, x[i], x[i + 1]);
+                for (int i = 0; i < 4; ++i) tops[i] = fmaxf(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+                for (int i = 8; i < 128; i += 2) tops[(i >> 1) & 3] = max3(tops[(i >> 1) & 3], x[i], x[i + 1]);
+                float top = max3(fmaxf(tops[0], tops[1]), tops[2], tops[3]);
                 if (!C::Q8) top *= c;
                 if (b == 0) {
                     m = top - LIFT<M>;
@@ -317,59 +369,61 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     const float by = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
                     m = mn;
                     l *= by;
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t o[32];
-                        tmem_load32(o_tm + 32 * i, o);
+#pragma unroll 1
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t o[16];
+                        tmem_load16(o_tm + 16 * i, o);
                         tmem_wait_load();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
-                        tmem_store32(o_tm + 32 * i, o);
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                        tmem_store16(o_tm + 16 * i, o);
                     }
                 }
                 const float ms = m == -INFINITY ? 0.0f : m;
-                float sum0 = 0.0f, sum1 = 0.0f;
+                const F2 c2 = f2(c, c), m2 = f2(-ms, -ms);
+                F2 sums[2] = {0, 0};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        float e[4];
+                        const int j = 32 * q + 2 * i;
+                        F2 e[2];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float v = x[32 * q + 2 * i + k];
-                            e[k] = exp2_fast(C::Q8 ? v - ms : fmaf(v, c, -ms));
+                        for (int k = 0; k < 2; ++k) {
+                            const F2 v = f2(x[j + 2 * k], x[j + 2 * k + 1]);
+                            const float2 z = f2_split(C::Q8 ? f2_add(v, m2) : f2_fma(v, c2, m2));
+                            const float2 w2 = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+                            p[i + k] = Pair<M>::pack(w2.x, w2.y);
+                            e[k] = f2(w2.x, w2.y);
                         }
                         if (C::Q8) {
-                            const uint4 iv = lds128(iv_at + (32 * q + 2 * i) * 4);
-                            sum0 = fmaf(e[0], __uint_as_float(iv.x), sum0);
-                            sum1 = fmaf(e[1], __uint_as_float(iv.y), sum1);
-                            sum0 = fmaf(e[2], __uint_as_float(iv.z), sum0);
-                            sum1 = fmaf(e[3], __uint_as_float(iv.w), sum1);
+                            F2 iv0, iv1;
+                            lds_f2x2(iv_at + 4 * j, iv0, iv1);
+                            sums[0] = f2_fma(e[0], iv0, sums[0]);
+                            sums[1] = f2_fma(e[1], iv1, sums[1]);
                         } else {
-                            sum0 += e[0]; sum1 += e[1]; sum0 += e[2]; sum1 += e[3];
+                            sums[0] = f2_add(sums[0], e[0]);
+                            sums[1] = f2_add(sums[1], e[1]);
                         }
-                        p[i] = Pair<M>::pack(e[0], e[1]);
-                        p[i + 1] = Pair<M>::pack(e[2], e[3]);
                     }
                     tmem_store16(s_tm + 16 * q, p);
-                }
-                l += sum0 + sum1;
-                tmem_wait_store();
-                if (!C::Q8 && h == 0 && (j0 < cur.t.kb || j0 + STEP > cur.t.ke)) {
-                    // rows of V outside the visible tokens may hold anything, and 0 * NaN is NaN: clear them
-                    const long long item = 2 * block + 1;
-                    const int stage = (int)(item % C::STAGES);
-                    if (!bar_wait(kv_full(stage), (uint32_t)(item / C::STAGES) & 1, gave_up)) { ok = false; break; }
-                    if (j0 + row < cur.t.kb || j0 + row >= cur.t.ke) {
-#pragma unroll
-                        for (int half = 0; half < D / 64; ++half)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                st_shared16(ring + stage * C::TILE_BYTES + half * BLOCK_BYTES + row * 128 + i * 16, make_uint4(0, 0, 0, 0));
+                    if (q == 1) {
+                        // the first half of the weights may be multiplied while the second is worked out
+                        if (!C::Q8 && h == 0 && (j0 < cur.t.kb || j0 + STEP > cur.t.ke)) {
+                            ok = clear_v(j0, 2 * block + 1);
+                            if (!ok) break;
+                        }
+                        tmem_wait_store();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(p_half(h));
                     }
-                    fence_async_smem();
                 }
+                if (!ok) break;
+                const float2 sum = f2_split(f2_add(sums[0], sums[1]));
+                l += sum.x + sum.y;
+                tmem_wait_store();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_ready(h));
@@ -416,25 +470,25 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 }
             }
             if (!whole && seg.starts && h == 0 && row == 0) {
-                const long long end = at + (cur.t.steps - cur.step);
+                const long long end = sh.lo + at + (cur.t.steps - cur.step);
                 meta[w] = Partial{cur.seq, cur.head, cur.tile, (int)((end * sh.active - 1) / sh.total)};
             }
             tc_fence_before();
             at += seg.blocks;
-            if (at < hi) list.next(cur);
+            if (at < share) list.next(cur);
         }
         if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
     } else {
         if (C::Q8) {
-            if (warp >= 12) fewer_registers<104>(); else fewer_registers<72>();
+            fewer_registers<80>();
         } else {
             fewer_registers<72>();
         }
-        if (warp == 8 && !C::Q8) {
+        if (warp == 8) {
             // ================================ K and V by TMA ================================
             const int box = min(STEP, 1 << a.kv.page_shift), pieces = STEP / box;
-            long long item = 0;
-            for (long long at = lo; at < hi;) {
+            uint32_t item = 0;
+            for (int at = 0; at < share;) {
                 const Segment seg = segment(at);
                 bool ok = true;
                 for (int b = 0; b < seg.blocks && ok; ++b) {
@@ -446,35 +500,34 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         else if (a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_INVALID);
                     }
                     for (int kv = 0; kv < 2; ++kv, ++item) {
-                        const int stage = (int)(item % C::STAGES);
-                        const uint32_t round = (uint32_t)(item / C::STAGES);
+                        const int stage = item % C::STAGES;
+                        const uint32_t round = item / C::STAGES;
                         if (!bar_wait(kv_free(stage), (round & 1) ^ 1, gave_up)) { ok = false; break; }
-                        if (lane == 0) bar_expect(kv_full(stage), C::TILE_BYTES);
+                        if (lane == 0) bar_expect(raw_full(stage), C::Q8 ? C::TILE_BYTES / 2 : C::TILE_BYTES);
                         __syncwarp();
                         if (lane < pieces) {
+                            // codes land in the second half of the stage that their fp16 values will fill
 #pragma unroll
-                            for (int half = 0; half < D / 64; ++half)
+                            for (int half = 0; half < (C::Q8 ? 1 : D / 64); ++half)
                                 asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                                             :: "r"(ring + stage * C::TILE_BYTES + half * BLOCK_BYTES + lane * box * 128),
+                                             :: "r"(ring + stage * C::TILE_BYTES +
+                                                    (C::Q8 ? C::TILE_BYTES / 2 + lane * box * D : half * BLOCK_BYTES + lane * box * 128)),
                                                 "l"(kv ? &v_map : &k_map), "r"(half * 64), "r"(j & ((1 << a.kv.page_shift) - 1)), "r"(cur.head), "r"(page),
-                                                "r"(kv_full(stage)) : "memory");
+                                                "r"(raw_full(stage)) : "memory");
                         }
                     }
                 }
                 if (!ok) break;
                 at += seg.blocks;
-                if (at < hi) list.next(cur);
+                if (at < share) list.next(cur);
             }
             // leave only when every copy has landed
-            for (long long i = item > C::STAGES ? item - C::STAGES : 0; i < item; ++i) {
-                const unsigned long long t0 = now_ns();
-                while (!bar_try(kv_full((int)(i % C::STAGES)), (uint32_t)(i / C::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
-            }
+            for (uint32_t i = item > C::STAGES ? item - C::STAGES : 0; i < item; ++i) bar_drain(raw_full(i % C::STAGES), (i / C::STAGES) & 1);
         } else if (warp == 9) {
             // ================================ the products ================================
             constexpr uint32_t QK = instr_desc(BF16, false, STEP), PV = instr_desc(BF16, true, D);
             uint32_t q_phase = 0, p_phase[2] = {0, 0};
-            long long item = 0;                                         // ring items consumed
+            uint32_t item = 0;                                         // ring items consumed
             bool ok = true, issued = false;
             auto product_qk = [&](int h, int stage) {
                 const uint64_t qa = smem_desc(q_smem + h * C::Q_BYTES, 16), kb = smem_desc(ring + stage * C::TILE_BYTES, 16);
@@ -485,61 +538,66 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 }
                 tc_commit(s_full(h));
             };
-            auto product_pv = [&](int h, int stage, bool add) {
+            auto product_pv = [&](int h, int stage, bool add, int part_of) {
                 const uint64_t vb = smem_desc(ring + stage * C::TILE_BYTES, BLOCK_BYTES);
 #pragma unroll
-                for (int k = 0; k < STEP / 16; ++k)
+                for (int k = part_of * (STEP / 32); k < (part_of + 1) * (STEP / 32); ++k)
                     mma_ts(tmem + 256 + h * D, tmem + h * 128 + 8 * k, vb + (uint64_t)((k * 16 * 128) >> 4), PV, add || k > 0);
             };
-            for (long long at = lo; at < hi && ok;) {
+            for (int at = 0; at < share && ok;) {
                 const Segment seg = segment(at);
-                const int halves = cur.t.rows > HALF ? 2 : 1;
+                const int halves = uniform(cur.t.rows > HALF ? 2 : 1), blocks = uniform(seg.blocks);
                 for (int h = 0; h < 2 && ok; ++h) ok = bar_wait(q_full(h), q_phase, gave_up);
                 q_phase ^= 1;
-                if (ok) ok = bar_wait(kv_full((int)(item % C::STAGES)), (uint32_t)(item / C::STAGES) & 1, gave_up);
+                if (ok) ok = bar_wait(kv_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up);
                 if (!ok) break;
                 tc_fence_after();
-                if (lane == 0) {
-                    issued = true;
-                    for (int h = 0; h < halves; ++h) product_qk(h, (int)(item % C::STAGES));
-                    tc_commit(kv_free((int)(item % C::STAGES)));
-                    if (seg.blocks == 1) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
+                issued = true;
+                if (elect_one()) {
+                    for (int h = 0; h < halves; ++h) product_qk(h, item % C::STAGES);
+                    tc_commit(kv_free(item % C::STAGES));
+                    if (blocks == 1) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
                 }
                 __syncwarp();
-                for (int b = 0; b < seg.blocks; ++b) {
-                    const long long vi = item + 1, ki = item + 2;
-                    const bool more = b + 1 < seg.blocks;
-                    ok = bar_wait(kv_full((int)(vi % C::STAGES)), (uint32_t)(vi / C::STAGES) & 1, gave_up);
-                    if (ok && more) ok = bar_wait(kv_full((int)(ki % C::STAGES)), (uint32_t)(ki / C::STAGES) & 1, gave_up);
+                for (int b = 0; b < blocks; ++b) {
+                    const uint32_t vi = item + 1, ki = item + 2;
+                    const bool more = b + 1 < blocks;
+                    ok = bar_wait(kv_full(vi % C::STAGES), (vi / C::STAGES) & 1, gave_up);
+                    if (ok && more) ok = bar_wait(kv_full(ki % C::STAGES), (ki / C::STAGES) & 1, gave_up);
                     if (!ok) break;
                     for (int h = 0; h < halves; ++h) {
+                        // the weights come in two halves
+                        ok = bar_wait(p_half(h), p_phase[h], gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) product_pv(h, vi % C::STAGES, b > 0, 0);
+                        __syncwarp();
                         ok = bar_wait(p_ready(h), p_phase[h], gave_up);
                         if (!ok) break;
                         p_phase[h] ^= 1;
                         tc_fence_after();
-                        if (lane == 0) {
-                            product_pv(h, (int)(vi % C::STAGES), b > 0);
-                            if (more) product_qk(h, (int)(ki % C::STAGES)); else tc_commit(o_done(h));
+                        if (elect_one()) {
+                            product_pv(h, vi % C::STAGES, true, 1);
+                            if (more) product_qk(h, ki % C::STAGES); else tc_commit(o_done(h));
                         }
                         __syncwarp();
                     }
                     if (!ok) break;
-                    if (lane == 0) {
-                        tc_commit(kv_free((int)(vi % C::STAGES)));
-                        if (more) tc_commit(kv_free((int)(ki % C::STAGES)));
-                        if (b + 2 == seg.blocks) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
+                    if (elect_one()) {
+                        tc_commit(kv_free(vi % C::STAGES));
+                        if (more) tc_commit(kv_free(ki % C::STAGES));
+                        if (b + 2 == blocks) { tc_commit(q_free(0)); tc_commit(q_free(1)); }
                     }
                     __syncwarp();
                     item += 2;
                 }
                 at += seg.blocks;
-                if (at < hi) list.next(cur);
+                if (at < share) list.next(cur);
             }
             // nothing of this warp's is in flight when the tensor memory is given back
-            if (issued && lane == 0) {
+            if (issued && elect_one()) {
                 tc_commit(drain);
-                const unsigned long long t0 = now_ns();
-                while (!bar_try(drain, 0) && now_ns() - t0 < WAIT_NS) {}
+                bar_drain(drain, 0);
             }
             __syncwarp();
         } else if (warp == 10 || warp == 11) {
@@ -548,20 +606,47 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             const int h = warp - 10;
             const uint32_t dst = q_smem + h * C::Q_BYTES;
             const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;   // the softmax works with |scale|
-            uint32_t phase = 1, q_buf = 0;                              // the first wait falls through
-            for (long long at = lo; at < hi;) {
+            uint32_t phase = 1, q_buf = 0, last = 2;                             // the first wait falls through
+            for (int at = 0; at < share;) {
                 const Segment seg = segment(at);
                 if (!bar_wait(q_free(h), phase, gave_up)) break;
                 phase ^= 1;
-#pragma unroll 8
-                for (int i = 0; i < HALF * CH / 32; ++i) {
-                    const int id = i * 32 + lane, r = id / CH, ch = id % CH;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (h * HALF + r < cur.t.rows) {
-                        const int pr = cur.tile * ROWS + h * HALF + r, tok = pr / a.group, hd = cur.head * a.group + pr - tok * a.group;
-                        v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + (long long)(cur.q.off + tok) * a.q_tok +
-                                                                 (long long)hd * a.q_head + ch * 8));
+                if (q_tma) {
+                    // a row is a token's query head: 128 rows are 128 / group whole tokens
+                    if (lane == 0) {
+                        bar_expect(q_full(h), C::Q_BYTES);
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half)
+                            asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                                         :: "r"(dst + half * BLOCK_BYTES), "l"(&q_map), "r"(half * 64), "r"(cur.head * a.group),
+                                            "r"(cur.q.off + (cur.tile * ROWS + h * HALF) / a.group), "r"(q_full(h)) : "memory");
                     }
+                    __syncwarp();
+                    at += seg.blocks;
+                    if (at < share) list.next(cur);
+                    last = phase;
+                    continue;
+                }
+                constexpr int BATCH = 8;                                // loads in flight
+#pragma unroll 1
+                for (int r0 = 0; r0 < HALF; r0 += 32) {
+                  // lane l knows where row r0 + l is
+                  const int pr = cur.tile * ROWS + h * HALF + r0 + lane, tok = pr / a.group, hd = cur.head * a.group + pr - tok * a.group;
+                  const long long where = h * HALF + r0 + lane < cur.t.rows ? (long long)(cur.q.off + tok) * a.q_tok + (long long)hd * a.q_head : -1;
+#pragma unroll 1
+                  for (int i0 = 0; i0 < CH; i0 += BATCH) {
+                    uint4 batch[BATCH];
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                      const int id = (i0 + i) * 32 + lane;
+                      const long long from = __shfl_sync(FULL, where, id / CH);
+                      batch[i] = make_uint4(0, 0, 0, 0);
+                      if (from >= 0) batch[i] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + from + (id % CH) * 8));
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                    const int id = (i0 + i) * 32 + lane, r = r0 + id / CH, ch = id % CH;
+                    const uint4 v = batch[i];
                     uint32_t x[4] = {v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
                     if (C::Q_RANGE) {
                         // a row whose largest element is outside [2^-6, 2^15) is brought to [2^13, 2^14) by a power of two
@@ -584,51 +669,49 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                                          "f"(__uint_as_float((uint32_t)(127 - sh) << 23)) : "memory");
                     }
                     st_shared16(dst + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16, make_uint4(x[0], x[1], x[2], x[3]));
+                    }
+                  }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) bar_arrive(q_full(h));
                 q_buf ^= 1;
                 at += seg.blocks;
-                if (at < hi) list.next(cur);
+                if (at < share) list.next(cur);
             }
+            if (last < 2) bar_drain(q_full(h), last);                   // the last copy has landed
         } else if (C::Q8 && warp >= 12) {
             // ================================ K and V of an 8-bit cache ================================
-            // A thread has 16 codes (one 16-byte load) of LANES-th of the rows; the next K or V is on its way from
-            // global memory while this one is turned into fp16.
+            // The four warps take a tile's codes out of the second half of its stage, wait for one another, and fill the
+            // stage with fp16 in the layout that the products read.
             constexpr int LANES = D / 16, PASSES = LANES, PER_PASS = 128 / LANES;
             const int tid = (int)threadIdx.x - 384, sub = tid % LANES, row0 = tid / LANES;
             const float c = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
-            uint4 kc[PASSES], vc[PASSES];
             float ks = 0.0f, vs = 0.0f;
             bool seen = false;
-            auto page_of = [&](int j) {                                 // -1: no such token, or no such page
-                if (j < cur.t.kb || j >= cur.t.ke) return -1;
+            // this thread's token's scales, on their way while the step before is converted
+            auto fetch_scales = [&]() {
+                const int j = cur.t.k0 + cur.step * STEP + tid;
+                seen = false;
+                if (j < cur.t.kb || j >= cur.t.ke) return;
                 const int p = __ldg(a.kv.table + (long long)cur.seq * a.kv.table_stride + (j >> a.kv.page_shift));
-                if ((unsigned)p < (unsigned)a.kv.n_pages) return p;
-                if (a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_INVALID);
-                return -1;
+                if ((unsigned)p >= (unsigned)a.kv.n_pages) return;
+                const long long e = scale_elem(a.kv, p, cur.head, j & ((1 << a.kv.page_shift) - 1));
+                ks = __ldg(a.kv.k_scale + e);
+                vs = __ldg(a.kv.v_scale + e);
+                seen = true;
             };
-            const int in_page = (1 << a.kv.page_shift) - 1;
-            auto fetch = [&](const unsigned char* src, int step, uint4 (&x)[PASSES]) {
-                const int j0 = cur.t.k0 + step * STEP;
+            auto convert = [&](uint32_t item, int first, int end) {     // rows outside [first, end) become zeros
+                const uint32_t stage = item % C::STAGES, at = ring + stage * C::TILE_BYTES;
+                if (!bar_wait(raw_full(stage), (item / C::STAGES) & 1, gave_up)) return false;
+                uint4 x[PASSES];
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
-                    const int j = j0 + i * PER_PASS + row0, p = page_of(j);
-                    x[i] = make_uint4(0, 0, 0, 0);
-                    if (p >= 0) x[i] = __ldg(reinterpret_cast<const uint4*>(src + page_elem(a.kv, p, cur.head, j & in_page) + sub * 16));
+                    const int r = i * PER_PASS + row0;
+                    x[i] = lds128(at + C::TILE_BYTES / 2 + r * D + sub * 16);
+                    if (r < first || r >= end) x[i] = make_uint4(0, 0, 0, 0);
                 }
-            };
-            auto fetch_scales = [&](int step) {
-                const int j = cur.t.k0 + step * STEP + tid, p = page_of(j);
-                seen = p >= 0;
-                if (seen) {
-                    const long long e = scale_elem(a.kv, p, cur.head, j & in_page);
-                    ks = __ldg(a.kv.k_scale + e);
-                    vs = __ldg(a.kv.v_scale + e);
-                }
-            };
-            auto convert = [&](int stage, const uint4 (&x)[PASSES]) {
+                asm volatile("bar.sync 1, 128;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int r = i * PER_PASS + row0;
@@ -642,43 +725,32 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int ch = sub * 2 + (swap ? 1 - e : e);
-                        st_shared16(ring + stage * C::TILE_BYTES + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16,
-                                    (e == 0) != swap ? lo4 : hi4);
+                        st_shared16(at + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16, (e == 0) != swap ? lo4 : hi4);
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) bar_arrive(kv_full(stage));
+                return true;
             };
-            long long item = 0, block = 0;
-            long long at = lo;
-            if (at < hi) {
-                fetch_scales(cur.step);
-                fetch(a.kv.k, cur.step, kc);
-            }
-            while (at < hi) {
-                const int step = cur.step;
-                fetch(a.kv.v, step, vc);
-                int stage = (int)(item % C::STAGES);
-                if (!bar_wait(kv_free(stage), ((uint32_t)(item / C::STAGES) & 1) ^ 1, gave_up)) break;
-                const uint32_t sc = scales + (uint32_t)(block % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
+            if (share > 0) fetch_scales();
+            for (int at = 0; at < share;) {
+                const int j0 = cur.t.k0 + cur.step * STEP, first = cur.t.kb - j0, end = cur.t.ke - j0;
+                // The buffer's last reader was done before the stage that V of this step will take was free, and K's
+                // copy was issued after that.
+                if (!bar_wait(raw_full((2 * at) % C::STAGES), ((uint32_t)(2 * at) / C::STAGES) & 1, gave_up)) break;
+                const uint32_t sc = scales + (at % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
                 // a V scale below 2^-80 counts as 2^-80 (of a vector of zeros, whose scale does not matter, or of values below 1e-21)
                 const float v1 = fmaxf(vs, 8.2718061e-25f);
                 const float f = seen ? c * ks : 0.0f, lv = seen ? (vs != vs ? vs : __log2f(v1)) : -INFINITY, iv = seen ? 1.0f / v1 : 0.0f;
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc), "f"(f) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + STEP * 4), "f"(lv) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + 2 * STEP * 4), "f"(iv) : "memory");
-                convert(stage, kc);
-                ++item; ++block; ++at;
-                if (++cur.step == cur.t.steps && at < hi) list.next(cur);
-                if (at < hi) {
-                    fetch_scales(cur.step);
-                    fetch(a.kv.k, cur.step, kc);
-                }
-                stage = (int)(item % C::STAGES);
-                if (!bar_wait(kv_free(stage), ((uint32_t)(item / C::STAGES) & 1) ^ 1, gave_up)) break;
-                convert(stage, vc);
-                ++item;
+                const uint32_t item = 2 * at;
+                ++at;
+                if (++cur.step == cur.t.steps && at < share) list.next(cur);
+                if (at < share) fetch_scales();
+                if (!convert(item, first, end) || !convert(item + 1, first, end)) break;
             }
         }
     }
@@ -688,7 +760,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
 }
 
-// Tensor map of k or v: {head_dim, row in page, KV head, page}, boxes of 64 elements by (part of) a page.
+// Tensor map of k or v: {head_dim, row in page, KV head, page}, boxes of 64 elements (8-bit: whole rows) by (part of) a page.
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                 CUtensorMapFloatOOBfill);
@@ -708,9 +780,21 @@ bool make_map(CUtensorMap* map, const KvView& c, void* base) {
     if (!f) return false;
     const int page = 1 << c.page_shift;
     const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)page, (cuuint64_t)c.n_kv, (cuuint64_t)c.n_pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)c.head_dim * 2, (cuuint64_t)page * c.head_dim * 2, (cuuint64_t)c.page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)(page < STEP ? page : STEP), 1, 1}, one[4] = {1, 1, 1, 1};
-    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const cuuint64_t bytes = c.k_scale ? 1 : 2;
+    const cuuint64_t strides[3] = {c.head_dim * bytes, (cuuint64_t)page * c.head_dim * bytes, (cuuint64_t)c.page_stride * bytes};
+    const cuuint32_t box[4] = {bytes == 1 ? (cuuint32_t)c.head_dim : 64, (cuuint32_t)(page < STEP ? page : STEP), 1, 1}, one[4] = {1, 1, 1, 1};
+    return f(map, bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, base, dims, strides, box, one,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, bytes == 1 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The queries: {head_dim, head, token}, boxes of 128 rows, token by token.
+bool make_q_map(CUtensorMap* map, const AttnView& a) {
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)a.kv.head_dim, (cuuint64_t)a.n_heads, (cuuint64_t)a.kv.n_tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_tok * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(HALF / a.group)}, one[3] = {1, 1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<unsigned char*>(a.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -719,10 +803,13 @@ cudaError_t run(const AttnView& a, int min_rows, Partial* meta, RowState* state,
     using C = Cfg<T, FMT, D>;
     cudaError_t e = allow_max_dynamic_smem(reinterpret_cast<const void*>(&k_attn_chunk<T, FMT, D>));
     if (e != cudaSuccess) return e;
-    CUtensorMap km = {}, vm = {};
-    if (!C::Q8 && (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v))) return cudaErrorInvalidValue;
+    CUtensorMap km = {}, vm = {}, qm = {};
+    // Queries come by TMA where 128 rows are whole tokens and nothing has to be done to them on the way; else by two warps.
+    // (Strides that a tensor map cannot hold, such as those of an expanded tensor, go the second way too.)
+    const bool q_tma = !C::Q_RANGE && HALF % a.group == 0 && a.scale_log2 >= 0.0f && a.q_head > 0 && a.q_tok > 0 && make_q_map(&qm, a);
+    if (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v)) return cudaErrorInvalidValue;
     launch_hook("k_attn_chunk", 0, st);
-    k_attn_chunk<T, FMT, D><<<attn_chunk_workers(), C::THREADS, C::SMEM, st>>>(a, km, vm, min_rows, meta, state, part);
+    k_attn_chunk<T, FMT, D><<<attn_chunk_workers(), C::THREADS, C::SMEM, st>>>(a, km, vm, qm, q_tma, min_rows, meta, state, part);
     launch_hook("k_attn_chunk", 1, st);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, attn_chunk_workers(), meta, state,
