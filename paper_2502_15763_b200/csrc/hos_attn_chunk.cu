@@ -809,16 +809,14 @@ cudaError_t run(const AttnView& a, int min_rows, Partial* meta, RowState* state,
     const bool q_tma = !C::Q_RANGE && HALF % a.group == 0 && a.scale_log2 >= 0.0f && a.q_head > 0 && a.q_tok > 0 && make_q_map(&qm, a);
     if (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v)) return cudaErrorInvalidValue;
     launch_hook("k_attn_chunk", 0, st);
-    k_attn_chunk<T, FMT, D><<<attn_chunk_workers(), C::THREADS, C::SMEM, st>>>(a, km, vm, qm, q_tma, min_rows, meta, state, part);
+    k_attn_chunk<T, FMT, D><<<ATTN_SMS, C::THREADS, C::SMEM, st>>>(a, km, vm, qm, q_tma, min_rows, meta, state, part);
     launch_hook("k_attn_chunk", 1, st);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, attn_chunk_workers(), meta, state,
+    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, ATTN_SMS, meta, state,
                                part, st);
 }
 
 }  // namespace
-
-int attn_chunk_workers() { return 148; }
 
 cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state, float* part,
                               cudaStream_t st) {

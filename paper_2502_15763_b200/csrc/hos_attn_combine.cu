@@ -76,7 +76,7 @@ cudaError_t run(const AttnView& a, int workers, const Partial* meta, const RowSt
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)workers, ROWS / 16);
+    cfg.gridDim = dim3((unsigned)workers, (ROWS + 15) / 16);
     cfg.blockDim = dim3(COMBINE_WARPS * 32);
     cfg.stream = st;
     cfg.attrs = &at;
@@ -89,6 +89,7 @@ cudaError_t run(const AttnView& a, int workers, const Partial* meta, const RowSt
 template <typename T, int D>
 cudaError_t with_rows(const AttnView& a, int rows, int workers, const Partial* meta, const RowState* state, const float* part,
                       cudaStream_t st) {
+    if (rows == 8) return run<T, D, 8>(a, workers, meta, state, part, st);
     return rows == 16 ? run<T, D, 16>(a, workers, meta, state, part, st) : run<T, D, 256>(a, workers, meta, state, part, st);
 }
 template <typename T>

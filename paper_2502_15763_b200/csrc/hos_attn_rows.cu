@@ -2,17 +2,19 @@
 //
 // What bounds it: the cache is read once, 2 * head_dim multiply-adds per cached element and 16 rows at
 // most, so HBM.  The kernel is built to keep loads in flight and nothing else:
-//   - The work is a list of steps of 16 tokens (sequence, KV head, tile of 16 rows, step).  Every WARP
+//   - The work is a list of steps of 16 tokens (sequence, KV head, tile of 8 or 16 rows, step).  Every WARP
 //     takes an equal, contiguous share of the list, whatever the lengths are; there is no barrier
 //     wider than a warp.  A tile cut by the ends of a share leaves a partial result (unnormalised output,
 //     maximum, normaliser) in the workspace, and k_attn_combine joins the pieces in list order, so the
 //     result does not depend on which warp finished first.
 //   - A warp copies its next steps into its own ring in shared memory (16-byte asynchronous copies), over
 //     the ends of tiles and sequences, while it works on the current one.
-//   - Rows are the query heads of a group times the new tokens.  S = Q K^T and O += P V are 16x8x16 matrix
-//     instructions.  The k index of the first product and the column index of the second may be
-//     permuted freely (the same way on both sides), so each lane reads its operands as whole 16-byte
-//     chunks of K and V rows; nothing is transposed but pairs of V rows (one byte permute a register).
+//   - Rows are the query heads of a group times the new tokens.  Both products are 16x8x16 matrix
+//     instructions with the rows as the 8 columns: S^T = K Q^T (16 tokens x 8 rows) and O^T += V^T P^T
+//     (16 of head_dim x 8 rows), so a tile of 8 rows wastes nothing.  The k index of the first product and the
+//     row index of the second may be permuted freely (the same way on both sides), so each lane reads its
+//     operands as whole 16-byte chunks of K and V rows; nothing is transposed but pairs of V rows (one byte
+//     permute a register) and the weights (one 8x8 exchange a half step).
 //   - 8-bit codes become fp16 exactly; K's scale multiplies the score, V's scale joins the exponent of
 //     the weight (w_j = exp2(x_j + log2 vs_j - max of that)), so no weight under- or overflows fp16
 //     whatever the scales are.
@@ -23,19 +25,19 @@
 namespace hos {
 namespace {
 
-constexpr int ROWS = 16, STEP = 16, WARPS = 4;
-using List = AttnList<ROWS, STEP>;
-using Cursor = List::Cursor;
+constexpr int STEP = 16, WARPS = 4;
 constexpr int MIN_STEPS = 2;                  // a worker's smallest share; fewer and the joining costs more than it saves
 
-template <typename T, int FMT, int D> struct Cfg {
+template <typename T, int FMT, int D, int NB> struct Cfg {
     static constexpr bool Q8 = FMT != HOS_KV_SAME;
+    static constexpr int ROWS = 8 * NB;
     static constexpr int ROW_BYTES = Q8 ? D : 2 * D;
     static constexpr int CHUNKS = ROW_BYTES / 16;
     static constexpr int KV_BYTES = STEP * ROW_BYTES;
     static constexpr int STAGE = 2 * KV_BYTES + (Q8 ? 2 * STEP * 4 : 0);
-    static constexpr int STAGES = Q8 ? (D == 128 ? 5 : 8) : (D == 128 ? 3 : 6);
-    static constexpr int CTAS = Q8 ? 2 : 2;
+    // CTAs of four warps on an SM, and the ring of each warp: as many bytes as fit
+    static constexpr int CTAS = !Q8 && D == 128 ? 2 : NB == 1 ? 4 : 2;
+    static constexpr int STAGES = (int)(SMEM_LIMIT / CTAS - 1024) / (WARPS * STAGE) < 8 ? (int)(SMEM_LIMIT / CTAS - 1024) / (WARPS * STAGE) : 8;
     static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
 // A row's weights are 2^(x - (maximum - LIFT)): in fp16 the largest is 2^14, so that small ones keep their bits
@@ -50,14 +52,34 @@ template <int CHUNKS> __device__ __forceinline__ int swizzle(int r) {
     return CHUNKS == 4 ? (r >> 1) & 3 : (((r >> 1) & 1) << 1) | ((((r >> 2) ^ r) & 1) << 2);
 }
 
-template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(WARPS * 32, Cfg<T, FMT, D>::CTAS)
+// Transposes an 8x8 matrix of 16-bit elements held as one pair a lane (lane / 4: row, lane % 4: pair of columns).
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+// Over the eight lanes of a column of 8x8 results.
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(FULL, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(FULL, v, 8));
+    return fmaxf(v, __shfl_xor_sync(FULL, v, 16));
+}
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor_sync(FULL, v, 4);
+    v += __shfl_xor_sync(FULL, v, 8);
+    return v + __shfl_xor_sync(FULL, v, 16);
+}
+
+template <typename T, int FMT, int D, int NB>
+__global__ void __launch_bounds__(WARPS * 32, Cfg<T, FMT, D, NB>::CTAS)
 k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __restrict__ meta,
             RowState* __restrict__ state, float* __restrict__ part) {
-    using C = Cfg<T, FMT, D>;
+    using C = Cfg<T, FMT, D, NB>;
     using M = typename MatType<T, FMT>::type;
-    constexpr int KS = D / 16;                 // matrix instructions along head_dim
-    constexpr int NT = D / 8;                  // column tiles of the output
+    using List = AttnList<C::ROWS, STEP>;
+    using Cursor = typename List::Cursor;
+    constexpr int ROWS = C::ROWS;
+    constexpr int KS = D / 16;                 // matrix instructions along head_dim, and tiles of O^T
     extern __shared__ __align__(128) unsigned char smem[];
     const int lane = lane_id(), g = lane >> 2, t4 = lane & 3;
     const int workers = (int)gridDim.x * WARPS;
@@ -125,28 +147,26 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     for (int i = 0; i < C::STAGES - 1; ++i) issue(i);
 
     // --- the rows of the current tile ---------------------------------------------------------
-    uint32_t aq[KS][4];
-    float o[NT][4];
-    float m[2], l[2], mt[2], qmul[2];          // [0]: row g, [1]: row g + 8
-    int see_lo[2], see_hi[2];                  // visible tokens of the two rows
+    // as columns of a product: row nb * 8 + g when read, rows nb * 8 + 2 * t4 + {0, 1} of the results
+    uint32_t bq[KS][NB][2];
+    float o[KS][NB][4];
+    float m[NB][2], l[NB][2], mt[NB][2], qmul[NB][2];
+    int see_lo[NB][2], see_hi[NB][2];          // visible tokens
     const int f = swizzle<C::CHUNKS>(g);
     const uint32_t k_at = g * C::ROW_BYTES + (t4 ^ (f & 3)) * 16, k_x = (f & 4) * 16;
 
     auto begin = [&]() {
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            m[h] = mt[h] = -INFINITY;
-            l[h] = 0.0f;
-            const int r = cons.tile * ROWS + g + 8 * h;
-            const bool there = g + 8 * h < cons.t.rows;
+                for (int j = 0; j < 4; ++j) o[i][nb][j] = 0.0f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int r = cons.tile * ROWS + nb * 8 + g;
+            const bool there = nb * 8 + g < cons.t.rows;
             const int i = r / a.group, hd = cons.head * a.group + r % a.group;
-            const int pos = cons.q.len - cons.q.n + i;
-            see_hi[h] = there ? (a.causal ? min(cons.q.len, pos + 1) : cons.q.len) : 0;
-            see_lo[h] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
             const T* src = reinterpret_cast<const T*>(a.q) + (long long)(cons.q.off + i) * a.q_tok + (long long)hd * a.q_head;
             uint32_t x[2 * KS];
 #pragma unroll
@@ -157,7 +177,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 if (there) v = __ldg(reinterpret_cast<const uint4*>(src + d));
                 x[4 * c] = v.x; x[4 * c + 1] = v.y; x[4 * c + 2] = v.z; x[4 * c + 3] = v.w;
             }
-            qmul[h] = a.scale_log2;
+            float mul = a.scale_log2;
             if (C::Q8 && !std::is_same<T, __half>::value) {
                 // bf16 queries meet fp16 keys: a power of two per row brings the row into fp16's range
                 // (exact but for elements 2^-38 of the row's largest)
@@ -173,7 +193,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 // top * 2^(140 - ex) is in [2^13, 2^14); rows of zeros, denormals or non-finite values stay
                 const int sh = ex >= 27 && ex < 254 ? 140 - ex : 0;
                 const float up = __uint_as_float((uint32_t)(127 + sh) << 23);
-                qmul[h] = a.scale_log2 * __uint_as_float((uint32_t)(127 - sh) << 23);
+                mul *= __uint_as_float((uint32_t)(127 - sh) << 23);
 #pragma unroll
                 for (int i2 = 0; i2 < 2 * KS; ++i2) {
                     const float2 v = Pair<T>::unpack(x[i2]);
@@ -181,68 +201,67 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 }
             }
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) { aq[ks][h] = x[2 * ks]; aq[ks][2 + h] = x[2 * ks + 1]; }
+            for (int ks = 0; ks < KS; ++ks) { bq[ks][nb][0] = x[2 * ks]; bq[ks][nb][1] = x[2 * ks + 1]; }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r2 = cons.tile * ROWS + nb * 8 + 2 * t4 + e;
+                const int pos = cons.q.len - cons.q.n + r2 / a.group;
+                see_hi[nb][e] = nb * 8 + 2 * t4 + e < cons.t.rows ? (a.causal ? min(cons.q.len, pos + 1) : cons.q.len) : 0;
+                see_lo[nb][e] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+                qmul[nb][e] = __shfl_sync(FULL, mul, (2 * t4 + e) * 4);
+                m[nb][e] = mt[nb][e] = -INFINITY;
+                l[nb][e] = 0.0f;
+            }
         }
     };
 
-    // Output column tile i, column 2 * t4 + cc of this lane: which element of head_dim.
-    auto dim_of = [&](int i, int cc) {
-        return C::Q8 && D == 128 ? (2 * t4 + cc) * 16 + i : (i >> 3) * 64 + (2 * t4 + cc) * 8 + (i & 7);
-    };
+    // Tiles 4 q .. 4 q + 3 of O^T are eight consecutive elements of head_dim in this lane.
+    auto dim_of = [&](int q) { return C::Q8 && D == 128 ? g * 16 + q * 8 : q * 64 + g * 8; };
     bool open_end = false;
     int seg_first = cons.step;                 // the step of the tile this warp began with
     auto finish = [&](long long unit) {
         const bool whole_start = seg_first == 0, whole_end = cons.step == cons.t.steps - 1;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l[h] += __shfl_xor_sync(FULL, l[h], 1);
-            l[h] += __shfl_xor_sync(FULL, l[h], 2);
-        }
-        if (whole_start && whole_end) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (g + 8 * h >= cons.t.rows) continue;
-                const int r = cons.tile * ROWS + g + 8 * h;
-                const int tok = cons.q.off + r / a.group, hd = cons.head * a.group + r % a.group;
-                float by = l[h] == 0.0f ? 0.0f : 1.0f / l[h];
-                if (C::Q8 && l[h] != 0.0f) by *= exp2f(mt[h] - m[h]);
-                T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head;
-#pragma unroll
-                for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-                    for (int i = 0; i < NT; i += 8) {
-                        uint4 v;
-                        v.x = Pair<T>::pack(o[i][2 * h + cc] * by, o[i + 1][2 * h + cc] * by);
-                        v.y = Pair<T>::pack(o[i + 2][2 * h + cc] * by, o[i + 3][2 * h + cc] * by);
-                        v.z = Pair<T>::pack(o[i + 4][2 * h + cc] * by, o[i + 5][2 * h + cc] * by);
-                        v.w = Pair<T>::pack(o[i + 6][2 * h + cc] * by, o[i + 7][2 * h + cc] * by);
-                        *reinterpret_cast<uint4*>(dst + dim_of(i, cc)) = v;
-                    }
-                if (a.lse && t4 == 0)
-                    a.lse[(long long)tok * a.n_heads + hd] =
-                        l[h] == 0.0f ? -INFINITY : (m[h] + log2f(l[h])) * 0.69314718055994530942f;
-            }
-            return;
-        }
+        const bool whole = whole_start && whole_end;
         const int slot = 2 * w + (whole_start ? 1 : 0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (g + 8 * h >= cons.t.rows) continue;
-            const long long r = (long long)slot * ROWS + g + 8 * h;
-            float* dst = part + r * D;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc)
+            for (int e = 0; e < 2; ++e) {
+                const float sum = column_sum(l[nb][e]);
+                const int in_tile = nb * 8 + 2 * t4 + e;
+                if (in_tile >= cons.t.rows) continue;
+                if (whole) {
+                    const int r = cons.tile * ROWS + in_tile;
+                    const int tok = cons.q.off + r / a.group, hd = cons.head * a.group + r % a.group;
+                    float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    if (C::Q8 && sum != 0.0f) by *= exp2f(mt[nb][e] - m[nb][e]);
+                    T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head;
 #pragma unroll
-                for (int i = 0; i < NT; i += 4)
-                    *reinterpret_cast<float4*>(dst + dim_of(i, cc)) =
-                        make_float4(o[i][2 * h + cc], o[i + 1][2 * h + cc], o[i + 2][2 * h + cc], o[i + 3][2 * h + cc]);
-            if (t4 == 0) state[r] = RowState{m[h], l[h], C::Q8 ? mt[h] : m[h], 0.0f};
-        }
-        if (whole_start && lane == 0) {
+                    for (int q = 0; q < KS / 4; ++q) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = Pair<T>::pack(o[4 * q + i][nb][e] * by, o[4 * q + i][nb][2 + e] * by);
+                        *reinterpret_cast<uint4*>(dst + dim_of(q)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                    if (a.lse && g == 0)
+                        a.lse[(long long)tok * a.n_heads + hd] =
+                            sum == 0.0f ? -INFINITY : (m[nb][e] + log2f(sum)) * 0.69314718055994530942f;
+                } else {
+                    const long long r = (long long)slot * ROWS + in_tile;
+#pragma unroll
+                    for (int q = 0; q < KS / 4; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2)
+                            *reinterpret_cast<float4*>(part + r * D + dim_of(q) + 2 * i) =
+                                make_float4(o[4 * q + i][nb][e], o[4 * q + i][nb][2 + e], o[4 * q + i + 1][nb][e], o[4 * q + i + 1][nb][2 + e]);
+                    if (g == 0) state[r] = RowState{m[nb][e], sum, C::Q8 ? mt[nb][e] : m[nb][e], 0.0f};
+                }
+            }
+        if (!whole && whole_start && lane == 0) {
             const long long end = unit + (cons.t.steps - cons.step);      // one past the tile's last step
             meta[w] = Partial{cons.seq, cons.head, cons.tile, (int)((end * active - 1) / total)};
         }
-        open_end = whole_start;
+        open_end = whole_start && !whole_end;
     };
 
     begin();
@@ -255,88 +274,86 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
         const uint32_t kd = ring + stage * C::STAGE, vd = kd + C::KV_BYTES;
         if (++stage == C::STAGES) stage = 0;
 
-        // scores of 16 tokens: x[nt][0..1] row g, x[nt][2..3] row g + 8, tokens nt * 8 + 2 * t4 + {0, 1}
-        float x[2][4];
+        // scores: x[nb][0..1] token g, x[nb][2..3] token g + 8, rows nb * 8 + 2 * t4 + {0, 1}
+        float x[NB][4];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[nt][j] = 0.0f;
-            const uint32_t at = kd + nt * 8 * C::ROW_BYTES + k_at;
+            for (int j = 0; j < 4; ++j) x[nb][j] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < C::CHUNKS / 4; ++c) {
-                const uint4 v = lds128(at + ((c * 64) ^ k_x));
-                const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
-                if (!C::Q8) {
-                    mma16816<M>(x[nt], aq[2 * c], wv[0], wv[1]);
-                    mma16816<M>(x[nt], aq[2 * c + 1], wv[2], wv[3]);
-                } else {
+        for (int c = 0; c < C::CHUNKS / 4; ++c) {
+            const uint4 v0 = lds128(kd + k_at + ((c * 64) ^ k_x)), v1 = lds128(kd + 8 * C::ROW_BYTES + k_at + ((c * 64) ^ k_x));
+            const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+            if (!C::Q8) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        mma16816<M>(x[nt], aq[(4 * c + i) % KS], codes_to_half2<FMT>(wv[i]), codes_to_half2<FMT>(wv[i] >> 16));
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t ak[4] = {w0[2 * i], w1[2 * i], w0[2 * i + 1], w1[2 * i + 1]};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(x[nb], ak, bq[2 * c + i][nb][0], bq[2 * c + i][nb][1]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t ak[4] = {codes_to_half2<FMT>(w0[i]), codes_to_half2<FMT>(w1[i]), codes_to_half2<FMT>(w0[i] >> 16),
+                                            codes_to_half2<FMT>(w1[i] >> 16)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(x[nb], ak, bq[(4 * c + i) % KS][nb][0], bq[(4 * c + i) % KS][nb][1]);
                 }
             }
         }
         const int j0 = cons.t.k0 + cons.step * STEP;
-        const bool edge = j0 < see_lo[0] || j0 + STEP > see_hi[0] || j0 < see_lo[1] || j0 + STEP > see_hi[1];
-        float vs[2][2];                        // log2 of V's scales
+        float ks[2] = {1.0f, 1.0f}, lv[2] = {0.0f, 0.0f};      // of tokens g and g + 8: K's scale, log2 of V's
+        if (C::Q8) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            float ks0 = 1.0f, ks1 = 1.0f;
-            if (C::Q8) {
-                const uint2 kk = lds64(vd + C::KV_BYTES + (nt * 8 + 2 * t4) * 4);
-                const uint2 vv = lds64(vd + C::KV_BYTES + STEP * 4 + (nt * 8 + 2 * t4) * 4);
-                ks0 = __uint_as_float(kk.x); ks1 = __uint_as_float(kk.y);
-                vs[nt][0] = __log2f(__uint_as_float(vv.x)); vs[nt][1] = __log2f(__uint_as_float(vv.y));
+            for (int i = 0; i < 2; ++i) {
+                ks[i] = lds32f(vd + C::KV_BYTES + (g + 8 * i) * 4);
+                lv[i] = __log2f(lds32f(vd + C::KV_BYTES + (STEP + g + 8 * i) * 4));
             }
+        }
+        float shrink[NB][2];
+        uint32_t bp[NB][2];
+        bool moved = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float p[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int h = j >> 1;
-                x[nt][j] *= C::Q8 ? qmul[h] * ((j & 1) ? ks1 : ks0) : a.scale_log2;
-                const int tok = j0 + nt * 8 + 2 * t4 + (j & 1);
-                if (edge && (tok < see_lo[h] || tok >= see_hi[h])) x[nt][j] = -INFINITY;
+                const int e = j & 1, tok = j0 + g + 8 * (j >> 1);
+                x[nb][j] *= C::Q8 ? qmul[nb][e] * ks[j >> 1] : a.scale_log2;
+                if (tok < see_lo[nb][e] || tok >= see_hi[nb][e]) x[nb][j] = -INFINITY;
             }
-        }
-        float shrink[2];
-        uint32_t ap[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float top = fmaxf(fmaxf(x[0][2 * h], x[0][2 * h + 1]), fmaxf(x[1][2 * h], x[1][2 * h + 1]));
-            top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
-            const float mn = fmaxf(m[h], C::Q8 ? top : top - LIFT<M>), ms = mn == -INFINITY ? 0.0f : mn;
-            shrink[h] = exp2_fast(m[h] - ms);
-            m[h] = mn;
-            float p[4], sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { p[i] = exp2_fast(x[i >> 1][2 * h + (i & 1)] - ms); sum += p[i]; }
-            l[h] = l[h] * shrink[h] + sum;
-            if (C::Q8) {
-                float y[4], ty = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float xi = x[i >> 1][2 * h + (i & 1)];
-                    y[i] = xi == -INFINITY ? xi : xi + vs[i >> 1][i & 1];
-                    ty = fmaxf(ty, y[i]);
+            for (int e = 0; e < 2; ++e) {
+                const float top = column_max(fmaxf(x[nb][e], x[nb][2 + e]));
+                const float mn = fmaxf(m[nb][e], C::Q8 ? top : top - LIFT<M>), ms = mn == -INFINITY ? 0.0f : mn;
+                shrink[nb][e] = exp2_fast(m[nb][e] - ms);
+                m[nb][e] = mn;
+                p[e] = exp2_fast(x[nb][e] - ms);
+                p[2 + e] = exp2_fast(x[nb][2 + e] - ms);
+                l[nb][e] = l[nb][e] * shrink[nb][e] + (p[e] + p[2 + e]);
+                if (C::Q8) {
+                    const float y0 = x[nb][e] == -INFINITY ? -INFINITY : x[nb][e] + lv[0];
+                    const float y1 = x[nb][2 + e] == -INFINITY ? -INFINITY : x[nb][2 + e] + lv[1];
+                    const float yn = fmaxf(mt[nb][e], column_max(fmaxf(y0, y1)) - LIFT<M>), ys = yn == -INFINITY ? 0.0f : yn;
+                    shrink[nb][e] = exp2_fast(mt[nb][e] - ys);
+                    mt[nb][e] = yn;
+                    p[e] = exp2_fast(y0 - ys);
+                    p[2 + e] = exp2_fast(y1 - ys);
                 }
-                ty = fmaxf(ty, __shfl_xor_sync(FULL, ty, 1));
-                ty = fmaxf(ty, __shfl_xor_sync(FULL, ty, 2));
-                const float yn = fmaxf(mt[h], ty - LIFT<M>), ys = yn == -INFINITY ? 0.0f : yn;
-                shrink[h] = exp2_fast(mt[h] - ys);
-                mt[h] = yn;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = exp2_fast(y[i] - ys);
+                moved |= shrink[nb][e] != 1.0f;
             }
-            ap[h] = Pair<M>::pack(p[0], p[1]);
-            ap[2 + h] = Pair<M>::pack(p[2], p[3]);
+            bp[nb][0] = transpose8x8(Pair<M>::pack(p[0], p[1]));
+            bp[nb][1] = transpose8x8(Pair<M>::pack(p[2], p[3]));
         }
-        if (__any_sync(FULL, shrink[0] != 1.0f || shrink[1] != 1.0f)) {
+        if (__any_sync(FULL, moved)) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                o[i][0] *= shrink[0]; o[i][1] *= shrink[0];
-                o[i][2] *= shrink[1]; o[i][3] *= shrink[1];
-            }
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[i][nb][j] *= shrink[nb][j & 1];
         }
-        // O += P V: this lane's rows of V are tokens 2 * t4 + {0, 1, 8, 9}
+        // O^T += V^T P^T: this lane's rows of V are tokens 2 * t4 + {0, 1, 8, 9}
         if (!C::Q8) {
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) {
@@ -350,8 +367,10 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                                            {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    mma16816<M>(o[half * 8 + 2 * i], ap, __byte_perm(vw[0][i], vw[1][i], 0x5410), __byte_perm(vw[2][i], vw[3][i], 0x5410));
-                    mma16816<M>(o[half * 8 + 2 * i + 1], ap, __byte_perm(vw[0][i], vw[1][i], 0x7632), __byte_perm(vw[2][i], vw[3][i], 0x7632));
+                    const uint32_t av[4] = {__byte_perm(vw[0][i], vw[1][i], 0x5410), __byte_perm(vw[0][i], vw[1][i], 0x7632),
+                                            __byte_perm(vw[2][i], vw[3][i], 0x5410), __byte_perm(vw[2][i], vw[3][i], 0x7632)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[half * 4 + i][nb], av, bp[nb][0], bp[nb][1]);
                 }
             }
         } else {
@@ -370,14 +389,15 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 }
             }
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) {
-                const uint32_t x0 = __byte_perm(vw[0][i], vw[1][i], 0x5140), y0 = __byte_perm(vw[0][i], vw[1][i], 0x7362);
-                const uint32_t x1 = __byte_perm(vw[2][i], vw[3][i], 0x5140), y1 = __byte_perm(vw[2][i], vw[3][i], 0x7362);
-                mma16816<M>(o[4 * i], ap, codes_to_half2<FMT>(x0), codes_to_half2<FMT>(x1));
-                mma16816<M>(o[4 * i + 1], ap, codes_to_half2<FMT>(x0 >> 16), codes_to_half2<FMT>(x1 >> 16));
-                mma16816<M>(o[4 * i + 2], ap, codes_to_half2<FMT>(y0), codes_to_half2<FMT>(y1));
-                mma16816<M>(o[4 * i + 3], ap, codes_to_half2<FMT>(y0 >> 16), codes_to_half2<FMT>(y1 >> 16));
-            }
+            for (int i = 0; i < WORDS; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t x0 = __byte_perm(vw[0][i], vw[1][i], k ? 0x7362 : 0x5140);
+                    const uint32_t x1 = __byte_perm(vw[2][i], vw[3][i], k ? 0x7362 : 0x5140);
+                    const uint32_t av[4] = {codes_to_half2<FMT>(x0), codes_to_half2<FMT>(x0 >> 16), codes_to_half2<FMT>(x1), codes_to_half2<FMT>(x1 >> 16)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[2 * i + k][nb], av, bp[nb][0], bp[nb][1]);
+                }
         }
         const bool tile_done = cons.step == cons.t.steps - 1;
         if (tile_done || unit + 1 == hi) {
@@ -395,30 +415,30 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     cp_async_wait<0>();
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, int NB>
 cudaError_t run(const AttnView& a, int max_rows, Partial* meta, RowState* state, float* part, cudaStream_t st) {
-    using C = Cfg<T, FMT, D>;
-    const void* f = reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D>);
+    using C = Cfg<T, FMT, D, NB>;
+    static_assert(C::CTAS * C::ROWS <= ATTN_ROWS_PER_SM / WARPS, "workspace");
+    const void* f = reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D, NB>);
     cudaError_t e = allow_max_dynamic_smem(f);
     if (e != cudaSuccess) return e;
-    const int ctas = attn_rows_workers() / WARPS;
+    const int ctas = 148 * C::CTAS;
     launch_hook("k_attn_rows", 0, st);
-    k_attn_rows<T, FMT, D><<<ctas, WARPS * 32, C::SMEM, st>>>(a, max_rows, meta, state, part);
+    k_attn_rows<T, FMT, D, NB><<<ctas, WARPS * 32, C::SMEM, st>>>(a, max_rows, meta, state, part);
     launch_hook("k_attn_rows", 1, st);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, attn_rows_workers(), meta,
+    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, C::ROWS, ctas * WARPS, meta,
                                state, part, st);
 }
 
 }  // namespace
 
-// Two CTAs of four warps on each of 148 SMs.
-int attn_rows_workers() { return 148 * 2 * WARPS; }
-
-cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int max_rows, Partial* meta, RowState* state,
+cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, Partial* meta, RowState* state,
                              float* part, cudaStream_t st) {
     return kv_dispatch(type, format, a.kv.head_dim, [&](auto t, auto f, auto d) {
-        return run<typename decltype(t)::type, decltype(f)::value, decltype(d)::value>(a, max_rows, meta, state, part, st);
+        using T = typename decltype(t)::type;
+        return tile_rows == 8 ? run<T, decltype(f)::value, decltype(d)::value, 1>(a, max_rows, meta, state, part, st)
+                              : run<T, decltype(f)::value, decltype(d)::value, 2>(a, max_rows, meta, state, part, st);
     });
 }
 

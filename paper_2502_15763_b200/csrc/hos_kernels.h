@@ -95,10 +95,10 @@ struct Partial;
 cudaError_t launch_kv_append(const KvView& c, int type, int format, const void* k, const void* v,
                              const long long (&strides)[4], cudaStream_t st);
 cudaError_t launch_kv_read(const KvView& c, int type, int format, void* k, void* v, cudaStream_t st);
-int attn_rows_workers();
-cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int max_rows, Partial* meta, RowState* state,
+// Work shares of the attention kernels: their number, and the rows that their pieces hold on one SM.
+constexpr int ATTN_SMS = 148, ATTN_WORKERS_PER_SM = 16, ATTN_ROWS_PER_SM = 256;
+cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, Partial* meta, RowState* state,
                              float* part, cudaStream_t st);
-int attn_chunk_workers();
 cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state,
                               float* part, cudaStream_t st);
 cudaError_t launch_attn_combine(const AttnView& a, int type, int rows, int workers, const Partial* meta, const RowState* state,

@@ -1,5 +1,4 @@
 // C-ABI layer of the KV-cache calls: argument validation, workspace carving, kernel sequencing.
-#include <algorithm>
 #include <cmath>
 
 #include "hos_kernels.h"
@@ -67,8 +66,6 @@ KvView view(const hos_kv_cache* c, const hos_kv_batch* b, int32_t* status) {
 
 inline int cuda_rc(cudaError_t e) { return e == cudaSuccess ? HOS_OK : HOS_E_CUDA; }
 
-constexpr int ROW_TILE = 16;                 // rows of a tile of the row kernel
-
 struct AttnWs {
     Partial* meta;
     RowState* state;
@@ -79,9 +76,8 @@ AttnWs carve_attention(int head_dim, void* ws) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     AttnWs w;
     unsigned char* base = static_cast<unsigned char*>(ws);
-    // the two kernels follow one another on the stream and share the space
-    const size_t n = (size_t)std::max(attn_rows_workers(), attn_chunk_workers());
-    const size_t rows = 2 * (size_t)std::max(attn_rows_workers() * 16, attn_chunk_workers() * 256);
+    // the two kernels follow one another on the stream and share the space; a share leaves two pieces at most
+    const size_t n = (size_t)ATTN_SMS * ATTN_WORKERS_PER_SM, rows = 2 * (size_t)ATTN_SMS * ATTN_ROWS_PER_SM;
     size_t off = 0;
     w.meta = reinterpret_cast<Partial*>(base + off);   off += up(n * sizeof(Partial));
     w.state = reinterpret_cast<RowState*>(base + off); off += up(rows * sizeof(RowState));
@@ -151,11 +147,15 @@ int hos_paged_attention(const hos_kv_cache* c, const hos_kv_batch* b, const void
     a.causal = causal != 0;
     a.window = window;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // Sequences of more rows than one tile of the row kernel go to the chunk kernel (all, if there is but one).
-    const bool chunks = (long long)b->max_new * a.group > ROW_TILE, alone = b->n_seq == 1;
-    if (chunks && (rc = cuda_rc(launch_attn_chunk(a, c->type, c->format, alone ? 0 : ROW_TILE, w.meta, w.state, w.part, st)))) return rc;
+    // A sequence has new tokens * group rows a KV head.  Up to 16: the row kernel, in tiles of 8 where that is enough for
+    // all.  If there are larger ones, they go to the chunk kernel (all, if there is but one sequence), and the row kernel
+    // keeps the single tokens: 8 rows, or 16 for groups above 8.
+    const long long most = (long long)b->max_new * a.group;
+    const bool chunks = most > 16, alone = b->n_seq == 1;
+    const int tile = chunks ? (a.group <= 8 ? 8 : 16) : most <= 8 ? 8 : 16;
+    if (chunks && (rc = cuda_rc(launch_attn_chunk(a, c->type, c->format, alone ? 0 : tile, w.meta, w.state, w.part, st)))) return rc;
     if (chunks && alone) return HOS_OK;
-    return cuda_rc(launch_attn_rows(a, c->type, c->format, chunks ? ROW_TILE : 0x7FFFFFFF, w.meta, w.state, w.part, st));
+    return cuda_rc(launch_attn_rows(a, c->type, c->format, tile, chunks ? tile : 0x7FFFFFFF, w.meta, w.state, w.part, st));
 }
 
 }  // extern "C"
