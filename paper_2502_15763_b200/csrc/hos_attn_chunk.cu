@@ -29,7 +29,8 @@ namespace hos {
 namespace {
 
 constexpr int ROWS = 256, STEP = 128, HALF = 128;
-using List = AttnList<ROWS, STEP>;
+constexpr int TILE_STEPS = 2;                 // what a tile's begin and end cost, in steps
+using List = AttnList<ROWS, STEP, TILE_STEPS>;
 using Cursor = List::Cursor;
 constexpr float GROWTH = 8.0f;                // log2 of how far a row's maximum may pass the one its reference was taken from
 // The reference is the maximum - LIFT: fp16 weights start at 2^7 and end below 2^15, so that small ones keep their bits.
@@ -262,13 +263,13 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     const uint32_t tmem = (uint32_t)uniform((int)sh.tmem);
     const int share = sh.share;
     Cursor cur = sh.first;
-    // the steps from number `at` of the share to the end of the tile or the share
-    auto segment = [&](int at) {
+    bool more = share > 0 && cur.step < list.end_of(cur, share);
+    auto segment = [&]() {                                              // of the current tile
         Segment s;
-        const int left = share - at, rest = cur.t.steps - cur.step;
-        s.blocks = min(left, rest);
+        const int end = list.end_of(cur, share);
+        s.blocks = end - cur.step;
         s.starts = cur.step == 0;
-        s.ends = s.blocks == rest;
+        s.ends = end == cur.t.steps;
         return s;
     };
 
@@ -296,13 +297,12 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             fence_async_smem();
             return true;
         };
-        for (int at = 0; at < share && ok;) {
-            const Segment seg = segment(at);
+        for (; more && ok; more = list.next(cur, share)) {
+            const Segment seg = segment();
             const bool active = cur.t.rows > h * HALF;
             q_buf ^= 1;
             if (!active) {
-                at += seg.blocks; block += seg.blocks;
-                if (at < share) list.next(cur);
+                block += seg.blocks;
                 continue;
             }
             const int r = cur.tile * ROWS + h * HALF + row;
@@ -331,7 +331,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 float* x = reinterpret_cast<float*>(s);
                 const uint32_t f_at = scales + buf * (3 * STEP * 4), lv_at = f_at + STEP * 4, iv_at = lv_at + STEP * 4;
                 if (C::Q_RANGE) {
-                    const float up = lds32f(q_scales + (q_buf * ROWS + h * HALF + row) * 4);
+                    const float up = lds<float>(q_scales + (q_buf * ROWS + h * HALF + row) * 4);
                     if (__any_sync(FULL, up != 1.0f)) {
 #pragma unroll
                         for (int i = 0; i < 128; ++i) x[i] *= up;
@@ -466,16 +466,14 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         a.lse[(long long)(cur.q.off + tok) * a.n_heads + hd] =
                             l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
                 } else {
-                    state[prow] = RowState{m, l, m, 0.0f};
+                    state[prow] = RowState{m, l};
                 }
             }
             if (!whole && seg.starts && h == 0 && row == 0) {
-                const long long end = sh.lo + at + (cur.t.steps - cur.step);
+                const long long end = sh.lo + cur.at + TILE_STEPS + cur.t.steps;
                 meta[w] = Partial{cur.seq, cur.head, cur.tile, (int)((end * sh.active - 1) / sh.total)};
             }
             tc_fence_before();
-            at += seg.blocks;
-            if (at < share) list.next(cur);
         }
         if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
     } else {
@@ -488,8 +486,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             // ================================ K and V by TMA ================================
             const int box = min(STEP, 1 << a.kv.page_shift), pieces = STEP / box;
             uint32_t item = 0;
-            for (int at = 0; at < share;) {
-                const Segment seg = segment(at);
+            for (; more; more = list.next(cur, share)) {
+                const Segment seg = segment();
                 bool ok = true;
                 for (int b = 0; b < seg.blocks && ok; ++b) {
                     const int j0 = cur.t.k0 + (cur.step + b) * STEP, j = j0 + lane * box;
@@ -518,8 +516,6 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     }
                 }
                 if (!ok) break;
-                at += seg.blocks;
-                if (at < share) list.next(cur);
             }
             // leave only when every copy has landed
             for (uint32_t i = item > C::STAGES ? item - C::STAGES : 0; i < item; ++i) bar_drain(raw_full(i % C::STAGES), (i / C::STAGES) & 1);
@@ -544,8 +540,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 for (int k = part_of * (STEP / 32); k < (part_of + 1) * (STEP / 32); ++k)
                     mma_ts(tmem + 256 + h * D, tmem + h * 128 + 8 * k, vb + (uint64_t)((k * 16 * 128) >> 4), PV, add || k > 0);
             };
-            for (int at = 0; at < share && ok;) {
-                const Segment seg = segment(at);
+            for (; more && ok; more = list.next(cur, share)) {
+                const Segment seg = segment();
                 const int halves = uniform(cur.t.rows > HALF ? 2 : 1), blocks = uniform(seg.blocks);
                 for (int h = 0; h < 2 && ok; ++h) ok = bar_wait(q_full(h), q_phase, gave_up);
                 q_phase ^= 1;
@@ -591,8 +587,6 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     __syncwarp();
                     item += 2;
                 }
-                at += seg.blocks;
-                if (at < share) list.next(cur);
             }
             // nothing of this warp's is in flight when the tensor memory is given back
             if (issued && elect_one()) {
@@ -607,8 +601,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             const uint32_t dst = q_smem + h * C::Q_BYTES;
             const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;   // the softmax works with |scale|
             uint32_t phase = 1, q_buf = 0, last = 2;                             // the first wait falls through
-            for (int at = 0; at < share;) {
-                const Segment seg = segment(at);
+            for (; more; more = list.next(cur, share)) {
+                const Segment seg = segment();
                 if (!bar_wait(q_free(h), phase, gave_up)) break;
                 phase ^= 1;
                 if (q_tma) {
@@ -622,8 +616,6 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                                             "r"(cur.q.off + (cur.tile * ROWS + h * HALF) / a.group), "r"(q_full(h)) : "memory");
                     }
                     __syncwarp();
-                    at += seg.blocks;
-                    if (at < share) list.next(cur);
                     last = phase;
                     continue;
                 }
@@ -676,8 +668,6 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 __syncwarp();
                 if (lane == 0) bar_arrive(q_full(h));
                 q_buf ^= 1;
-                at += seg.blocks;
-                if (at < share) list.next(cur);
             }
             if (last < 2) bar_drain(q_full(h), last);                   // the last copy has landed
         } else if (C::Q8 && warp >= 12) {
@@ -708,17 +698,16 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int r = i * PER_PASS + row0;
-                    x[i] = lds128(at + C::TILE_BYTES / 2 + r * D + sub * 16);
+                    x[i] = lds<uint4>(at + C::TILE_BYTES / 2 + r * D + sub * 16);
                     if (r < first || r >= end) x[i] = make_uint4(0, 0, 0, 0);
                 }
                 asm volatile("bar.sync 1, 128;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int r = i * PER_PASS + row0;
-                    const uint4 lo4 = make_uint4(codes_to_half2<FMT>(x[i].x), codes_to_half2<FMT>(x[i].x >> 16),
-                                                 codes_to_half2<FMT>(x[i].y), codes_to_half2<FMT>(x[i].y >> 16));
-                    const uint4 hi4 = make_uint4(codes_to_half2<FMT>(x[i].z), codes_to_half2<FMT>(x[i].z >> 16),
-                                                 codes_to_half2<FMT>(x[i].w), codes_to_half2<FMT>(x[i].w >> 16));
+                    const uint2 c0 = codes_to_half4<FMT>(x[i].x), c1 = codes_to_half4<FMT>(x[i].y);
+                    const uint2 c2 = codes_to_half4<FMT>(x[i].z), c3 = codes_to_half4<FMT>(x[i].w);
+                    const uint4 lo4 = make_uint4(c0.x, c0.y, c1.x, c1.y), hi4 = make_uint4(c2.x, c2.y, c3.x, c3.y);
                     // lanes 4-7 of a row go to the other block of the tile: they store their chunks the other way
                     // round, so that eight lanes always fill eight different chunk positions
                     const bool swap = sub & 4;
@@ -733,23 +722,25 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 if (lane == 0) bar_arrive(kv_full(stage));
                 return true;
             };
-            if (share > 0) fetch_scales();
-            for (int at = 0; at < share;) {
+            if (more) fetch_scales();
+            int end_step = list.end_of(cur, share);
+            for (int block = 0; more; ++block) {
                 const int j0 = cur.t.k0 + cur.step * STEP, first = cur.t.kb - j0, end = cur.t.ke - j0;
+                const uint32_t item = 2 * block;
                 // The buffer's last reader was done before the stage that V of this step will take was free, and K's
                 // copy was issued after that.
-                if (!bar_wait(raw_full((2 * at) % C::STAGES), ((uint32_t)(2 * at) / C::STAGES) & 1, gave_up)) break;
-                const uint32_t sc = scales + (at % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
-                // a V scale below 2^-80 counts as 2^-80 (of a vector of zeros, whose scale does not matter, or of values below 1e-21)
-                const float v1 = fmaxf(vs, 8.2718061e-25f);
+                if (!bar_wait(raw_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up)) break;
+                const uint32_t sc = scales + (block % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
+                const float v1 = fmaxf(vs, LEAST_V_SCALE);
                 const float f = seen ? c * ks : 0.0f, lv = seen ? (vs != vs ? vs : __log2f(v1)) : -INFINITY, iv = seen ? 1.0f / v1 : 0.0f;
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc), "f"(f) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + STEP * 4), "f"(lv) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + 2 * STEP * 4), "f"(iv) : "memory");
-                const uint32_t item = 2 * at;
-                ++at;
-                if (++cur.step == cur.t.steps && at < share) list.next(cur);
-                if (at < share) fetch_scales();
+                if (++cur.step == end_step) {
+                    more = list.next(cur, share);
+                    end_step = list.end_of(cur, share);
+                }
+                if (more) fetch_scales();
                 if (!convert(item, first, end) || !convert(item + 1, first, end)) break;
             }
         }

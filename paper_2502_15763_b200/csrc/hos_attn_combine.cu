@@ -1,7 +1,7 @@
 // Second half of an attention call: the pieces of split tiles become outputs.
 //
-// A piece holds, per row, the unnormalised output, the maximum m and the normaliser l of its tokens (exponents
-// in base 2), so out = sum_i 2^(mt_i - m) o_i / sum_i 2^(m_i - m) l_i with m = max_i m_i.  Pieces are added in list
+// A piece holds, per row, the unnormalised output, the reference m and the normaliser l of its tokens (exponents
+// in base 2), so out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i with m = max_i m_i.  Pieces are added in list
 // order.  Launched so that it may start while the attention kernel drains.
 #include "hos_kernels.h"
 #include "hos_kv.cuh"
@@ -9,64 +9,77 @@
 namespace hos {
 namespace {
 
-// Joins the pieces of the tiles that the workers' shares cut: block (w, y) has rows 16 y .. 16 y + 15 of the tile that begins in worker
-// w's share and ends in a later one's; the pieces are slot 1 of w and slot 0 of the workers up to `last`.
-constexpr int COMBINE_WARPS = 8;
+// Worker w's record, if it has one, names the tile that begins in its share and ends in a later one's: the pieces are slot 1
+// of w and slot 0 of the workers up to `last`.  A block looks through the records of every gridDim.x-th worker; its 16 warps
+// take rows, and where there are fewer rows than warps several warps share a row's pieces.  D / 4 lanes read a piece's row.
+constexpr int WARPS = 16, BLOCKS = 4 * ATTN_SMS;
 template <typename T, int D, int ROWS>
-__global__ void __launch_bounds__(COMBINE_WARPS * 32) k_attn_combine(const __grid_constant__ AttnView a, const Partial* __restrict__ meta,
-                                                                    const RowState* __restrict__ state,
-                                                                    const float* __restrict__ part) {
+__global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_constant__ AttnView a, const Partial* __restrict__ meta, const int workers,
+                                                            const RowState* __restrict__ state, const float* __restrict__ part) {
+    constexpr int LANES = D / 4, PER = 32 / LANES;                     // pieces that a warp reads at once
+    __shared__ float4 sum_o[WARPS][LANES];
+    __shared__ float sum_l[WARPS];
+    const int lane = lane_id(), warp = warp_id(), sub = lane / LANES;
     pdl_wait();
-    const int w = (int)blockIdx.x;
-    const Partial p = meta[w];
-    if (p.last < 0) return;
-    constexpr int PER = D / 32;                // elements a lane
-    const SeqInfo q = load_seq(a.kv, p.seq, false);
-    const int rows = min(min(ROWS, q.n * a.group - p.tile * ROWS), (int)(blockIdx.y + 1) * 16);
-    for (int r = blockIdx.y * 16 + warp_id(); r < rows; r += COMBINE_WARPS) {
-        // row state i of the pieces: slot 2w + 1, then 2(w + 1), 2(w + 2), ...
-        auto slot = [&](int i) { return (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * ROWS + r; };
-        const int n = p.last - w + 1;
-        float m = -INFINITY;
-        for (int i = lane_id(); i < n; i += 32) m = fmaxf(m, state[slot(i)].m);
+    for (int w0 = blockIdx.x; w0 < workers; w0 += 32 * gridDim.x) {
+        // 32 records at a time
+        const int wl = w0 + lane * (int)gridDim.x;
+        Partial mine{0, 0, 0, -1};
+        if (wl < workers) mine = meta[wl];
+        for (unsigned some = __ballot_sync(FULL, mine.last >= 0); some; some &= some - 1) {
+            const int src = __ffs(some) - 1, w = w0 + src * (int)gridDim.x;
+            const int seq = __shfl_sync(FULL, mine.seq, src), head = __shfl_sync(FULL, mine.head, src);
+            const int tile = __shfl_sync(FULL, mine.tile, src), n = __shfl_sync(FULL, mine.last, src) - w + 1;
+            const SeqInfo q = load_seq(a.kv, seq, false);
+            const int first = blockIdx.y * 16, rows = min(min(ROWS, q.n * a.group - tile * ROWS) - first, 16);
+            const int shares = rows > 8 ? 1 : rows > 4 ? 2 : rows > 2 ? 4 : rows == 2 ? 8 : 16;   // warps a row
+            const int row = warp / shares, share = warp % shares;
+            const bool busy = row < rows;
+            auto slot = [&](int i) { return (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * ROWS + first + row; };
+            float m = -INFINITY, l = 0.0f;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (busy) {
+                for (int i = lane; i < n; i += 32) m = fmaxf(m, state[slot(i)].m);
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, d));
-        const float ms = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f, o[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            float by = 0.0f;
-            if (i0 + lane_id() < n) {
-                const RowState st = state[slot(i0 + lane_id())];
-                l += st.l * exp2f(st.m - ms);
-                by = st.mt == -INFINITY ? 0.0f : exp2f(st.mt - ms);
-            }
-            const int some = min(32, n - i0);
-#pragma unroll 8
-            for (int i = 0; i < some; ++i) {
-                const float b = __shfl_sync(FULL, by, i);
-                const float* src = part + slot(i0 + i) * D + lane_id() * PER;
-                if (PER == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(src);
-                    o[0] += b * v.x; o[1] += b * v.y; o[PER - 2] += b * v.z; o[PER - 1] += b * v.w;
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
-                    o[0] += b * v.x; o[1] += b * v.y;
+                for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, d));
+                const float ms = m == -INFINITY ? 0.0f : m;
+                // pieces share * PER + sub, + shares * PER, ...
+#pragma unroll 4
+                for (int i = share * PER + sub; i < n; i += shares * PER) {
+                    const RowState st = state[slot(i)];
+                    const float4 v = reinterpret_cast<const float4*>(part + slot(i) * D)[lane % LANES];
+                    const float by = exp2f(st.m - ms);
+                    if (lane % LANES == 0) l += st.l * by;
+                    o.x += by * v.x; o.y += by * v.y; o.z += by * v.z; o.w += by * v.w;
                 }
+                if (PER == 2) {
+                    o.x += __shfl_xor_sync(FULL, o.x, 16); o.y += __shfl_xor_sync(FULL, o.y, 16);
+                    o.z += __shfl_xor_sync(FULL, o.z, 16); o.w += __shfl_xor_sync(FULL, o.w, 16);
+                    l += __shfl_xor_sync(FULL, l, 16);
+                }
+                if (lane < LANES) sum_o[warp][lane] = o;
+                if (lane == 0) sum_l[warp] = l;
             }
+            __syncthreads();
+            if (busy && share == 0) {
+                l = 0.0f;
+                for (int k = 0; k < shares; ++k) l += sum_l[warp + k];
+                const float by = l == 0.0f ? 0.0f : 1.0f / l;
+                const int r = tile * ROWS + first + row, tok = q.off + r / a.group, hd = head * a.group + r % a.group;
+                if (lane < LANES) {
+                    o = sum_o[warp][lane];
+                    for (int k = 1; k < shares; ++k) {
+                        const float4 v = sum_o[warp + k][lane];
+                        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+                    }
+                    T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head;
+                    reinterpret_cast<uint2*>(dst)[lane] = make_uint2(Pair<T>::pack(o.x * by, o.y * by), Pair<T>::pack(o.z * by, o.w * by));
+                }
+                if (a.lse && lane == 0)
+                    a.lse[(long long)tok * a.n_heads + hd] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+            }
+            __syncthreads();
         }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(FULL, l, d);
-        const float by = l == 0.0f ? 0.0f : 1.0f / l;
-        const int row = p.tile * ROWS + r, tok = q.off + row / a.group, hd = p.head * a.group + row % a.group;
-        T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head + lane_id() * PER;
-        if (PER == 4)
-            *reinterpret_cast<uint2*>(dst) = make_uint2(Pair<T>::pack(o[0] * by, o[1] * by), Pair<T>::pack(o[PER - 2] * by, o[PER - 1] * by));
-        else
-            *reinterpret_cast<uint32_t*>(dst) = Pair<T>::pack(o[0] * by, o[1] * by);
-        if (a.lse && lane_id() == 0)
-            a.lse[(long long)tok * a.n_heads + hd] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
     }
 }
 
@@ -76,13 +89,13 @@ cudaError_t run(const AttnView& a, int workers, const Partial* meta, const RowSt
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)workers, (ROWS + 15) / 16);
-    cfg.blockDim = dim3(COMBINE_WARPS * 32);
+    cfg.gridDim = dim3((unsigned)(workers < BLOCKS ? workers : BLOCKS), (ROWS + 15) / 16);
+    cfg.blockDim = dim3(WARPS * 32);
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     launch_hook("k_attn_combine", 0, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D, ROWS>, a, meta, state, part);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D, ROWS>, a, meta, workers, state, part);
     launch_hook("k_attn_combine", 1, st);
     return e;
 }

@@ -1,6 +1,10 @@
 // The work list of an attention call: steps of STEP tokens, in the order (sequence, KV head, tile of ROWS
 // rows, step).  Rows of a sequence and KV head are its new tokens times the query heads of the group,
 // token by token.  Nothing is stored: a worker finds its place in the list from the lengths alone.
+//
+// A tile costs a worker more than its steps (queries in, result out), so it counts START steps more: these
+// come first and hold no work.  A share that begins among them begins with the tile's first real step,
+// one that ends among them ends before the tile.
 #pragma once
 
 #include "hos_kv.cuh"
@@ -16,13 +20,14 @@ __device__ __forceinline__ long long warp_scan_i64(long long v) {
     return v;
 }
 
-template <int ROWS, int STEP> struct AttnList {
+template <int ROWS, int STEP, int START> struct AttnList {
     const AttnView& a;
     int min_rows, max_rows;                    // sequences with rows in (min_rows, max_rows] are in the list
 
     struct Tile { int k0, kb, ke, steps, rows; };   // steps from k0 on; tokens [kb, ke) are seen by some row
     struct Cursor {
         int seq, head, tile, tiles, step;
+        int at;                                // where the tile begins in the list, relative to the share's begin
         SeqInfo q;
         Tile t;
     };
@@ -45,13 +50,13 @@ template <int ROWS, int STEP> struct AttnList {
         return r > min_rows && r <= max_rows;
     }
 
-    // Steps of one KV head of this lane's sequence (called by the whole warp; q.n = 0 for none).  Sequences
+    // Length in the list of one KV head of this lane's sequence (called by the whole warp; q.n = 0 for none).  Sequences
     // of more than two tiles are summed by all lanes together.
     __device__ __forceinline__ long long steps_of(const SeqInfo& q) const {
         long long sum = 0;
         const int nt = has(q) ? tiles_of(q) : 0;
         if (nt > 0 && nt <= 2)
-            for (int t = 0; t < nt; ++t) sum += tile_of(q, t).steps;
+            for (int t = 0; t < nt; ++t) sum += tile_of(q, t).steps + START;
         for (unsigned big = __ballot_sync(FULL, nt > 2); big; big &= big - 1) {
             const int l = __ffs(big) - 1;
             SeqInfo b;
@@ -60,7 +65,7 @@ template <int ROWS, int STEP> struct AttnList {
             b.len = __shfl_sync(FULL, q.len, l);
             const int n = tiles_of(b);
             unsigned long long part = 0;
-            for (int t = lane_id(); t < n; t += 32) part += (unsigned long long)tile_of(b, t).steps;
+            for (int t = lane_id(); t < n; t += 32) part += (unsigned long long)(tile_of(b, t).steps + START);
             part = warp_sum_u64(part);
             if (lane_id() == l) sum = (long long)part;
         }
@@ -72,15 +77,19 @@ template <int ROWS, int STEP> struct AttnList {
         return q;
     }
 
-    // Steps of the whole list; `flag`: report sequences with bad offsets or lengths.
+    // Length of the whole list; `flag`: report sequences with bad offsets or lengths.
     __device__ __forceinline__ long long total(bool flag) const {
         long long sum = 0;
         for (int s0 = 0; s0 < a.kv.n_seq; s0 += 32) sum += steps_of(lane_seq(s0 + lane_id(), flag));
         return (long long)warp_sum_u64((unsigned long long)sum) * a.kv.n_kv;
     }
 
-    // To the next tile (the caller knows that there is one).
-    __device__ __forceinline__ void next(Cursor& c) const {
+    // The real steps of the cursor's tile below this one belong to a share of `length`.
+    __device__ __forceinline__ int end_of(const Cursor& c, int length) const { return min(c.t.steps, length - c.at - START); }
+    // To the next tile; false if none of its steps belong to the share.
+    __device__ __forceinline__ bool next(Cursor& c, int length) const {
+        c.at += START + c.t.steps;
+        if (c.at + START >= length) return false;
         c.step = 0;
         if (++c.tile == c.tiles) {
             c.tile = 0;
@@ -94,9 +103,10 @@ template <int ROWS, int STEP> struct AttnList {
             }
         }
         c.t = tile_of(c.q, c.tile);
+        return true;
     }
 
-    // Step number `at` (below the total) of the list; called by the whole warp.
+    // Place number `at` (below the total) of the list; called by the whole warp.
     __device__ __forceinline__ Cursor locate(long long at) const {
         Cursor c;
         long long before = 0, per_head = 1;
@@ -121,7 +131,7 @@ template <int ROWS, int STEP> struct AttnList {
         rest -= (long long)c.head * per_head;
         c.tile = 0;
         for (int t0 = 0; t0 < c.tiles; t0 += 32) {
-            const int steps = t0 + lane_id() < c.tiles ? tile_of(c.q, t0 + lane_id()).steps : 0;
+            const int steps = t0 + lane_id() < c.tiles ? tile_of(c.q, t0 + lane_id()).steps + START : 0;
             const long long scan = warp_scan_i64(steps);
             const unsigned hit = __ballot_sync(FULL, scan > rest);
             if (hit) {
@@ -133,7 +143,8 @@ template <int ROWS, int STEP> struct AttnList {
             rest -= __shfl_sync(FULL, scan, 31);
         }
         c.t = tile_of(c.q, c.tile);
-        c.step = (int)rest;
+        c.at = -(int)rest;
+        c.step = max(0, (int)rest - START);
         return c;
     }
 };

@@ -2,11 +2,12 @@
 //
 // What bounds it: the cache is read once, 2 * head_dim multiply-adds per cached element and 16 rows at
 // most, so HBM.  The kernel is built to keep loads in flight and nothing else:
-//   - The work is a list of steps of 16 tokens (sequence, KV head, tile of 8 or 16 rows, step).  Every WARP
-//     takes an equal, contiguous share of the list, whatever the lengths are; there is no barrier
-//     wider than a warp.  A tile cut by the ends of a share leaves a partial result (unnormalised output,
-//     maximum, normaliser) in the workspace, and k_attn_combine joins the pieces in list order, so the
-//     result does not depend on which warp finished first.
+//   - The work is a list of steps of 16 or 32 tokens (sequence, KV head, tile of 8 or 16 rows, step).  Every CTA
+//     of four warps takes an equal, contiguous share of the list, whatever the lengths are; within a tile the
+//     steps go round the warps, which meet only at the tile's end to add up their parts.  A tile cut by
+//     the ends of a share leaves a partial result (unnormalised output, reference, normaliser) in the
+//     workspace, and k_attn_combine joins the pieces in list order, so the result does not depend on which
+//     CTA finished first.
 //   - A warp copies its next steps into its own ring in shared memory (16-byte asynchronous copies), over
 //     the ends of tiles and sequences, while it works on the current one.
 //   - Rows are the query heads of a group times the new tokens.  Both products are 16x8x16 matrix
@@ -16,8 +17,8 @@
 //     operands as whole 16-byte chunks of K and V rows; nothing is transposed but pairs of V rows (one byte
 //     permute a register) and the weights (one 8x8 exchange a half step).
 //   - 8-bit codes become fp16 exactly; K's scale multiplies the score, V's scale joins the exponent of
-//     the weight (w_j = exp2(x_j + log2 vs_j - max of that)), so no weight under- or overflows fp16
-//     whatever the scales are.
+//     the weight (w_j = 2^(x_j + log2 vs_j - m), m the maximum of that), so no weight under- or overflows fp16
+//     whatever the scales are; the normaliser is sum w_j / vs_j.
 #include "hos_attn_list.cuh"
 #include "hos_kernels.h"
 #include "hos_kv.cuh"
@@ -25,21 +26,24 @@
 namespace hos {
 namespace {
 
-constexpr int STEP = 16, WARPS = 4;
-constexpr int MIN_STEPS = 2;                  // a worker's smallest share; fewer and the joining costs more than it saves
+constexpr int WARPS = 4;
 
 template <typename T, int FMT, int D, int NB> struct Cfg {
     static constexpr bool Q8 = FMT != HOS_KV_SAME;
     static constexpr int ROWS = 8 * NB;
     static constexpr int ROW_BYTES = Q8 ? D : 2 * D;
     static constexpr int CHUNKS = ROW_BYTES / 16;
+    // Steps of 32 tokens share the reductions over tokens; with rows of 256 bytes their ring would leave too few warps.
+    static constexpr int SUB = ROW_BYTES > 128 ? 1 : 2, STEP = 16 * SUB;
     static constexpr int KV_BYTES = STEP * ROW_BYTES;
     static constexpr int STAGE = 2 * KV_BYTES + (Q8 ? 2 * STEP * 4 : 0);
-    // CTAs of four warps on an SM, and the ring of each warp: as many bytes as fit
-    static constexpr int CTAS = !Q8 && D == 128 ? 2 : NB == 1 ? 4 : 2;
-    static constexpr int STAGES = (int)(SMEM_LIMIT / CTAS - 1024) / (WARPS * STAGE) < 8 ? (int)(SMEM_LIMIT / CTAS - 1024) / (WARPS * STAGE) : 8;
+    // CTAs on an SM, and the ring of each warp: as many bytes as fit
+    static constexpr int CTAS = SUB == 1 || NB == 2 ? 2 : 3;
+    static constexpr int FIT = (int)(SMEM_LIMIT / CTAS - 2048) / (WARPS * STAGE), STAGES = FIT < 8 ? FIT : 8;
     static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
+constexpr int MIN_STEPS = WARPS;              // a CTA's smallest share
+constexpr int TILE_STEPS = 4;                 // what a tile's begin and end cost, in steps
 // A row's weights are 2^(x - (maximum - LIFT)): in fp16 the largest is 2^14, so that small ones keep their bits
 // down to 2^-28 of it.
 template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 14.0f : 0.0f;
@@ -55,7 +59,7 @@ template <int CHUNKS> __device__ __forceinline__ int swizzle(int r) {
 // Transposes an 8x8 matrix of 16-bit elements held as one pair a lane (lane / 4: row, lane % 4: pair of columns).
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 // Over the eight lanes of a column of 8x8 results.
@@ -76,38 +80,60 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
             RowState* __restrict__ state, float* __restrict__ part) {
     using C = Cfg<T, FMT, D, NB>;
     using M = typename MatType<T, FMT>::type;
-    using List = AttnList<C::ROWS, STEP>;
+    constexpr int STEP = C::STEP, SUB = C::SUB;
+    using List = AttnList<C::ROWS, STEP, TILE_STEPS>;
     using Cursor = typename List::Cursor;
     constexpr int ROWS = C::ROWS;
     constexpr int KS = D / 16;                 // matrix instructions along head_dim, and tiles of O^T
     extern __shared__ __align__(128) unsigned char smem[];
-    const int lane = lane_id(), g = lane >> 2, t4 = lane & 3;
-    const int workers = (int)gridDim.x * WARPS;
-    const int w = warp_id() * (int)gridDim.x + (int)blockIdx.x;
+    __shared__ RowState warp_state[WARPS][ROWS];
+    const int lane = lane_id(), warp = warp_id(), g = lane >> 2, t4 = lane & 3;
+    const int w = (int)blockIdx.x;
     pdl_launch_dependents();
 
-    // this warp's share of the list
+    // this CTA's share of the list
     const List list{a, 0, max_rows};
-    const long long total = list.total(w == 0);
-    const int active = (int)min((long long)workers, (total + MIN_STEPS - 1) / MIN_STEPS);
+    const long long total = list.total(w == 0 && warp == 0);
+    const int active = (int)min((long long)gridDim.x, (total + MIN_STEPS - 1) / MIN_STEPS);
     if (w >= active) {
-        if (lane == 0) meta[w].last = -1;
+        if (threadIdx.x == 0) meta[w].last = -1;
         return;
     }
-    const long long lo = total * w / active, hi = total * (w + 1) / active;
+    const long long lo = total * w / active;
+    const int share = (int)(total * (w + 1) / active - lo);
     Cursor cons = list.locate(lo);
+    // where the copies are: this warp's steps of a tile, every fourth one, then the next tile
     Cursor prod = cons;
-    int to_issue = (int)(hi - lo);
-    const uint32_t ring = smem_u32(smem) + warp_id() * C::STAGES * C::STAGE;
+    int prod_end = list.end_of(prod, share);
+    bool prod_more = prod.step < prod_end;
+    prod.step += warp;
+    const uint32_t ring = smem_u32(smem) + warp * C::STAGES * C::STAGE;
 
     // --- copies -------------------------------------------------------------------------------
     int pages = 0, pages_at = -1;              // this lane's entry of 32 cached page numbers, and the first one's index
+    constexpr int PASSES = 16 * C::CHUNKS / 32, PERIOD = C::CHUNKS / 4;        // copies of 512 bytes for 16 rows; for 8
+    uint32_t dst_at[PERIOD];                   // where this lane's chunk goes: the layout repeats every 8 rows
+#pragma unroll
+    for (int i = 0; i < PERIOD; ++i) {
+        const int id = i * 32 + lane, r = id / C::CHUNKS, c = id % C::CHUNKS;
+        dst_at[i] = r * C::ROW_BYTES + ((c ^ swizzle<C::CHUNKS>(r)) * 16);
+    }
+    auto dst_of = [&](int i) { return dst_at[i % PERIOD] + (i / PERIOD) * 8 * C::ROW_BYTES; };
+    auto settle = [&]() {                      // to this warp's next step, if it has one
+        while (prod_more && prod.step >= prod_end) {
+            prod_more = list.next(prod, share);
+            prod_end = list.end_of(prod, share);
+            prod.step = warp;
+            pages_at = -1;
+        }
+    };
+    settle();
     auto issue = [&](int stage) {
-        if (to_issue > 0) {
-            --to_issue;
+        if (prod_more) {
             const int j0 = prod.t.k0 + prod.step * STEP;
             const int pi = j0 >> a.kv.page_shift;
-            if (pages_at < 0 || pi >= pages_at + 32) {
+            // a step of 32 tokens may be two pages of 16
+            if (pages_at < 0 || ((j0 + STEP - 1) >> a.kv.page_shift) >= pages_at + 32) {
                 pages_at = pi;
                 pages = -1;
                 if (pi + lane <= (prod.t.ke - 1) >> a.kv.page_shift && prod.t.ke > 0) {
@@ -118,28 +144,38 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                     }
                 }
             }
-            const int page = __shfl_sync(FULL, pages, pi - pages_at);
-            const int row0 = j0 & ((1 << a.kv.page_shift) - 1);
-            const long long e = page_elem(a.kv, max(page, 0), prod.head, row0) * (C::Q8 ? 1 : 2);
-            const unsigned char* ksrc = a.kv.k + e;
-            const unsigned char* vsrc = a.kv.v + e;
             const uint32_t kd = ring + stage * C::STAGE, vd = kd + C::KV_BYTES;
 #pragma unroll
-            for (int it = 0; it < STEP * C::CHUNKS / 32; ++it) {
-                const int id = it * 32 + lane, r = id / C::CHUNKS, c = id % C::CHUNKS;
-                const bool real = page >= 0 && j0 + r >= prod.t.kb && j0 + r < prod.t.ke;
-                const uint32_t dst = r * C::ROW_BYTES + ((c ^ swizzle<C::CHUNKS>(r)) * 16);
-                cp_async16(kd + dst, ksrc + (long long)id * 16, real);
-                cp_async16(vd + dst, vsrc + (long long)id * 16, real);
+            for (int sub = 0; sub < SUB; ++sub) {
+                const int js = j0 + 16 * sub, row0 = js & ((1 << a.kv.page_shift) - 1);
+                const int page = __shfl_sync(FULL, pages, (js >> a.kv.page_shift) - pages_at);
+                const long long e = page_elem(a.kv, max(page, 0), prod.head, row0) * (C::Q8 ? 1 : 2) + lane * 16;
+                const unsigned char* ksrc = a.kv.k + e;
+                const unsigned char* vsrc = a.kv.v + e;
+                const uint32_t ks = kd + sub * 16 * C::ROW_BYTES, vs = ks + C::KV_BYTES;
+                if (page >= 0 && js >= prod.t.kb && js + 16 <= prod.t.ke) {
+#pragma unroll
+                    for (int i = 0; i < PASSES; ++i) {
+                        cp_async16(ks + dst_of(i), ksrc + i * 512);
+                        cp_async16(vs + dst_of(i), vsrc + i * 512);
+                    }
+                } else {                       // tokens that no row sees become zeros, whatever memory holds
+#pragma unroll
+                    for (int i = 0; i < PASSES; ++i) {
+                        const int j = js + (i * 32 + lane) / C::CHUNKS;
+                        const bool real = page >= 0 && j >= prod.t.kb && j < prod.t.ke;
+                        cp_async16(ks + dst_of(i), ksrc + i * 512, real);
+                        cp_async16(vs + dst_of(i), vsrc + i * 512, real);
+                    }
+                }
+                if (C::Q8 && lane < 8) {
+                    const long long se = scale_elem(a.kv, max(page, 0), prod.head, row0) + (lane & 3) * 4;
+                    cp_async16(vd + C::KV_BYTES + (lane < 4 ? 0 : STEP * 4) + sub * 64 + (lane & 3) * 16,
+                               (lane < 4 ? a.kv.k_scale : a.kv.v_scale) + se, page >= 0);
+                }
             }
-            if (C::Q8 && lane < 8) {
-                const long long se = scale_elem(a.kv, max(page, 0), prod.head, row0) + (lane & 3) * 4;
-                cp_async16(vd + C::KV_BYTES + lane * 16, (lane < 4 ? a.kv.k_scale : a.kv.v_scale) + se, page >= 0);
-            }
-            if (++prod.step == prod.t.steps && to_issue > 0) {
-                list.next(prod);
-                pages_at = -1;
-            }
+            prod.step += WARPS;
+            settle();
         }
         cp_async_commit();
     };
@@ -150,12 +186,19 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     // as columns of a product: row nb * 8 + g when read, rows nb * 8 + 2 * t4 + {0, 1} of the results
     uint32_t bq[KS][NB][2];
     float o[KS][NB][4];
-    float m[NB][2], l[NB][2], mt[NB][2], qmul[NB][2];
+    float m[NB][2], l[NB][2], qmul[NB][2];     // m: the exponents' reference, the running maximum - LIFT
     int see_lo[NB][2], see_hi[NB][2];          // visible tokens
+    int all_lo = 0, all_hi = 0;                // tokens that every row of the tile sees
     const int f = swizzle<C::CHUNKS>(g);
     const uint32_t k_at = g * C::ROW_BYTES + (t4 ^ (f & 3)) * 16, k_x = (f & 4) * 16;
 
     auto begin = [&]() {
+        {
+            const int first = cons.q.len - cons.q.n + cons.tile * ROWS / a.group;
+            const int last = cons.q.len - cons.q.n + (cons.tile * ROWS + cons.t.rows - 1) / a.group;
+            all_hi = a.causal ? min(cons.q.len, first + 1) : cons.q.len;
+            all_lo = a.window > 0 ? max(0, last - a.window + 1) : 0;
+        }
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
@@ -206,144 +249,241 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
             for (int e = 0; e < 2; ++e) {
                 const int r2 = cons.tile * ROWS + nb * 8 + 2 * t4 + e;
                 const int pos = cons.q.len - cons.q.n + r2 / a.group;
-                see_hi[nb][e] = nb * 8 + 2 * t4 + e < cons.t.rows ? (a.causal ? min(cons.q.len, pos + 1) : cons.q.len) : 0;
-                see_lo[nb][e] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+                // columns past the tile see everything that its rows do; they are not written
+                const bool real = nb * 8 + 2 * t4 + e < cons.t.rows;
+                see_hi[nb][e] = real && a.causal ? min(cons.q.len, pos + 1) : cons.q.len;
+                see_lo[nb][e] = real && a.window > 0 ? max(0, pos - a.window + 1) : 0;
                 qmul[nb][e] = __shfl_sync(FULL, mul, (2 * t4 + e) * 4);
-                m[nb][e] = mt[nb][e] = -INFINITY;
+                m[nb][e] = -INFINITY;
                 l[nb][e] = 0.0f;
             }
         }
     };
 
-    // Tiles 4 q .. 4 q + 3 of O^T are eight consecutive elements of head_dim in this lane.
-    auto dim_of = [&](int q) { return C::Q8 && D == 128 ? g * 16 + q * 8 : q * 64 + g * 8; };
+    int stage = 0;
+    // Element of head_dim of this lane's first value of tile i of O^T (the second one's is the next).
+    auto dim_of = [&](int i) { return C::Q8 && D == 128 ? g * 16 + i * 2 : (i >> 2) * 64 + g * 8 + (i & 3) * 2; };
     bool open_end = false;
-    int seg_first = cons.step;                 // the step of the tile this warp began with
-    auto finish = [&](long long unit) {
-        const bool whole_start = seg_first == 0, whole_end = cons.step == cons.t.steps - 1;
+    // The four warps' parts of a tile are added up: warp k ends with tiles OWN k .. OWN k + OWN - 1 of O^T and writes them.
+    // What it has of the others' tiles goes through its stage that was read last (nothing is on its way there).
+    auto finish = [&](bool whole_start, bool whole_end, long long end) {
+        constexpr int OWN = KS / WARPS;
         const bool whole = whole_start && whole_end;
-        const int slot = 2 * w + (whole_start ? 1 : 0);
+        auto buffer = [&](int k, int st) { return smem_u32(smem) + (k * C::STAGES + st) * C::STAGE + lane * (OWN * NB * 16); };
+        __shared__ int free_stage[WARPS];
+        const int free = stage == 0 ? C::STAGES - 1 : stage - 1;
+        if (lane == 0) free_stage[warp] = free;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {
+            if (k == warp) continue;
+            const uint32_t at = buffer(warp, free) + ((k - (k > warp ? 1 : 0)) * 32) * (OWN * NB * 16);
+#pragma unroll
+            for (int i = 0; i < OWN; ++i)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(at + (i * NB + nb) * 16), "f"(o[k * OWN + i][nb][0]),
+                                 "f"(o[k * OWN + i][nb][1]), "f"(o[k * OWN + i][nb][2]), "f"(o[k * OWN + i][nb][3]) : "memory");
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float sum = column_sum(l[nb][e]);
+                if (g == 0) warp_state[warp][nb * 8 + 2 * t4 + e] = RowState{m[nb][e], sum};
+            }
+        __syncthreads();
+        float ref[NB][2], norm[NB][2], by[WARPS][NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = nb * 8 + 2 * t4 + e;
+                float top = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < WARPS; ++k) top = fmaxf(top, warp_state[k][r].m);
+                const float ms = top == -INFINITY ? 0.0f : top;
+                ref[nb][e] = top;
+                norm[nb][e] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < WARPS; ++k) {
+                    by[k][nb][e] = exp2_fast(warp_state[k][r].m - ms);
+                    norm[nb][e] = fmaf(warp_state[k][r].l, by[k][nb][e], norm[nb][e]);
+                }
+            }
+        float own[OWN][NB][4];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) own[i][nb][j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {      // in the order of the warps, whichever one adds
+            if (k == warp) {
+#pragma unroll
+                for (int i = 0; i < OWN; ++i)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float v = o[i][nb][j];
+#pragma unroll
+                            for (int q = 1; q < WARPS; ++q) v = warp == q ? o[q * OWN + i][nb][j] : v;
+                            own[i][nb][j] = fmaf(v, by[k][nb][j & 1], own[i][nb][j]);
+                        }
+            } else {
+                const uint32_t at = buffer(k, free_stage[k]) + ((warp - (warp > k ? 1 : 0)) * 32) * (OWN * NB * 16);
+#pragma unroll
+                for (int i = 0; i < OWN; ++i)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const uint4 v = lds<uint4>(at + (i * NB + nb) * 16);
+                        own[i][nb][0] = fmaf(__uint_as_float(v.x), by[k][nb][0], own[i][nb][0]);
+                        own[i][nb][1] = fmaf(__uint_as_float(v.y), by[k][nb][1], own[i][nb][1]);
+                        own[i][nb][2] = fmaf(__uint_as_float(v.z), by[k][nb][0], own[i][nb][2]);
+                        own[i][nb][3] = fmaf(__uint_as_float(v.w), by[k][nb][1], own[i][nb][3]);
+                    }
+            }
+        }
+        const int slot = 2 * w + (whole_start ? 1 : 0);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
                 const int in_tile = nb * 8 + 2 * t4 + e;
                 if (in_tile >= cons.t.rows) continue;
+                const int d0 = dim_of(warp * OWN);
                 if (whole) {
                     const int r = cons.tile * ROWS + in_tile;
                     const int tok = cons.q.off + r / a.group, hd = cons.head * a.group + r % a.group;
-                    float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    if (C::Q8 && sum != 0.0f) by *= exp2f(mt[nb][e] - m[nb][e]);
-                    T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head;
+                    const float inv = norm[nb][e] == 0.0f ? 0.0f : 1.0f / norm[nb][e];
+                    T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head + d0;
+                    uint32_t v[OWN];
 #pragma unroll
-                    for (int q = 0; q < KS / 4; ++q) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = Pair<T>::pack(o[4 * q + i][nb][e] * by, o[4 * q + i][nb][2 + e] * by);
-                        *reinterpret_cast<uint4*>(dst + dim_of(q)) = make_uint4(v[0], v[1], v[2], v[3]);
-                    }
-                    if (a.lse && g == 0)
+                    for (int i = 0; i < OWN; ++i) v[i] = Pair<T>::pack(own[i][nb][e] * inv, own[i][nb][2 + e] * inv);
+                    if (OWN == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(v[0], v[OWN - 1]);
+                    else *reinterpret_cast<uint32_t*>(dst) = v[0];
+                    if (a.lse && g == 0 && warp == 0)
                         a.lse[(long long)tok * a.n_heads + hd] =
-                            sum == 0.0f ? -INFINITY : (m[nb][e] + log2f(sum)) * 0.69314718055994530942f;
+                            norm[nb][e] == 0.0f ? -INFINITY : (ref[nb][e] + log2f(norm[nb][e])) * 0.69314718055994530942f;
                 } else {
                     const long long r = (long long)slot * ROWS + in_tile;
-#pragma unroll
-                    for (int q = 0; q < KS / 4; ++q)
-#pragma unroll
-                        for (int i = 0; i < 4; i += 2)
-                            *reinterpret_cast<float4*>(part + r * D + dim_of(q) + 2 * i) =
-                                make_float4(o[4 * q + i][nb][e], o[4 * q + i][nb][2 + e], o[4 * q + i + 1][nb][e], o[4 * q + i + 1][nb][2 + e]);
-                    if (g == 0) state[r] = RowState{m[nb][e], sum, C::Q8 ? mt[nb][e] : m[nb][e], 0.0f};
+                    float* dst = part + r * D + d0;
+                    if (OWN == 2)
+                        *reinterpret_cast<float4*>(dst) = make_float4(own[0][nb][e], own[0][nb][2 + e], own[OWN - 1][nb][e], own[OWN - 1][nb][2 + e]);
+                    else
+                        *reinterpret_cast<float2*>(dst) = make_float2(own[0][nb][e], own[0][nb][2 + e]);
+                    if (g == 0 && warp == 0) state[r] = RowState{ref[nb][e], norm[nb][e]};
                 }
             }
-        if (!whole && whole_start && lane == 0) {
-            const long long end = unit + (cons.t.steps - cons.step);      // one past the tile's last step
+        if (!whole && whole_start && threadIdx.x == 0)
             meta[w] = Partial{cons.seq, cons.head, cons.tile, (int)((end * active - 1) / total)};
-        }
         open_end = whole_start && !whole_end;
+        __syncthreads();                       // the buffers may be written again
     };
 
-    begin();
-    int stage = 0;
+    for (bool more = cons.step < list.end_of(cons, share); more; more = list.next(cons, share)) {
+        begin();
+        const int first = cons.step, end = list.end_of(cons, share);
 #pragma unroll 1
-    for (long long unit = lo; unit < hi; ++unit) {
+    for (int step = first + warp; step < end; step += WARPS) {
         cp_async_wait<C::STAGES - 2>();
         __syncwarp();
         issue(stage == 0 ? C::STAGES - 1 : stage - 1);
         const uint32_t kd = ring + stage * C::STAGE, vd = kd + C::KV_BYTES;
         if (++stage == C::STAGES) stage = 0;
 
-        // scores: x[nb][0..1] token g, x[nb][2..3] token g + 8, rows nb * 8 + 2 * t4 + {0, 1}
-        float x[NB][4];
+        // scores: x[sub][nb][0..1] token g, x[sub][nb][2..3] token g + 8 of 16, rows nb * 8 + 2 * t4 + {0, 1}
+        float x[SUB][NB][4];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int sub = 0; sub < SUB; ++sub) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[nb][j] = 0.0f;
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int c = 0; c < C::CHUNKS / 4; ++c) {
-            const uint4 v0 = lds128(kd + k_at + ((c * 64) ^ k_x)), v1 = lds128(kd + 8 * C::ROW_BYTES + k_at + ((c * 64) ^ k_x));
-            const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-            if (!C::Q8) {
+                for (int j = 0; j < 4; ++j) x[sub][nb][j] = 0.0f;
+            const uint32_t ka = kd + sub * 16 * C::ROW_BYTES + k_at;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t ak[4] = {w0[2 * i], w1[2 * i], w0[2 * i + 1], w1[2 * i + 1]};
+            for (int c = 0; c < C::CHUNKS / 4; ++c) {
+                const uint4 v0 = lds<uint4>(ka + ((c * 64) ^ k_x)), v1 = lds<uint4>(ka + 8 * C::ROW_BYTES + ((c * 64) ^ k_x));
+                const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+                if (!C::Q8) {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(x[nb], ak, bq[2 * c + i][nb][0], bq[2 * c + i][nb][1]);
-                }
-            } else {
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t ak[4] = {w0[2 * i], w1[2 * i], w0[2 * i + 1], w1[2 * i + 1]};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t ak[4] = {codes_to_half2<FMT>(w0[i]), codes_to_half2<FMT>(w1[i]), codes_to_half2<FMT>(w0[i] >> 16),
-                                            codes_to_half2<FMT>(w1[i] >> 16)};
+                        for (int nb = 0; nb < NB; ++nb) mma16816<M>(x[sub][nb], ak, bq[2 * c + i][nb][0], bq[2 * c + i][nb][1]);
+                    }
+                } else {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(x[nb], ak, bq[(4 * c + i) % KS][nb][0], bq[(4 * c + i) % KS][nb][1]);
+                    for (int i = 0; i < 4; ++i) {
+                        const uint2 h0 = codes_to_half4<FMT>(w0[i]), h1 = codes_to_half4<FMT>(w1[i]);
+                        const uint32_t ak[4] = {h0.x, h1.x, h0.y, h1.y};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+                            mma16816<M>(x[sub][nb], ak, bq[(4 * c + i) % KS][nb][0], bq[(4 * c + i) % KS][nb][1]);
+                    }
                 }
             }
         }
-        const int j0 = cons.t.k0 + cons.step * STEP;
-        float ks[2] = {1.0f, 1.0f}, lv[2] = {0.0f, 0.0f};      // of tokens g and g + 8: K's scale, log2 of V's
-        if (C::Q8) {
+        const int j0 = cons.t.k0 + step * STEP;
+        const bool edge = j0 < all_lo || j0 + STEP > all_hi;
+        // of tokens g and g + 8: K's scale; log2 of V's scale, which joins the exponent, and its inverse, which takes it out of
+        // the normaliser again
+        float iv[SUB][2];
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                ks[i] = lds32f(vd + C::KV_BYTES + (g + 8 * i) * 4);
-                lv[i] = __log2f(lds32f(vd + C::KV_BYTES + (STEP + g + 8 * i) * 4));
+                float ks = 1.0f, lv = 0.0f;
+                iv[sub][i] = 1.0f;
+                if (C::Q8) {
+                    ks = lds<float>(vd + C::KV_BYTES + (16 * sub + g + 8 * i) * 4);
+                    const float vs = lds<float>(vd + C::KV_BYTES + (STEP + 16 * sub + g + 8 * i) * 4);
+                    const float v1 = vs < LEAST_V_SCALE ? LEAST_V_SCALE : vs;      // a NaN stays one
+                    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v1));
+                    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[sub][i]) : "f"(v1));
+                }
+                const int tok = j0 + 16 * sub + g + 8 * i;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float& v = x[sub][nb][2 * i + e];
+                        v = C::Q8 ? fmaf(v, qmul[nb][e] * ks, lv) : v * a.scale_log2;
+                        if (edge && (tok < see_lo[nb][e] || tok >= see_hi[nb][e])) v = -INFINITY;
+                    }
+                if (edge && (tok < cons.t.kb || tok >= cons.t.ke)) iv[sub][i] = 0.0f;      // its scale may be anything
             }
-        }
         float shrink[NB][2];
-        uint32_t bp[NB][2];
+        uint32_t bp[SUB][NB][2];
         bool moved = false;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            float p[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int e = j & 1, tok = j0 + g + 8 * (j >> 1);
-                x[nb][j] *= C::Q8 ? qmul[nb][e] * ks[j >> 1] : a.scale_log2;
-                if (tok < see_lo[nb][e] || tok >= see_hi[nb][e]) x[nb][j] = -INFINITY;
-            }
+            float p[SUB][4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float top = column_max(fmaxf(x[nb][e], x[nb][2 + e]));
-                const float mn = fmaxf(m[nb][e], C::Q8 ? top : top - LIFT<M>), ms = mn == -INFINITY ? 0.0f : mn;
+                float top = fmaxf(x[0][nb][e], x[0][nb][2 + e]);
+                if (SUB == 2) top = fmaxf(top, fmaxf(x[SUB - 1][nb][e], x[SUB - 1][nb][2 + e]));
+                top = column_max(top);
+                const float mn = fmaxf(m[nb][e], top - LIFT<M>), ms = mn == -INFINITY ? 0.0f : mn;
                 shrink[nb][e] = exp2_fast(m[nb][e] - ms);
                 m[nb][e] = mn;
-                p[e] = exp2_fast(x[nb][e] - ms);
-                p[2 + e] = exp2_fast(x[nb][2 + e] - ms);
-                l[nb][e] = l[nb][e] * shrink[nb][e] + (p[e] + p[2 + e]);
-                if (C::Q8) {
-                    const float y0 = x[nb][e] == -INFINITY ? -INFINITY : x[nb][e] + lv[0];
-                    const float y1 = x[nb][2 + e] == -INFINITY ? -INFINITY : x[nb][2 + e] + lv[1];
-                    const float yn = fmaxf(mt[nb][e], column_max(fmaxf(y0, y1)) - LIFT<M>), ys = yn == -INFINITY ? 0.0f : yn;
-                    shrink[nb][e] = exp2_fast(mt[nb][e] - ys);
-                    mt[nb][e] = yn;
-                    p[e] = exp2_fast(y0 - ys);
-                    p[2 + e] = exp2_fast(y1 - ys);
-                }
+                float sum = 0.0f;
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        p[sub][2 * i + e] = exp2_fast(x[sub][nb][2 * i + e] - ms);
+                        sum = C::Q8 ? fmaf(p[sub][2 * i + e], iv[sub][i], sum) : sum + p[sub][2 * i + e];
+                    }
+                l[nb][e] = fmaf(l[nb][e], shrink[nb][e], sum);
                 moved |= shrink[nb][e] != 1.0f;
             }
-            bp[nb][0] = transpose8x8(Pair<M>::pack(p[0], p[1]));
-            bp[nb][1] = transpose8x8(Pair<M>::pack(p[2], p[3]));
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) {
+                bp[sub][nb][0] = transpose8x8(Pair<M>::pack(p[sub][0], p[sub][1]));
+                bp[sub][nb][1] = transpose8x8(Pair<M>::pack(p[sub][2], p[sub][3]));
+            }
         }
         if (__any_sync(FULL, moved)) {
 #pragma unroll
@@ -353,72 +493,69 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[i][nb][j] *= shrink[nb][j & 1];
         }
-        // O^T += V^T P^T: this lane's rows of V are tokens 2 * t4 + {0, 1, 8, 9}
-        if (!C::Q8) {
+        // O^T += V^T P^T: this lane's rows of V are tokens 2 * t4 + {0, 1, 8, 9} of 16
 #pragma unroll
-            for (int half = 0; half < D / 64; ++half) {
-                uint4 v[4];
+        for (int sub = 0; sub < SUB; ++sub) {
+            const uint32_t va = vd + sub * 16 * C::ROW_BYTES;
+            if (!C::Q8) {
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 2 * t4 + (i & 1) + (i >> 1) * 8;
+                        v[i] = lds<uint4>(va + r * C::ROW_BYTES + ((g ^ swizzle<C::CHUNKS>(r)) + half * 8) * 16);
+                    }
+                    const uint32_t vw[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
+                                               {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t av[4] = {__byte_perm(vw[0][i], vw[1][i], 0x5410), __byte_perm(vw[0][i], vw[1][i], 0x7632),
+                                                __byte_perm(vw[2][i], vw[3][i], 0x5410), __byte_perm(vw[2][i], vw[3][i], 0x7632)};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[half * 4 + i][nb], av, bp[sub][nb][0], bp[sub][nb][1]);
+                    }
+                }
+            } else {
+                constexpr int WORDS = D / 32;  // 32-bit words of a lane's codes per V row
+                uint32_t vw[4][WORDS];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = 2 * t4 + (i & 1) + (i >> 1) * 8;
-                    v[i] = lds128(vd + r * C::ROW_BYTES + ((g ^ swizzle<C::CHUNKS>(r)) + half * 8) * 16);
+                    const int sw = swizzle<C::CHUNKS>(r);
+                    if (D == 128) {
+                        const uint4 v = lds<uint4>(va + r * C::ROW_BYTES + (g ^ sw) * 16);
+                        vw[i][0] = v.x; vw[i][1] = v.y; vw[i][WORDS - 2] = v.z; vw[i][WORDS - 1] = v.w;
+                    } else {
+                        const uint2 v = lds<uint2>(va + r * C::ROW_BYTES + ((g >> 1) ^ sw) * 16 + (g & 1) * 8);
+                        vw[i][0] = v.x; vw[i][1] = v.y;
+                    }
                 }
-                const uint32_t vw[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
-                                           {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t av[4] = {__byte_perm(vw[0][i], vw[1][i], 0x5410), __byte_perm(vw[0][i], vw[1][i], 0x7632),
-                                            __byte_perm(vw[2][i], vw[3][i], 0x5410), __byte_perm(vw[2][i], vw[3][i], 0x7632)};
+                for (int i = 0; i < WORDS; ++i)
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[half * 4 + i][nb], av, bp[nb][0], bp[nb][1]);
-                }
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t x0 = __byte_perm(vw[0][i], vw[1][i], k ? 0x7362 : 0x5140);
+                        const uint32_t x1 = __byte_perm(vw[2][i], vw[3][i], k ? 0x7362 : 0x5140);
+                        const uint2 h0 = codes_to_half4<FMT>(x0), h1 = codes_to_half4<FMT>(x1);
+                        const uint32_t av[4] = {h0.x, h0.y, h1.x, h1.y};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[2 * i + k][nb], av, bp[sub][nb][0], bp[sub][nb][1]);
+                    }
             }
-        } else {
-            constexpr int WORDS = D / 32;      // 32-bit words of a lane's codes per V row
-            uint32_t vw[4][WORDS];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 2 * t4 + (i & 1) + (i >> 1) * 8;
-                const int sw = swizzle<C::CHUNKS>(r);
-                if (D == 128) {
-                    const uint4 v = lds128(vd + r * C::ROW_BYTES + (g ^ sw) * 16);
-                    vw[i][0] = v.x; vw[i][1] = v.y; vw[i][WORDS - 2] = v.z; vw[i][WORDS - 1] = v.w;
-                } else {
-                    const uint2 v = lds64(vd + r * C::ROW_BYTES + ((g >> 1) ^ sw) * 16 + (g & 1) * 8);
-                    vw[i][0] = v.x; vw[i][1] = v.y;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t x0 = __byte_perm(vw[0][i], vw[1][i], k ? 0x7362 : 0x5140);
-                    const uint32_t x1 = __byte_perm(vw[2][i], vw[3][i], k ? 0x7362 : 0x5140);
-                    const uint32_t av[4] = {codes_to_half2<FMT>(x0), codes_to_half2<FMT>(x0 >> 16), codes_to_half2<FMT>(x1), codes_to_half2<FMT>(x1 >> 16)};
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma16816<M>(o[2 * i + k][nb], av, bp[nb][0], bp[nb][1]);
-                }
-        }
-        const bool tile_done = cons.step == cons.t.steps - 1;
-        if (tile_done || unit + 1 == hi) {
-            finish(unit);
-            if (unit + 1 < hi) {
-                list.next(cons);
-                seg_first = 0;
-                begin();
-            }
-        } else {
-            ++cons.step;
         }
     }
-    if (!open_end && lane == 0) meta[w].last = -1;
+        __syncwarp();                          // every lane has read the stage that finish() may use
+        finish(first == 0, end == cons.t.steps, lo + cons.at + TILE_STEPS + cons.t.steps);
+    }
+    if (!open_end && threadIdx.x == 0) meta[w].last = -1;
     cp_async_wait<0>();
 }
 
 template <typename T, int FMT, int D, int NB>
 cudaError_t run(const AttnView& a, int max_rows, Partial* meta, RowState* state, float* part, cudaStream_t st) {
     using C = Cfg<T, FMT, D, NB>;
-    static_assert(C::CTAS * C::ROWS <= ATTN_ROWS_PER_SM / WARPS, "workspace");
+    static_assert(C::CTAS <= ATTN_WORKERS_PER_SM && C::CTAS * C::ROWS <= ATTN_ROWS_PER_SM && C::STAGES >= 2, "");
     const void* f = reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D, NB>);
     cudaError_t e = allow_max_dynamic_smem(f);
     if (e != cudaSuccess) return e;
@@ -427,7 +564,7 @@ cudaError_t run(const AttnView& a, int max_rows, Partial* meta, RowState* state,
     k_attn_rows<T, FMT, D, NB><<<ctas, WARPS * 32, C::SMEM, st>>>(a, max_rows, meta, state, part);
     launch_hook("k_attn_rows", 1, st);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, C::ROWS, ctas * WARPS, meta,
+    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, C::ROWS, ctas, meta,
                                state, part, st);
 }
 

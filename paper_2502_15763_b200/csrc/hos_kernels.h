@@ -96,7 +96,7 @@ cudaError_t launch_kv_append(const KvView& c, int type, int format, const void* 
                              const long long (&strides)[4], cudaStream_t st);
 cudaError_t launch_kv_read(const KvView& c, int type, int format, void* k, void* v, cudaStream_t st);
 // Work shares of the attention kernels: their number, and the rows that their pieces hold on one SM.
-constexpr int ATTN_SMS = 148, ATTN_WORKERS_PER_SM = 16, ATTN_ROWS_PER_SM = 256;
+constexpr int ATTN_SMS = 148, ATTN_WORKERS_PER_SM = 3, ATTN_ROWS_PER_SM = 256;
 cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, Partial* meta, RowState* state,
                              float* part, cudaStream_t st);
 cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state,

@@ -75,16 +75,18 @@ template <> struct Pair<__nv_bfloat16> {
     }
 };
 
-// Two 8-bit codes in the low half of x -> fp16 pair (exact for both formats).
-template <int FMT> __device__ __forceinline__ uint32_t codes_to_half2(uint32_t x) {
-    uint32_t r;
+// Four 8-bit codes -> two fp16 pairs (exact for both formats).
+template <int FMT> __device__ __forceinline__ uint2 codes_to_half4(uint32_t x) {
+    uint2 r;
     if (FMT == HOS_KV_E4M3) {
-        asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l; }" : "=r"(r) : "r"(x));
+        asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(r.x), "=r"(r.y) : "r"(x));
     } else {
         // 1024 + (code + 128) in fp16 is 0x6400 | (code ^ 0x80); subtracting 1152 is exact
-        const uint32_t u = __byte_perm(x ^ 0x8080u, 0x64646464u, 0x4140);
-        const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
-        r = *reinterpret_cast<const uint32_t*>(&h);
+        const uint32_t u = x ^ 0x80808080u;
+        const uint32_t lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 off = __half2half2(__ushort_as_half(0x6480));
+        const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&lo), off), b = __hsub2(*reinterpret_cast<const __half2*>(&hi), off);
+        r = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
     }
     return r;
 }
@@ -96,23 +98,13 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ float lds32f(uint32_t a) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
-    return v;
-}
+// Loads by shared-memory address, as ordinary memory reads (the compiler may move them between barriers).
+template <typename V> __device__ __forceinline__ V lds(uint32_t a) { return *static_cast<const V*>(__cvta_shared_to_generic(a)); }
 
 // exp2 with results below 2^-126 flushed; exp2(-inf) = 0.  Relative error about 2^-22.
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -124,12 +116,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // c[16][8] += a[16][16] b[16][8], 32-bit sums.
 template <typename T> __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -158,7 +150,10 @@ struct AttnView {
 struct Partial {                              // per worker, what slot 1 holds
     int32_t seq, head, tile, last;            // last: the worker in whose range the tile ends; -1: slot unused
 };
-struct RowState { float m, l, mt, pad; };     // of one row: maximum, normaliser, the exponent o is relative to (all in log2)
+struct RowState { float m, l; };              // of one row: what its exponents (base 2) are relative to, and the sum of its weights
+
+// The smallest V scale that the attention kernels tell from zero (a vector of values below 1e-21).
+constexpr float LEAST_V_SCALE = 8.2718061e-25f;                       // 2^-80
 
 // Calls f(type tag, format tag, head_dim tag) for the run-time combination.
 template <typename T> struct TypeTag { using type = T; };

@@ -104,10 +104,11 @@ __device__ __forceinline__ Vec16 dequantise16(const uint4& c, float scale) {
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
     Vec16 v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t h = codes_to_half2<FMT>(w[i >> 1] >> (16 * (i & 1)));
-        const float2 f = Pair<__half>::unpack(h);
-        v.w[i] = Pair<T>::pack(__fmul_rn(f.x, scale), __fmul_rn(f.y, scale));
+    for (int i = 0; i < 4; ++i) {
+        const uint2 h = codes_to_half4<FMT>(w[i]);
+        const float2 f = Pair<__half>::unpack(h.x), g = Pair<__half>::unpack(h.y);
+        v.w[2 * i] = Pair<T>::pack(__fmul_rn(f.x, scale), __fmul_rn(f.y, scale));
+        v.w[2 * i + 1] = Pair<T>::pack(__fmul_rn(g.x, scale), __fmul_rn(g.y, scale));
     }
     return v;
 }
