@@ -41,13 +41,16 @@ template <typename T, int FMT, int D> struct Cfg {
     static constexpr int THREADS = Q8 ? 512 : 384;
     static constexpr int TILE_BYTES = STEP * D * 2;            // K or V of a step, 16-bit
     static constexpr int Q_BYTES = HALF * D * 2;               // one half's queries
-    static constexpr int STAGES = D == 128 ? (Q8 ? 4 : 5) : 8;
+    static constexpr int STAGES = D == 128 ? 4 : 8;
+    static constexpr int OUT_PIECE = Q8 ? 64 : 128;            // bytes of a row that a warp writes at once
+    static constexpr int OUT_BYTES = 8 * 32 * OUT_PIECE;
     static constexpr int SCALE_BUFS = STAGES / 2 + 1;
     static constexpr int SCALES = Q8 ? SCALE_BUFS * 3 * STEP * 4 : 0;
     static constexpr bool Q_RANGE = Q8 && !std::is_same<T, __half>::value;   // bf16 queries become fp16
     static constexpr int Q_SCALES = Q_RANGE ? 2 * ROWS * 4 : 0;
     static constexpr int HEAD = 1024;                          // barriers, the cursor, the tensor memory address
-    static constexpr int SMEM = 1024 /*alignment*/ + HEAD + 2 * Q_BYTES + STAGES * TILE_BYTES + SCALES + Q_SCALES;
+    static constexpr int SMEM = 1024 /*alignment*/ + HEAD + 2 * Q_BYTES + STAGES * TILE_BYTES + OUT_BYTES + SCALES + Q_SCALES;
+    static_assert(SMEM <= (int)SMEM_LIMIT, "");
 };
 template <typename T, int FMT> struct MatType { using type = __half; };
 template <typename T> struct MatType<T, HOS_KV_SAME> { using type = T; };
@@ -204,7 +207,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     Shared& sh = *reinterpret_cast<Shared*>(base);
     volatile int* gave_up = &sh.gave_up;
     const uint32_t q_smem = smem_u32(base) + C::HEAD, ring = q_smem + 2 * C::Q_BYTES;
-    const uint32_t scales = ring + C::STAGES * C::TILE_BYTES;          // [buffer][scale log2(e) ks | log2 vs | 1 / vs][token]
+    const uint32_t out_buf = ring + C::STAGES * C::TILE_BYTES, scales = out_buf + C::OUT_BYTES;          // [buffer][scale log2(e) ks | log2 vs | 1 / vs][token]
     const uint32_t q_scales = scales + C::SCALES;                      // [tile parity][row]: what a row of queries was divided by
     const uint32_t bar0 = smem_u32(sh.bars);
     auto kv_full = [&](uint32_t i) { return bar0 + 8 * i; };
@@ -307,7 +310,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             }
             const int r = cur.tile * ROWS + h * HALF + row;
             const bool there = h * HALF + row < cur.t.rows;
-            const int tok = r / a.group, hd = cur.head * a.group + r - tok * a.group;
+            const int tok = by_group(a, r), hd = cur.head * a.group + r - tok * a.group;
             const int pos = cur.q.len - cur.q.n + tok;
             // rows past the tile see everything: no masking, and they are not written
             const int see_hi = !there ? 0x7FFFFFFF : a.causal ? min(cur.q.len, pos + 1) : cur.q.len;
@@ -349,10 +352,17 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     }
                 }
                 if (__any_sync(FULL, j0 < see_lo || j0 + STEP > see_hi)) {
-                    const int first = see_lo - j0, end = see_hi - j0;
+                    // only the 32 columns that some row's limits fall into are looked at one by one
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (i < first || i >= end) x[i] = -INFINITY;
+                    for (int q = 0; q < 4; ++q) {
+                        const int first = see_lo - j0 - 32 * q, end = see_hi - j0 - 32 * q;
+                        if (!__any_sync(FULL, first > 0 || end < 32)) continue;
+                        const uint32_t below = end >= 32 ? FULL : (1u << max(end, 0)) - 1u;
+                        const uint32_t keep = below & (first <= 0 ? FULL : first >= 32 ? 0u : FULL << first);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(keep & (1u << i))) x[32 * q + i] = -INFINITY;
+                    }
                 }
                 float tops[4];
 #pragma unroll
@@ -435,29 +445,45 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             tc_fence_after();
             const bool whole = seg.starts && seg.ends;
             const int slot = 2 * w + (seg.starts ? 1 : 0);
-            const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-            T* dst = reinterpret_cast<T*>(a.out) + (long long)(cur.q.off + tok) * a.o_tok + (long long)hd * a.o_head;
+            const float by = l == 0.0f ? 0.0f : 1.0f / l;
             const long long prow = (long long)slot * ROWS + h * HALF + row;
+            unsigned char* dst = whole ? a.out + 2 * ((long long)(cur.q.off + tok) * a.o_tok + (long long)hd * a.o_head)
+                                       : reinterpret_cast<unsigned char*>(part + prow * D);
+            // A lane has a row; through shared memory eight (four) lanes write PIECE bytes of a row together.
+            constexpr int PIECE = C::OUT_PIECE, CHUNKS = PIECE / 16;
+            const uint32_t buf_at = out_buf + warp * 32 * PIECE;
+            auto place = [&](int r, int ch) { return buf_at + r * PIECE + (ch ^ (CHUNKS == 8 ? r & 7 : (r >> 1) & 3)) * 16; };
+            auto write_out = [&](int at, const uint32_t* v) {           // PIECE bytes of every row from byte `at` on
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                uint32_t o[32];
-                tmem_load32(o_tm + 32 * i, o);
-                tmem_wait_load();
-                if (!there) continue;
-                if (whole) {
+                for (int ch = 0; ch < CHUNKS; ++ch) st_shared16(place(lane, ch), make_uint4(v[4 * ch], v[4 * ch + 1], v[4 * ch + 2], v[4 * ch + 3]));
+                __syncwarp();
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint4 v;
-                        uint32_t* vw = &v.x;
+                for (int i = 0; i < CHUNKS; ++i) {
+                    const int r = i * (32 / CHUNKS) + lane / CHUNKS, ch = lane % CHUNKS;
+                    unsigned char* to = reinterpret_cast<unsigned char*>(__shfl_sync(FULL, reinterpret_cast<unsigned long long>(there ? dst : nullptr), r));
+                    const uint4 x4 = lds<uint4>(place(r, ch));
+                    if (to) *reinterpret_cast<uint4*>(to + at + ch * 16) = x4;
+                }
+                __syncwarp();
+            };
+            if (whole) {
+#pragma unroll 1
+                for (int i = 0; i < D / (PIECE / 2); ++i) {             // PIECE / 2 columns become PIECE bytes
+                    uint32_t o[PIECE / 2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            vw[e] = Pair<T>::pack(__uint_as_float(o[8 * k + 2 * e]) * by, __uint_as_float(o[8 * k + 2 * e + 1]) * by);
-                        *reinterpret_cast<uint4*>(dst + 32 * i + 8 * k) = v;
-                    }
-                } else {
+                    for (int k = 0; k < PIECE / 64; ++k) tmem_load32(o_tm + i * (PIECE / 2) + 32 * k, o + 32 * k);
+                    tmem_wait_load();
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        *reinterpret_cast<uint4*>(part + prow * D + 32 * i + 4 * k) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    for (int k = 0; k < PIECE / 4; ++k) o[k] = Pair<T>::pack(__uint_as_float(o[2 * k]) * by, __uint_as_float(o[2 * k + 1]) * by);
+                    write_out(i * PIECE, o);
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < D / (PIECE / 4); ++i) {
+                    uint32_t o[PIECE / 4];
+                    if (PIECE == 128) tmem_load32(o_tm + i * 32, o); else tmem_load16(o_tm + i * 16, o);
+                    tmem_wait_load();
+                    write_out(i * PIECE, o);
                 }
             }
             if (there) {
@@ -613,7 +639,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         for (int half = 0; half < D / 64; ++half)
                             asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                                          :: "r"(dst + half * BLOCK_BYTES), "l"(&q_map), "r"(half * 64), "r"(cur.head * a.group),
-                                            "r"(cur.q.off + (cur.tile * ROWS + h * HALF) / a.group), "r"(q_full(h)) : "memory");
+                                            "r"(cur.q.off + by_group(a, cur.tile * ROWS + h * HALF)), "r"(q_full(h)) : "memory");
                     }
                     __syncwarp();
                     last = phase;
@@ -623,7 +649,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 #pragma unroll 1
                 for (int r0 = 0; r0 < HALF; r0 += 32) {
                   // lane l knows where row r0 + l is
-                  const int pr = cur.tile * ROWS + h * HALF + r0 + lane, tok = pr / a.group, hd = cur.head * a.group + pr - tok * a.group;
+                  const int pr = cur.tile * ROWS + h * HALF + r0 + lane, tok = by_group(a, pr), hd = cur.head * a.group + pr - tok * a.group;
                   const long long where = h * HALF + r0 + lane < cur.t.rows ? (long long)(cur.q.off + tok) * a.q_tok + (long long)hd * a.q_head : -1;
 #pragma unroll 1
                   for (int i0 = 0; i0 < CH; i0 += BATCH) {

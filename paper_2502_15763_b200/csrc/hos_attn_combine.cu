@@ -31,11 +31,11 @@ __global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_consta
             const int seq = __shfl_sync(FULL, mine.seq, src), head = __shfl_sync(FULL, mine.head, src);
             const int tile = __shfl_sync(FULL, mine.tile, src), n = __shfl_sync(FULL, mine.last, src) - w + 1;
             const SeqInfo q = load_seq(a.kv, seq, false);
-            const int first = blockIdx.y * 16, rows = min(min(ROWS, q.n * a.group - tile * ROWS) - first, 16);
+            const int rows = min(ROWS, q.n * a.group - tile * ROWS);
             const int shares = rows > 8 ? 1 : rows > 4 ? 2 : rows > 2 ? 4 : rows == 2 ? 8 : 16;   // warps a row
             const int row = warp / shares, share = warp % shares;
             const bool busy = row < rows;
-            auto slot = [&](int i) { return (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * ROWS + first + row; };
+            auto slot = [&](int i) { return (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * ROWS + row; };
             float m = -INFINITY, l = 0.0f;
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (busy) {
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_consta
                 l = 0.0f;
                 for (int k = 0; k < shares; ++k) l += sum_l[warp + k];
                 const float by = l == 0.0f ? 0.0f : 1.0f / l;
-                const int r = tile * ROWS + first + row, tok = q.off + r / a.group, hd = head * a.group + r % a.group;
+                const int r = tile * ROWS + row, i = by_group(a, r), tok = q.off + i, hd = head * a.group + r - i * a.group;
                 if (lane < LANES) {
                     o = sum_o[warp][lane];
                     for (int k = 1; k < shares; ++k) {
@@ -83,19 +83,88 @@ __global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_consta
     }
 }
 
+// The same for the chunk kernel's tiles of 256 rows, whose pieces are few: a warp takes four rows, whose loads do not wait for one
+// another, and goes through the pieces with a running maximum.
+constexpr int BIG_ROWS = 256, BIG_WARPS = 8, BIG_SPAN = 4 * BIG_WARPS;
+template <typename T, int D>
+__global__ void __launch_bounds__(BIG_WARPS * 32) k_attn_combine_tiles(const __grid_constant__ AttnView a, const Partial* __restrict__ meta,
+                                                                      const RowState* __restrict__ state, const float* __restrict__ part) {
+    constexpr int PER = D / 32;                // elements a lane
+    const int lane = lane_id(), w = blockIdx.x;
+    pdl_wait();
+    const Partial p = meta[w];
+    if (p.last < 0) return;
+    const SeqInfo q = load_seq(a.kv, p.seq, false);
+    const int rows = min(BIG_ROWS, q.n * a.group - p.tile * BIG_ROWS), r0 = blockIdx.y * BIG_SPAN + warp_id() * 4;
+    if (r0 >= rows) return;
+    float m[4], l[4], o[4][PER];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        m[k] = -INFINITY;
+        l[k] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[k][e] = 0.0f;
+    }
+    const int n = p.last - w + 1;
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+        // rows past the tile's end have room in the workspace, too; what they hold is not used
+        const long long at = (long long)(i == 0 ? 2 * w + 1 : 2 * (w + i)) * BIG_ROWS + r0;
+        RowState st[4];
+        float v[4][PER];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            st[k] = state[at + k];
+            const float* src = part + (at + k) * D + lane * PER;
+            if (PER == 4) {
+                const float4 f = *reinterpret_cast<const float4*>(src);
+                v[k][0] = f.x; v[k][1] = f.y; v[k][PER - 2] = f.z; v[k][PER - 1] = f.w;
+            } else {
+                const float2 f = *reinterpret_cast<const float2*>(src);
+                v[k][0] = f.x; v[k][1] = f.y;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float mn = fmaxf(m[k], st[k].m), ms = mn == -INFINITY ? 0.0f : mn;
+            const float old = exp2f(m[k] - ms), by = exp2f(st[k].m - ms);
+            m[k] = mn;
+            l[k] = l[k] * old + st[k].l * by;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) o[k][e] = o[k][e] * old + v[k][e] * by;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (r0 + k >= rows) break;
+        const float by = l[k] == 0.0f ? 0.0f : 1.0f / l[k];
+        const int r = p.tile * BIG_ROWS + r0 + k, i = by_group(a, r), tok = q.off + i, hd = p.head * a.group + r - i * a.group;
+        T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head + lane * PER;
+        if (PER == 4)
+            *reinterpret_cast<uint2*>(dst) = make_uint2(Pair<T>::pack(o[k][0] * by, o[k][1] * by), Pair<T>::pack(o[k][PER - 2] * by, o[k][PER - 1] * by));
+        else
+            *reinterpret_cast<uint32_t*>(dst) = Pair<T>::pack(o[k][0] * by, o[k][1] * by);
+        if (a.lse && lane == 0)
+            a.lse[(long long)tok * a.n_heads + hd] = l[k] == 0.0f ? -INFINITY : (m[k] + log2f(l[k])) * 0.69314718055994530942f;
+    }
+}
+
 template <typename T, int D, int ROWS>
 cudaError_t run(const AttnView& a, int workers, const Partial* meta, const RowState* state, const float* part, cudaStream_t st) {
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(workers < BLOCKS ? workers : BLOCKS), (ROWS + 15) / 16);
-    cfg.blockDim = dim3(WARPS * 32);
+    constexpr bool BIG = ROWS == BIG_ROWS;
+    cfg.gridDim = BIG ? dim3((unsigned)workers, BIG_ROWS / BIG_SPAN) : dim3((unsigned)(workers < BLOCKS ? workers : BLOCKS));
+    cfg.blockDim = dim3((BIG ? BIG_WARPS : WARPS) * 32);
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     launch_hook("k_attn_combine", 0, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D, ROWS>, a, meta, workers, state, part);
+    cudaError_t e;
+    if constexpr (BIG) e = cudaLaunchKernelEx(&cfg, k_attn_combine_tiles<T, D>, a, meta, state, part);
+    else e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D, ROWS>, a, meta, workers, state, part);
     launch_hook("k_attn_combine", 1, st);
     return e;
 }

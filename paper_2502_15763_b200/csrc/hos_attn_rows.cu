@@ -194,8 +194,8 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
 
     auto begin = [&]() {
         {
-            const int first = cons.q.len - cons.q.n + cons.tile * ROWS / a.group;
-            const int last = cons.q.len - cons.q.n + (cons.tile * ROWS + cons.t.rows - 1) / a.group;
+            const int first = cons.q.len - cons.q.n + by_group(a, cons.tile * ROWS);
+            const int last = cons.q.len - cons.q.n + by_group(a, cons.tile * ROWS + cons.t.rows - 1);
             all_hi = a.causal ? min(cons.q.len, first + 1) : cons.q.len;
             all_lo = a.window > 0 ? max(0, last - a.window + 1) : 0;
         }
@@ -209,7 +209,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
         for (int nb = 0; nb < NB; ++nb) {
             const int r = cons.tile * ROWS + nb * 8 + g;
             const bool there = nb * 8 + g < cons.t.rows;
-            const int i = r / a.group, hd = cons.head * a.group + r % a.group;
+            const int i = by_group(a, r), hd = cons.head * a.group + r - i * a.group;
             const T* src = reinterpret_cast<const T*>(a.q) + (long long)(cons.q.off + i) * a.q_tok + (long long)hd * a.q_head;
             uint32_t x[2 * KS];
 #pragma unroll
@@ -248,7 +248,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r2 = cons.tile * ROWS + nb * 8 + 2 * t4 + e;
-                const int pos = cons.q.len - cons.q.n + r2 / a.group;
+                const int pos = cons.q.len - cons.q.n + by_group(a, r2);
                 // columns past the tile see everything that its rows do; they are not written
                 const bool real = nb * 8 + 2 * t4 + e < cons.t.rows;
                 see_hi[nb][e] = real && a.causal ? min(cons.q.len, pos + 1) : cons.q.len;
@@ -355,12 +355,12 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
                 const int d0 = dim_of(warp * OWN);
                 if (whole) {
                     const int r = cons.tile * ROWS + in_tile;
-                    const int tok = cons.q.off + r / a.group, hd = cons.head * a.group + r % a.group;
+                    const int i = by_group(a, r), tok = cons.q.off + i, hd = cons.head * a.group + r - i * a.group;
                     const float inv = norm[nb][e] == 0.0f ? 0.0f : 1.0f / norm[nb][e];
                     T* dst = reinterpret_cast<T*>(a.out) + (long long)tok * a.o_tok + (long long)hd * a.o_head + d0;
                     uint32_t v[OWN];
 #pragma unroll
-                    for (int i = 0; i < OWN; ++i) v[i] = Pair<T>::pack(own[i][nb][e] * inv, own[i][nb][2 + e] * inv);
+                    for (int k = 0; k < OWN; ++k) v[k] = Pair<T>::pack(own[k][nb][e] * inv, own[k][nb][2 + e] * inv);
                     if (OWN == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(v[0], v[OWN - 1]);
                     else *reinterpret_cast<uint32_t*>(dst) = v[0];
                     if (a.lse && g == 0 && warp == 0)

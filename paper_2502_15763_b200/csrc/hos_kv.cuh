@@ -140,9 +140,17 @@ struct AttnView {
     long long o_tok, o_head;
     float* lse;
     int n_heads, group;
+    uint32_t group_magic, group_shift;        // for by_group
     float scale_log2;                         // sm_scale * log2(e)
     int causal, window;
 };
+
+// n / group for 0 <= n < 2^31: with 2^shift the smallest power of two >= group and magic = floor(2^32 (2^shift - group) / group) + 1
+// the quotient is (n + floor(n magic / 2^32)) >> shift (Granlund, Montgomery, "Division by invariant integers using
+// multiplication", 1994).
+__device__ __forceinline__ int by_group(const AttnView& a, int n) {
+    return (int)(((uint32_t)n + __umulhi((uint32_t)n, a.group_magic)) >> a.group_shift);
+}
 
 // Workspace of an attention call.  A worker (warp or CTA) owns a contiguous range of the call's work
 // units; a tile that crosses the range's ends is left as a partial result: slot 0 if the tile began in an

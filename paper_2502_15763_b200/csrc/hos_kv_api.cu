@@ -143,6 +143,9 @@ int hos_paged_attention(const hos_kv_cache* c, const hos_kv_batch* b, const void
     a.lse = lse;
     a.n_heads = n_heads;
     a.group = n_heads / c->n_kv_heads;
+    a.group_shift = 0;
+    while ((1ll << a.group_shift) < a.group) ++a.group_shift;
+    a.group_magic = (uint32_t)((((1ull << a.group_shift) - a.group) << 32) / a.group + 1);
     a.scale_log2 = sm_scale * 1.44269504088896340736f;
     a.causal = causal != 0;
     a.window = window;
