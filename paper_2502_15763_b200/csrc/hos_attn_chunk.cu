@@ -28,10 +28,11 @@
 namespace hos {
 namespace {
 
-constexpr int ROWS = 256, STEP = 128, HALF = 128;
+constexpr int ROWS = ATTN_CHUNK_ROWS, STEP = 128, HALF = 128;
 constexpr int TILE_STEPS = 2;                 // what a tile's begin and end cost, in steps
 using List = AttnList<ROWS, STEP, TILE_STEPS>;
 using Cursor = List::Cursor;
+constexpr int FIRST_PART = 96;                // of a step's 128 weights a row, those whose product is issued before the rest is known
 constexpr float GROWTH = 8.0f;                // log2 of how far a row's maximum may pass the one its reference was taken from
 // The reference is the maximum - LIFT: fp16 weights start at 2^7 and end below 2^15, so that small ones keep their bits.
 template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 7.0f : 0.0f;
@@ -198,7 +199,8 @@ struct Segment { int blocks; bool starts, ends; };   // steps of the current til
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(Cfg<T, FMT, D>::THREADS, 1)
 k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-             const __grid_constant__ CUtensorMap q_map, const bool q_tma, const int min_rows, Partial* __restrict__ meta, RowState* __restrict__ state, float* __restrict__ part) {
+             const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap o_map, const bool q_tma, const bool o_tma,
+             const int min_rows, Partial* __restrict__ meta, RowState* __restrict__ state, float* __restrict__ part) {
     using C = Cfg<T, FMT, D>;
     using M = typename MatType<T, FMT>::type;
     constexpr bool BF16 = std::is_same<M, __nv_bfloat16>::value;
@@ -226,11 +228,12 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     pdl_launch_dependents();
 
     if (warp == 0) {
-        const long long total = list.total(w == 0);
+        long long mine;
+        const long long total = list.total(w == 0, mine);
         const int active = (int)min((long long)gridDim.x, total);
         const long long lo = w < active ? total * w / active : 0, hi = w < active ? total * (w + 1) / active : 0;
         Cursor c = {};
-        if (hi > lo) c = list.locate(lo);
+        if (hi > lo) c = list.locate(lo, mine);
         if (lane == 0) {
             sh.first = c;
             sh.lo = lo;
@@ -418,8 +421,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         }
                     }
                     tmem_store16(s_tm + 16 * q, p);
-                    if (q == 1) {
-                        // the first half of the weights may be multiplied while the second is worked out
+                    if (q == FIRST_PART / 32 - 1) {
+                        // these may be multiplied while the rest is worked out
                         if (!C::Q8 && h == 0 && (j0 < cur.t.kb || j0 + STEP > cur.t.ke)) {
                             ok = clear_v(j0, 2 * block + 1);
                             if (!ok) break;
@@ -446,44 +449,57 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             const bool whole = seg.starts && seg.ends;
             const int slot = 2 * w + (seg.starts ? 1 : 0);
             const float by = l == 0.0f ? 0.0f : 1.0f / l;
-            const long long prow = (long long)slot * ROWS + h * HALF + row;
-            unsigned char* dst = whole ? a.out + 2 * ((long long)(cur.q.off + tok) * a.o_tok + (long long)hd * a.o_head)
-                                       : reinterpret_cast<unsigned char*>(part + prow * D);
-            // A lane has a row; through shared memory eight (four) lanes write PIECE bytes of a row together.
+            // A lane has a row.  Whole tiles: PIECE bytes of each of the warp's 32 rows at a time go through shared memory, from where
+            // they leave by TMA, or, where the rows are not all there or not a box of the output, eight (four) lanes to a row.
             constexpr int PIECE = C::OUT_PIECE, CHUNKS = PIECE / 16;
             const uint32_t buf_at = out_buf + warp * 32 * PIECE;
             auto place = [&](int r, int ch) { return buf_at + r * PIECE + (ch ^ (CHUNKS == 8 ? r & 7 : (r >> 1) & 3)) * 16; };
-            auto write_out = [&](int at, const uint32_t* v) {           // PIECE bytes of every row from byte `at` on
-#pragma unroll
-                for (int ch = 0; ch < CHUNKS; ++ch) st_shared16(place(lane, ch), make_uint4(v[4 * ch], v[4 * ch + 1], v[4 * ch + 2], v[4 * ch + 3]));
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) {
-                    const int r = i * (32 / CHUNKS) + lane / CHUNKS, ch = lane % CHUNKS;
-                    unsigned char* to = reinterpret_cast<unsigned char*>(__shfl_sync(FULL, reinterpret_cast<unsigned long long>(there ? dst : nullptr), r));
-                    const uint4 x4 = lds<uint4>(place(r, ch));
-                    if (to) *reinterpret_cast<uint4*>(to + at + ch * 16) = x4;
-                }
-                __syncwarp();
-            };
             if (whole) {
+                const bool by_tma = o_tma && __all_sync(FULL, there);
+                unsigned char* dst = a.out + 2 * ((long long)(cur.q.off + tok) * a.o_tok + (long long)hd * a.o_head);
 #pragma unroll 1
                 for (int i = 0; i < D / (PIECE / 2); ++i) {             // PIECE / 2 columns become PIECE bytes
                     uint32_t o[PIECE / 2];
 #pragma unroll
                     for (int k = 0; k < PIECE / 64; ++k) tmem_load32(o_tm + i * (PIECE / 2) + 32 * k, o + 32 * k);
                     tmem_wait_load();
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the buffer has been read
+                    __syncwarp();
 #pragma unroll
                     for (int k = 0; k < PIECE / 4; ++k) o[k] = Pair<T>::pack(__uint_as_float(o[2 * k]) * by, __uint_as_float(o[2 * k + 1]) * by);
-                    write_out(i * PIECE, o);
+#pragma unroll
+                    for (int ch = 0; ch < CHUNKS; ++ch) st_shared16(place(lane, ch), make_uint4(o[4 * ch], o[4 * ch + 1], o[4 * ch + 2], o[4 * ch + 3]));
+                    if (by_tma) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                                         :: "l"(&o_map), "r"(i * (PIECE / 2)), "r"(hd), "r"(cur.q.off + tok), "r"(buf_at) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    } else {
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < CHUNKS; ++k) {
+                            const int r2 = k * (32 / CHUNKS) + lane / CHUNKS, ch = lane % CHUNKS;
+                            unsigned char* to = reinterpret_cast<unsigned char*>(__shfl_sync(FULL, reinterpret_cast<unsigned long long>(there ? dst : nullptr), r2));
+                            const uint4 x4 = lds<uint4>(place(r2, ch));
+                            if (to) *reinterpret_cast<uint4*>(to + i * PIECE + ch * 16) = x4;
+                        }
+                        __syncwarp();
+                    }
                 }
             } else {
+                // a piece: four columns of every row together, so that the lanes' 16 bytes lie next to each other
+                float* dst = part + (long long)slot * ROWS * D + (h * HALF + row) * 4;
 #pragma unroll 1
-                for (int i = 0; i < D / (PIECE / 4); ++i) {
-                    uint32_t o[PIECE / 4];
-                    if (PIECE == 128) tmem_load32(o_tm + i * 32, o); else tmem_load16(o_tm + i * 16, o);
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32];
+                    tmem_load32(o_tm + i * 32, o);
                     tmem_wait_load();
-                    write_out(i * PIECE, o);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *reinterpret_cast<uint4*>(dst + (long long)(i * 8 + k) * (ROWS * 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                 }
             }
             if (there) {
@@ -492,7 +508,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         a.lse[(long long)(cur.q.off + tok) * a.n_heads + hd] =
                             l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
                 } else {
-                    state[prow] = RowState{m, l};
+                    state[(long long)slot * ROWS + h * HALF + row] = RowState{m, l};
                 }
             }
             if (!whole && seg.starts && h == 0 && row == 0) {
@@ -501,6 +517,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             }
             tc_fence_before();
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
     } else {
         if (C::Q8) {
@@ -563,7 +580,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             auto product_pv = [&](int h, int stage, bool add, int part_of) {
                 const uint64_t vb = smem_desc(ring + stage * C::TILE_BYTES, BLOCK_BYTES);
 #pragma unroll
-                for (int k = part_of * (STEP / 32); k < (part_of + 1) * (STEP / 32); ++k)
+                for (int k = part_of ? FIRST_PART / 16 : 0; k < (part_of ? STEP : FIRST_PART) / 16; ++k)
                     mma_ts(tmem + 256 + h * D, tmem + h * 128 + 8 * k, vb + (uint64_t)((k * 16 * 128) >> 4), PV, add || k > 0);
             };
             for (; more && ok; more = list.next(cur, share)) {
@@ -588,7 +605,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     if (ok && more) ok = bar_wait(kv_full(ki % C::STAGES), (ki / C::STAGES) & 1, gave_up);
                     if (!ok) break;
                     for (int h = 0; h < halves; ++h) {
-                        // the weights come in two halves
+                        // the weights come in two parts
                         ok = bar_wait(p_half(h), p_phase[h], gave_up);
                         if (!ok) break;
                         tc_fence_after();
@@ -804,41 +821,42 @@ bool make_map(CUtensorMap* map, const KvView& c, void* base) {
              CU_TENSOR_MAP_INTERLEAVE_NONE, bytes == 1 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The queries: {head_dim, head, token}, boxes of 128 rows, token by token.
-bool make_q_map(CUtensorMap* map, const AttnView& a) {
+// Rows of queries or outputs: {head_dim, head, token}; a box is `columns` of `rows` consecutive rows of a KV head, token by token.
+// False where these are no box (or the strides are none that a tensor map can hold, such as those of an expanded tensor).
+bool make_rows_map(CUtensorMap* map, const AttnView& a, const unsigned char* base, long long tok, long long head, int columns, int rows) {
     const EncodeTiled f = encoder();
-    if (!f) return false;
+    const int heads = a.group < rows ? a.group : rows;
+    if (!f || rows % heads || a.group % heads || head <= 0 || tok <= 0) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)a.kv.head_dim, (cuuint64_t)a.n_heads, (cuuint64_t)a.kv.n_tokens};
-    const cuuint64_t strides[2] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_tok * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(HALF / a.group)}, one[3] = {1, 1, 1};
-    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<unsigned char*>(a.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t strides[2] = {(cuuint64_t)head * 2, (cuuint64_t)tok * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)columns, (cuuint32_t)heads, (cuuint32_t)(rows / heads)}, one[3] = {1, 1, 1};
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<unsigned char*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int FMT, int D>
-cudaError_t run(const AttnView& a, int min_rows, Partial* meta, RowState* state, float* part, cudaStream_t st) {
+cudaError_t run(const AttnView& a, int min_rows, const AttnWs& ws, cudaStream_t st) {
     using C = Cfg<T, FMT, D>;
     cudaError_t e = allow_max_dynamic_smem(reinterpret_cast<const void*>(&k_attn_chunk<T, FMT, D>));
     if (e != cudaSuccess) return e;
-    CUtensorMap km = {}, vm = {}, qm = {};
-    // Queries come by TMA where 128 rows are whole tokens and nothing has to be done to them on the way; else by two warps.
-    // (Strides that a tensor map cannot hold, such as those of an expanded tensor, go the second way too.)
-    const bool q_tma = !C::Q_RANGE && HALF % a.group == 0 && a.scale_log2 >= 0.0f && a.q_head > 0 && a.q_tok > 0 && make_q_map(&qm, a);
+    CUtensorMap km = {}, vm = {}, qm = {}, om = {};
+    // Queries come by TMA where 128 rows are a box and nothing has to be done to them on the way; else by two warps.  (A tile's 128
+    // rows begin at a whole token where the group divides 128.)
+    const bool q_tma = !C::Q_RANGE && HALF % a.group == 0 && a.scale_log2 >= 0.0f && make_rows_map(&qm, a, a.q, a.q_tok, a.q_head, 64, HALF);
+    const bool o_tma = make_rows_map(&om, a, a.out, a.o_tok, a.o_head, C::OUT_PIECE / 2, 32);
     if (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v)) return cudaErrorInvalidValue;
     launch_hook("k_attn_chunk", 0, st);
-    k_attn_chunk<T, FMT, D><<<ATTN_SMS, C::THREADS, C::SMEM, st>>>(a, km, vm, qm, q_tma, min_rows, meta, state, part);
+    k_attn_chunk<T, FMT, D><<<ATTN_SMS, C::THREADS, C::SMEM, st>>>(a, km, vm, qm, om, q_tma, o_tma, min_rows, ws.meta, ws.state, ws.part);
     launch_hook("k_attn_chunk", 1, st);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, ROWS, ATTN_SMS, meta, state,
-                               part, st);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, Partial* meta, RowState* state, float* part,
-                              cudaStream_t st) {
+cudaError_t launch_attn_chunk(const AttnView& a, int type, int format, int min_rows, const AttnWs& ws, cudaStream_t st) {
     return kv_dispatch(type, format, a.kv.head_dim, [&](auto t, auto f, auto d) {
-        return run<typename decltype(t)::type, decltype(f)::value, decltype(d)::value>(a, min_rows, meta, state, part, st);
+        return run<typename decltype(t)::type, decltype(f)::value, decltype(d)::value>(a, min_rows, ws, st);
     });
 }
 

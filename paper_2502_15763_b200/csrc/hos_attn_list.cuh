@@ -51,13 +51,13 @@ template <int ROWS, int STEP, int START> struct AttnList {
     }
 
     // Length in the list of one KV head of this lane's sequence (called by the whole warp; q.n = 0 for none).  Sequences
-    // of more than two tiles are summed by all lanes together.
+    // of more than 16 tiles are summed by all lanes together.
     __device__ __forceinline__ long long steps_of(const SeqInfo& q) const {
         long long sum = 0;
         const int nt = has(q) ? tiles_of(q) : 0;
-        if (nt > 0 && nt <= 2)
+        if (nt > 0 && nt <= 16)
             for (int t = 0; t < nt; ++t) sum += tile_of(q, t).steps + START;
-        for (unsigned big = __ballot_sync(FULL, nt > 2); big; big &= big - 1) {
+        for (unsigned big = __ballot_sync(FULL, nt > 16); big; big &= big - 1) {
             const int l = __ffs(big) - 1;
             SeqInfo b;
             b.off = 0;
@@ -77,10 +77,12 @@ template <int ROWS, int STEP, int START> struct AttnList {
         return q;
     }
 
-    // Length of the whole list; `flag`: report sequences with bad offsets or lengths.
-    __device__ __forceinline__ long long total(bool flag) const {
-        long long sum = 0;
-        for (int s0 = 0; s0 < a.kv.n_seq; s0 += 32) sum += steps_of(lane_seq(s0 + lane_id(), flag));
+    // Length of the whole list; `flag`: report sequences with bad offsets or lengths; `mine`: this lane's of the first 32
+    // sequences, for locate().
+    __device__ __forceinline__ long long total(bool flag, long long& mine) const {
+        mine = steps_of(lane_seq(lane_id(), flag));
+        long long sum = mine;
+        for (int s0 = 32; s0 < a.kv.n_seq; s0 += 32) sum += steps_of(lane_seq(s0 + lane_id(), flag));
         return (long long)warp_sum_u64((unsigned long long)sum) * a.kv.n_kv;
     }
 
@@ -107,12 +109,12 @@ template <int ROWS, int STEP, int START> struct AttnList {
     }
 
     // Place number `at` (below the total) of the list; called by the whole warp.
-    __device__ __forceinline__ Cursor locate(long long at) const {
+    __device__ __forceinline__ Cursor locate(long long at, long long mine) const {
         Cursor c;
         long long before = 0, per_head = 1;
         c.seq = 0;
         for (int s0 = 0; s0 < a.kv.n_seq; s0 += 32) {
-            const long long steps = steps_of(lane_seq(s0 + lane_id(), false));
+            const long long steps = s0 == 0 ? mine : steps_of(lane_seq(s0 + lane_id(), false));
             const long long scan = warp_scan_i64(steps * a.kv.n_kv);
             const unsigned hit = __ballot_sync(FULL, before + scan > at);
             if (hit) {

@@ -93,15 +93,17 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
 
     // this CTA's share of the list
     const List list{a, 0, max_rows};
-    const long long total = list.total(w == 0 && warp == 0);
+    long long mine;
+    const long long total = list.total(w == 0 && warp == 0, mine);
     const int active = (int)min((long long)gridDim.x, (total + MIN_STEPS - 1) / MIN_STEPS);
     if (w >= active) {
         if (threadIdx.x == 0) meta[w].last = -1;
+        pdl_wait();
         return;
     }
     const long long lo = total * w / active;
     const int share = (int)(total * (w + 1) / active - lo);
-    Cursor cons = list.locate(lo);
+    Cursor cons = list.locate(lo, mine);
     // where the copies are: this warp's steps of a tile, every fourth one, then the next tile
     Cursor prod = cons;
     int prod_end = list.end_of(prod, share);
@@ -550,32 +552,42 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     }
     if (!open_end && threadIdx.x == 0) meta[w].last = -1;
     cp_async_wait<0>();
+    pdl_wait();                                // the chunk kernel, if one was launched before, is done when this one is
 }
 
 template <typename T, int FMT, int D, int NB>
-cudaError_t run(const AttnView& a, int max_rows, Partial* meta, RowState* state, float* part, cudaStream_t st) {
+cudaError_t run(const AttnView& a, int max_rows, bool beside, const AttnWs& ws, int* workers, cudaStream_t st) {
     using C = Cfg<T, FMT, D, NB>;
     static_assert(C::CTAS <= ATTN_WORKERS_PER_SM && C::CTAS * C::ROWS <= ATTN_ROWS_PER_SM && C::STAGES >= 2, "");
-    const void* f = reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D, NB>);
-    cudaError_t e = allow_max_dynamic_smem(f);
+    cudaError_t e = allow_max_dynamic_smem(reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D, NB>));
     if (e != cudaSuccess) return e;
     const int ctas = 148 * C::CTAS;
+    *workers = ctas;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(WARPS * 32);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = beside ? 1 : 0;
     launch_hook("k_attn_rows", 0, st);
-    k_attn_rows<T, FMT, D, NB><<<ctas, WARPS * 32, C::SMEM, st>>>(a, max_rows, meta, state, part);
+    e = cudaLaunchKernelEx(&cfg, k_attn_rows<T, FMT, D, NB>, a, max_rows, ws.meta, ws.state, ws.part);
     launch_hook("k_attn_rows", 1, st);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_attn_combine(a, std::is_same<T, __half>::value ? HOS_TYPE_FP16 : HOS_TYPE_BF16, C::ROWS, ctas, meta,
-                               state, part, st);
+    return e;
 }
 
 }  // namespace
 
-cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, Partial* meta, RowState* state,
-                             float* part, cudaStream_t st) {
+// `beside`: the chunk kernel of the same call was launched just before, and this one may start while that runs.
+cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, bool beside, const AttnWs& ws, int* workers,
+                             cudaStream_t st) {
     return kv_dispatch(type, format, a.kv.head_dim, [&](auto t, auto f, auto d) {
         using T = typename decltype(t)::type;
-        return tile_rows == 8 ? run<T, decltype(f)::value, decltype(d)::value, 1>(a, max_rows, meta, state, part, st)
-                              : run<T, decltype(f)::value, decltype(d)::value, 2>(a, max_rows, meta, state, part, st);
+        return tile_rows == 8 ? run<T, decltype(f)::value, decltype(d)::value, 1>(a, max_rows, beside, ws, workers, st)
+                              : run<T, decltype(f)::value, decltype(d)::value, 2>(a, max_rows, beside, ws, workers, st);
     });
 }
 

@@ -66,24 +66,30 @@ KvView view(const hos_kv_cache* c, const hos_kv_batch* b, int32_t* status) {
 
 inline int cuda_rc(cudaError_t e) { return e == cudaSuccess ? HOS_OK : HOS_E_CUDA; }
 
-struct AttnWs {
-    Partial* meta;
-    RowState* state;
-    float* part;
+struct AttnSpace {
+    AttnWs rows, chunks;
     size_t bytes;
 };
-AttnWs carve_attention(int head_dim, void* ws) {
-    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-    AttnWs w;
+AttnSpace carve_attention(int head_dim, void* ws) {
+    AttnSpace s;
     unsigned char* base = static_cast<unsigned char*>(ws);
-    // the two kernels follow one another on the stream and share the space; a share leaves two pieces at most
-    const size_t n = (size_t)ATTN_SMS * ATTN_WORKERS_PER_SM, rows = 2 * (size_t)ATTN_SMS * ATTN_ROWS_PER_SM;
     size_t off = 0;
-    w.meta = reinterpret_cast<Partial*>(base + off);   off += up(n * sizeof(Partial));
-    w.state = reinterpret_cast<RowState*>(base + off); off += up(rows * sizeof(RowState));
-    w.part = reinterpret_cast<float*>(base + off);     off += up(rows * (size_t)head_dim * 4);
-    w.bytes = off;
-    return w;
+    auto take = [&](size_t bytes) {
+        unsigned char* p = base + off;
+        off += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    auto carve = [&](size_t shares, size_t rows) {       // a share leaves two pieces at most
+        AttnWs w;
+        w.meta = reinterpret_cast<Partial*>(take(shares * sizeof(Partial)));
+        w.state = reinterpret_cast<RowState*>(take(2 * rows * sizeof(RowState)));
+        w.part = reinterpret_cast<float*>(take(2 * rows * (size_t)head_dim * 4));
+        return w;
+    };
+    s.rows = carve((size_t)ATTN_SMS * ATTN_WORKERS_PER_SM, (size_t)ATTN_SMS * ATTN_ROWS_PER_SM);
+    s.chunks = carve(ATTN_SMS, (size_t)ATTN_SMS * ATTN_CHUNK_ROWS);
+    s.bytes = off;
+    return s;
 }
 
 }  // namespace
@@ -130,7 +136,7 @@ int hos_paged_attention(const hos_kv_cache* c, const hos_kv_batch* b, const void
     if (!q || !out || !aligned16(q) || !aligned16(out)) return HOS_E_INVALID;
     for (long long s : {(long long)q_tok_stride, (long long)q_head_stride, (long long)out_tok_stride, (long long)out_head_stride})
         if (!multiple16(s, 2)) return HOS_E_INVALID;
-    const AttnWs w = carve_attention(c->head_dim, ws);
+    const AttnSpace w = carve_attention(c->head_dim, ws);
     if (!ws || ws_bytes < w.bytes || (reinterpret_cast<uintptr_t>(ws) & 255)) return HOS_E_WORKSPACE;
     AttnView a;
     a.kv = view(c, b, status);
@@ -156,9 +162,12 @@ int hos_paged_attention(const hos_kv_cache* c, const hos_kv_batch* b, const void
     const long long most = (long long)b->max_new * a.group;
     const bool chunks = most > 16, alone = b->n_seq == 1;
     const int tile = chunks ? (a.group <= 8 ? 8 : 16) : most <= 8 ? 8 : 16;
-    if (chunks && (rc = cuda_rc(launch_attn_chunk(a, c->type, c->format, alone ? 0 : tile, w.meta, w.state, w.part, st)))) return rc;
-    if (chunks && alone) return HOS_OK;
-    return cuda_rc(launch_attn_rows(a, c->type, c->format, tile, chunks ? tile : 0x7FFFFFFF, w.meta, w.state, w.part, st));
+    int row_workers = 0;
+    if (chunks && (rc = cuda_rc(launch_attn_chunk(a, c->type, c->format, alone ? 0 : tile, w.chunks, st)))) return rc;
+    if (!(chunks && alone) && (rc = cuda_rc(launch_attn_rows(a, c->type, c->format, tile, chunks ? tile : 0x7FFFFFFF, chunks, w.rows,
+                                                             &row_workers, st))))
+        return rc;
+    return cuda_rc(launch_attn_combine(a, c->type, chunks, w.chunks, tile, row_workers, w.rows, st));
 }
 
 }  // extern "C"

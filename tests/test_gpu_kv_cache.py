@@ -397,3 +397,33 @@ def test_refusals():
     none = z((0,), dtype=torch.int32, device="cuda")
     r = h.hos_paged_attention(q[:0], handle, z((1,), dtype=torch.int32, device="cuda"), none, z((0, 1), dtype=torch.int32, device="cuda"), 0)
     assert r["out"].shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("n", [1, 150])
+@pytest.mark.parametrize("fmt", ["same", "e4m3", "int8"])
+def test_a_non_finite_value_is_not_lost(bad, where, n, fmt):
+    """Every row that sees a NaN or infinity (in every column position of a step) has a non-finite output."""
+    h = hos()
+    t, page, d = 300, 32, 128
+    off, kv_len, table, n_pages = R.make_batch([(n, t)], page, 0, 1)
+    q = torch.randn((n, 2, d), device="cuda").bfloat16()
+    x = torch.randn((t, 1, d), device="cuda").bfloat16()
+    first = torch.zeros(2, dtype=torch.int32, device="cuda")
+    first[1] = t
+    for j in (0, 1, 2, 3, 5, 9, 13, 64, 127, 128, 149):
+        cache = make_cache(n_pages, 1, page, d, torch.bfloat16, fmt, 2)
+        handle = h.hos_kv_cache(*cache, dtype=torch.bfloat16)
+        y = x.clone()
+        y[j, 0, 7] = bad
+        h.hos_kv_append(handle, y if where == "k" else x, y if where == "v" else x, first, kv_len, table)
+        out = h.hos_paged_attention(q, handle, off, kv_len, table, n)["out"]
+        # -infinity as a score is a weight of zero: only an 8-bit cache, whose whole vector is NaN then, has to show it;
+        # an infinite score may have either sign
+        if fmt == "same" and where == "k" and not math.isnan(bad):
+            s = (q[:, :, 7].float() * bad) > 0
+            seen = ~torch.isfinite(out).all(-1)
+            assert bool(seen[s].all())
+        else:
+            assert not bool(torch.isfinite(out).all(-1).any())
