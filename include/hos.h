@@ -325,7 +325,7 @@ int hos_trace_offsets(const hos_client_result* cres, int64_t n_units, int64_t* t
  * Element types: queries, new keys and values, and outputs are all HOS_TYPE_BF16 or all
  * HOS_TYPE_FP16.  The cache holds that type (HOS_KV_SAME) or 8-bit codes with one 32-bit scale per
  * token and KV head (HOS_KV_E4M3: floating point, 4 exponent and 3 mantissa bits; HOS_KV_INT8):
- *   a = max(max_d |x_d|, 1e-30), scale = a / Q, code_d = round_to_nearest_even(x_d * (Q / a)),
+ *   a = max(max_d |x_d|, 1e-30), scale = a * (1 / Q), code_d = round_to_nearest_even(x_d * ((1 / a) * Q)),
  *   Q = 448 or 127, each operation rounded to 32 bits;  the value of a code is code * scale.
  * A vector that holds a NaN or an infinity reads back as NaN.
  */

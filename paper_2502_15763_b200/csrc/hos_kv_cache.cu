@@ -1,18 +1,24 @@
 // Keys and values into the pages of the cache (quantised on the way) and back out.
 //
-// Both kernels move each byte once: HBM is the bound, there is next to no arithmetic.  One warp takes
-// one token and HEADS_PER_WARP heads of it.  A vector of head_dim elements is spread over
-// head_dim / 16 lanes with 16 elements (32 bytes) each, so a warp moves four (head_dim 128) or eight
-// (64) vectors per instruction, the largest magnitude of a vector takes two or three shuffles, and a
-// lane's 16 codes leave in one 16-byte store.
+// Both kernels move each byte once: HBM is the bound, there is next to no arithmetic.  A block takes a few
+// consecutive tokens and up to 16 heads: its warps look up the tokens' places together (two or three dependent
+// loads, paid once a block), then the block goes through the vectors, heads first, so that neighbouring vectors
+// lie together on the packed side and neighbouring tokens on the side of the pages.  A vector of head_dim
+// elements is spread over head_dim / 16 lanes with 16 elements (32 bytes) each: the largest magnitude of a vector
+// takes two or three shuffles, and a lane's 16 codes are one 16-byte access.
+#include <initializer_list>
+
 #include "hos_kernels.h"
 #include "hos_kv.cuh"
 
 namespace hos {
 namespace {
 
-constexpr int WARPS = 8;
-constexpr int HEADS_PER_WARP = 16;
+constexpr int WARPS = 8, MOST_TOKENS = 16, APPEND_TOKENS = 4, MOST_HEADS = 16;
+// Vectors that a thread has on the way at once; blocks an SM.  Few and many: reading 31,896 tokens of 64 int8 heads (1.6 GB) takes
+// 331 us with 4 vectors and 4 blocks, 305 with 2 and 5, 265 with 1 and 7; appending 6,634 tokens of 64 heads as e4m3 (329 MB)
+// takes 66, 62 and 63 us.
+constexpr int APPEND_AHEAD = 2, APPEND_BLOCKS = 5, READ_AHEAD = 1, READ_BLOCKS = 7;
 
 // The sequence that owns packed token t: the last one whose offset is <= t (offsets ascend).  All lanes
 // probe at once, so 32 sequences fall in one step, 1,024 in two.
@@ -49,12 +55,24 @@ __device__ __forceinline__ bool find_place(const KvView& c, int t, int& page, in
 
 struct Vec16 { uint32_t w[8]; };                   // 16 elements of 16 bits
 
-__device__ __forceinline__ Vec16 load16(const void* p) {
+// 32 bytes of a lane: one access (and a whole sector) where the addresses allow it.
+__device__ __forceinline__ Vec16 load16(const void* p, bool wide) {
+    Vec16 v;
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7]) : "l"(p));
+        return v;
+    }
     const uint4* q = static_cast<const uint4*>(p);
     const uint4 a = __ldg(q), b = __ldg(q + 1);
     return Vec16{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
-__device__ __forceinline__ void store16(void* p, const Vec16& v) {
+__device__ __forceinline__ void store16(void* p, const Vec16& v, bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     :: "l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]), "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7]) : "memory");
+        return;
+    }
     uint4* q = static_cast<uint4*>(p);
     q[0] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
     q[1] = make_uint4(v.w[4], v.w[5], v.w[6], v.w[7]);
@@ -75,9 +93,9 @@ __device__ __forceinline__ uint4 quantise16(const Vec16& v, int lanes, float* sc
     }
     for (int d = lanes >> 1; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(FULL, top, d));
     const float a = __uint_as_float(top);
-    const float inv = __fdiv_rn(TOP, a);
+    const float inv = __fmul_rn(__frcp_rn(a), TOP);
     // a NaN or an infinity anywhere makes the scale NaN, and with it the whole vector
-    *scale = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __fdiv_rn(a, TOP);
+    *scale = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __fmul_rn(a, 1.0f / TOP);
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -113,120 +131,154 @@ __device__ __forceinline__ Vec16 dequantise16(const uint4& c, float scale) {
     return v;
 }
 
+struct Place { int page, row; };                   // page -1: none
+
+// What a block works on: `tokens` tokens from t0, heads h0 .. h0 + 2^head_shift - 1 (those below n_kv).
+struct Work {
+    int t0, tokens, h0, head_shift;
+};
+__device__ __forceinline__ Work block_work(const KvView& c, int tokens, int head_shift) {
+    Work w;
+    w.t0 = (int)blockIdx.x * tokens;
+    w.tokens = min(tokens, c.n_tokens - w.t0);
+    w.h0 = (int)blockIdx.y << head_shift;
+    w.head_shift = head_shift;
+    return w;
+}
+__device__ __forceinline__ void find_places(const KvView& c, const Work& w, Place* place) {
+    for (int i = warp_id(); i < w.tokens; i += WARPS) {
+        Place p{-1, 0};
+        if (!find_place(c, w.t0 + i, p.page, p.row)) p.page = -1;
+        if (lane_id() == 0) place[i] = p;
+    }
+}
+
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(WARPS * 32) k_kv_append(const __grid_constant__ KvView c, const T* __restrict__ k,
+__global__ void __launch_bounds__(WARPS * 32, APPEND_BLOCKS) k_kv_append(const __grid_constant__ KvView c, const T* __restrict__ k,
                                                          const T* __restrict__ v, long long k_tok, long long k_head,
-                                                         long long v_tok, long long v_head) {
-    constexpr int LANES = D / 16, PER = 32 / LANES, STEPS = HEADS_PER_WARP / PER;
-    const long long t = (long long)blockIdx.x * WARPS + warp_id();
-    if (t >= c.n_tokens) return;
-    const int sub = lane_id() / LANES, at = (lane_id() % LANES) * 16;
-    const int h0 = blockIdx.y * HEADS_PER_WARP;
-    // the loads do not depend on the place, so they are issued before it is known
-    Vec16 xk[STEPS], xv[STEPS];
+                                                         long long v_tok, long long v_head, int tokens, int head_shift, bool wide) {
+    constexpr int AHEAD = APPEND_AHEAD, LANES = D / 16, SPAN = WARPS * 32 / LANES;           // vectors that the block moves at once
+    __shared__ Place place[MOST_TOKENS];
+    const Work w = block_work(c, tokens, head_shift);
+    const int at = ((int)threadIdx.x % LANES) * 16, per_side = w.tokens << head_shift;
+    bool known = false;
+    for (int id0 = (int)threadIdx.x / LANES; id0 - (int)threadIdx.x / LANES < 2 * per_side; id0 += AHEAD * SPAN) {
+        Vec16 x[AHEAD];
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int h = h0 + i * PER + sub;
-        if (h < c.n_kv) {
-            xk[i] = load16(k + t * k_tok + h * k_head + at);
-            xv[i] = load16(v + t * v_tok + h * v_head + at);
-        } else {
-            xk[i] = Vec16{{0, 0, 0, 0, 0, 0, 0, 0}};
-            xv[i] = xk[i];
+        for (int i = 0; i < AHEAD; ++i) {
+            const int id = id0 + i * SPAN, side = id >= per_side, r = side ? id - per_side : id;
+            const int h = w.h0 + (r & ((1 << head_shift) - 1));
+            const long long t = w.t0 + (r >> head_shift);
+            x[i] = Vec16{{0, 0, 0, 0, 0, 0, 0, 0}};
+            if (id < 2 * per_side && h < c.n_kv) x[i] = load16((side ? v + t * v_tok + h * v_head : k + t * k_tok + h * k_head) + at, wide);
         }
-    }
-    int page, row;
-    if (!find_place(c, (int)t, page, row)) return;
+        if (!known) {                              // the first loads are on their way meanwhile
+            find_places(c, w, place);
+            __syncthreads();
+            known = true;
+        }
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int h = h0 + i * PER + sub;
-        const long long e = page_elem(c, page, h, row) + at;
-        if (FMT == HOS_KV_SAME) {
-            if (h < c.n_kv) {
-                store16(c.k + 2 * e, xk[i]);
-                store16(c.v + 2 * e, xv[i]);
-            }
-        } else {
-            float sk, sv;
-            const uint4 ck = quantise16<T, FMT>(xk[i], LANES, &sk);
-            const uint4 cv = quantise16<T, FMT>(xv[i], LANES, &sv);
-            if (h < c.n_kv) {
-                *reinterpret_cast<uint4*>(c.k + e) = ck;
-                *reinterpret_cast<uint4*>(c.v + e) = cv;
-                if (at == 0) {
-                    const long long se = scale_elem(c, page, h, row);
-                    c.k_scale[se] = sk;
-                    c.v_scale[se] = sv;
-                }
+        for (int i = 0; i < AHEAD; ++i) {
+            const int id = id0 + i * SPAN, side = id >= per_side, r = side ? id - per_side : id;
+            const int h = w.h0 + (r & ((1 << head_shift) - 1));
+            uint4 codes = make_uint4(0, 0, 0, 0);
+            float scale = 0.0f;
+            if (FMT != HOS_KV_SAME) codes = quantise16<T, FMT>(x[i], LANES, &scale);
+            if (id >= 2 * per_side || h >= c.n_kv) continue;
+            const Place p = place[r >> head_shift];
+            if (p.page < 0) continue;
+            const long long e = page_elem(c, p.page, h, p.row) + at;
+            if (FMT == HOS_KV_SAME) {
+                store16((side ? c.v : c.k) + 2 * e, x[i], wide);
+            } else {
+                *reinterpret_cast<uint4*>((side ? c.v : c.k) + e) = codes;
+                if (at == 0) (side ? c.v_scale : c.k_scale)[scale_elem(c, p.page, h, p.row)] = scale;
             }
         }
     }
 }
 
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(WARPS * 32) k_kv_read(const __grid_constant__ KvView c, T* __restrict__ k, T* __restrict__ v) {
-    constexpr int LANES = D / 16, PER = 32 / LANES, STEPS = HEADS_PER_WARP / PER;
-    const long long t = (long long)blockIdx.x * WARPS + warp_id();
-    if (t >= c.n_tokens) return;
-    const int sub = lane_id() / LANES, at = (lane_id() % LANES) * 16;
-    const int h0 = blockIdx.y * HEADS_PER_WARP;
-    int page = 0, row = 0;
-    const bool there = find_place(c, (int)t, page, row);
-    Vec16 xk[STEPS], xv[STEPS];
-    uint4 ck[STEPS], cv[STEPS];
-    float sk[STEPS], sv[STEPS];
+__global__ void __launch_bounds__(WARPS * 32, READ_BLOCKS) k_kv_read(const __grid_constant__ KvView c, T* __restrict__ k, T* __restrict__ v,
+                                                       int tokens, int head_shift, bool wide) {
+    constexpr int AHEAD = READ_AHEAD, LANES = D / 16, SPAN = WARPS * 32 / LANES;
+    __shared__ Place place[MOST_TOKENS];
+    const Work w = block_work(c, tokens, head_shift);
+    find_places(c, w, place);
+    __syncthreads();
+    const int at = ((int)threadIdx.x % LANES) * 16, per_side = w.tokens << head_shift;
+    for (int id0 = (int)threadIdx.x / LANES; id0 < 2 * per_side; id0 += AHEAD * SPAN) {
+        Vec16 x[AHEAD];
+        uint4 codes[AHEAD];
+        float scale[AHEAD];
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int h = h0 + i * PER + sub;
-        const long long e = page_elem(c, page, h, row) + at;
-        if (FMT == HOS_KV_SAME) {
-            xk[i] = Vec16{{0, 0, 0, 0, 0, 0, 0, 0}};
-            xv[i] = xk[i];
-            if (there && h < c.n_kv) { xk[i] = load16(c.k + 2 * e); xv[i] = load16(c.v + 2 * e); }
-        } else {
-            ck[i] = make_uint4(0, 0, 0, 0);
-            cv[i] = ck[i];
-            sk[i] = sv[i] = 0.0f;
-            if (there && h < c.n_kv) {
-                ck[i] = __ldg(reinterpret_cast<const uint4*>(c.k + e));
-                cv[i] = __ldg(reinterpret_cast<const uint4*>(c.v + e));
-                const long long se = scale_elem(c, page, h, row);
-                sk[i] = __ldg(c.k_scale + se);
-                sv[i] = __ldg(c.v_scale + se);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int id = id0 + i * SPAN, side = id >= per_side, r = side ? id - per_side : id;
+            const int h = w.h0 + (r & ((1 << head_shift) - 1));
+            x[i] = Vec16{{0, 0, 0, 0, 0, 0, 0, 0}};
+            codes[i] = make_uint4(0, 0, 0, 0);
+            scale[i] = 0.0f;
+            if (id >= 2 * per_side || h >= c.n_kv) continue;
+            const Place p = place[r >> head_shift];
+            if (p.page < 0) continue;
+            const long long e = page_elem(c, p.page, h, p.row) + at;
+            if (FMT == HOS_KV_SAME) {
+                x[i] = load16((side ? c.v : c.k) + 2 * e, wide);
+            } else {
+                codes[i] = __ldg(reinterpret_cast<const uint4*>((side ? c.v : c.k) + e));
+                scale[i] = __ldg((side ? c.v_scale : c.k_scale) + scale_elem(c, p.page, h, p.row));
             }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int h = h0 + i * PER + sub;
-        if (h >= c.n_kv) continue;
-        const long long e = ((long long)t * c.n_kv + h) * D + at;
-        if (FMT != HOS_KV_SAME) {
-            xk[i] = dequantise16<T, FMT>(ck[i], sk[i]);
-            xv[i] = dequantise16<T, FMT>(cv[i], sv[i]);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int id = id0 + i * SPAN, side = id >= per_side, r = side ? id - per_side : id;
+            const int h = w.h0 + (r & ((1 << head_shift) - 1));
+            if (id >= 2 * per_side || h >= c.n_kv) continue;
+            if (FMT != HOS_KV_SAME) x[i] = dequantise16<T, FMT>(codes[i], scale[i]);
+            store16((side ? v : k) + ((long long)(w.t0 + (r >> head_shift)) * c.n_kv + h) * D + at, x[i], wide);
         }
-        store16(k + e, xk[i]);
-        store16(v + e, xv[i]);
     }
 }
 
-struct Grid { dim3 g; };
-dim3 grid_of(const KvView& c) {
-    return dim3((unsigned)((c.n_tokens + WARPS - 1) / WARPS), (unsigned)((c.n_kv + HEADS_PER_WARP - 1) / HEADS_PER_WARP));
+bool multiples32(std::initializer_list<long long> bytes) {
+    for (long long b : bytes)
+        if (b % 32) return false;
+    return true;
+}
+long long address(const void* p) { return static_cast<long long>(reinterpret_cast<uintptr_t>(p)); }
+
+// Blocks of `most_tokens` tokens where there are enough of them to fill the device, else of fewer, for latency.
+struct Shape { dim3 grid; int tokens, head_shift; };
+Shape shape_of(const KvView& c, int most_tokens) {
+    Shape s;
+    s.head_shift = 0;
+    while ((1 << s.head_shift) < c.n_kv && (1 << s.head_shift) < MOST_HEADS) ++s.head_shift;
+    const long long rows = (c.n_kv + (1 << s.head_shift) - 1) >> s.head_shift;
+    s.tokens = most_tokens;
+    while (s.tokens > 1 && (c.n_tokens + s.tokens - 1) / s.tokens * rows < 4 * ATTN_SMS) s.tokens >>= 1;
+    s.grid = dim3((unsigned)((c.n_tokens + s.tokens - 1) / s.tokens), (unsigned)rows);
+    return s;
 }
 
 template <typename T, int FMT, int D>
 cudaError_t append(const KvView& c, const void* k, const void* v, const long long (&st)[4], cudaStream_t stream) {
+    // four tokens: all loads of a block are on their way at once, before the places are known
+    const Shape s = shape_of(c, APPEND_TOKENS);
+    const bool wide = multiples32({address(k), address(v), 2 * st[0], 2 * st[1], 2 * st[2], 2 * st[3]}) &&
+                      (FMT != HOS_KV_SAME || multiples32({address(c.k), address(c.v), 2 * c.page_stride}));
     launch_hook("k_kv_append", 0, stream);
-    k_kv_append<T, FMT, D><<<grid_of(c), WARPS * 32, 0, stream>>>(c, static_cast<const T*>(k), static_cast<const T*>(v),
-                                                                  st[0], st[1], st[2], st[3]);
+    k_kv_append<T, FMT, D><<<s.grid, WARPS * 32, 0, stream>>>(c, static_cast<const T*>(k), static_cast<const T*>(v), st[0], st[1], st[2], st[3],
+                                                              s.tokens, s.head_shift, wide);
     launch_hook("k_kv_append", 1, stream);
     return cudaGetLastError();
 }
 template <typename T, int FMT, int D>
 cudaError_t read(const KvView& c, void* k, void* v, cudaStream_t stream) {
+    const Shape s = shape_of(c, MOST_TOKENS);
+    const bool wide = multiples32({address(k), address(v)}) &&
+                      (FMT != HOS_KV_SAME || multiples32({address(c.k), address(c.v), 2 * c.page_stride}));
     launch_hook("k_kv_read", 0, stream);
-    k_kv_read<T, FMT, D><<<grid_of(c), WARPS * 32, 0, stream>>>(c, static_cast<T*>(k), static_cast<T*>(v));
+    k_kv_read<T, FMT, D><<<s.grid, WARPS * 32, 0, stream>>>(c, static_cast<T*>(k), static_cast<T*>(v), s.tokens, s.head_shift, wide);
     launch_hook("k_kv_read", 1, stream);
     return cudaGetLastError();
 }

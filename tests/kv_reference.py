@@ -29,8 +29,8 @@ def quantise(x, code):
     x = x.float()
     a = x.abs().amax(-1).clamp_min(1e-30)
     top = torch.tensor(TOP[code], dtype=torch.float32, device=x.device)
-    y = x * (top / a)[..., None]
-    return (y.round().to(code) if code == torch.int8 else y.to(code)), a / top
+    y = x * (a.reciprocal() * top)[..., None]
+    return (y.round().to(code) if code == torch.int8 else y.to(code)), a * top.reciprocal()
 
 
 def values(codes, scale):
