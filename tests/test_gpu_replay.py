@@ -1,0 +1,39 @@
+"""A scheduled client's iterations run on the KV-cache operators: every iteration agrees with its trace record, and what the
+cache holds at the end of a prefill and some decode rounds gives the attention that the formulas give."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt,heads,kv_heads,page", [("int8", 16, 2, 128), ("same", 4, 4, 16)])
+def test_replay_follows_the_trace(fmt, heads, kv_heads, page):
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2502_15763_b200 import replay as R
+    from workload import workload
+    w = workload("c0")
+    p, o = (x[0] for x in w.lengths())
+    recs, queue = R.client_schedule(p, o, w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 1)
+    assert len(queue) > 0 and len(recs) > 300
+    r = R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=heads, kv_heads=kv_heads, head_dim=64, page=page, fmt=fmt, repeat=0)
+    assert len(r["us"]) == len(recs) and r["most_pages"] <= r["n_pages"]
+    # every request was prefilled once and decoded o times
+    assert int(r["tokens"][r["prefill"]].sum()) == int(p[queue].sum())
+    assert int(r["n"][~r["prefill"]].sum()) == int(o[queue].sum())
+    timed = R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=heads, kv_heads=kv_heads, head_dim=64, page=page, fmt=fmt, max_iters=30,
+                     repeat=2)
+    f = R.fit(timed, 2)
+    assert f["iterations"] == 30 and (timed["us"] > 0).all() and np.isfinite(f["decode_us_per_kv_token"])
+
+
+def test_replay_notices_a_wrong_trace():
+    from paper_2502_15763_b200 import replay as R
+    from workload import workload
+    w = workload("c0")
+    p, o = (x[0] for x in w.lengths())
+    recs, queue = R.client_schedule(p, o, w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 0)
+    recs = recs.copy()
+    recs["tokens"][5] += 1
+    with pytest.raises(RuntimeError, match="iteration 5"):
+        R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=2, kv_heads=1, head_dim=64, fmt="same", max_iters=10, repeat=0)
