@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -60,6 +61,32 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     return path
 
 
+# The Python module behind kv_cache.py: host code only, against the interpreter's and torch's headers.
+BINDING_SOURCE = os.path.join(CSRC, "hos_kv_binding.cpp")
+BINDING_PATH = os.path.join(_PKG, "_kv.so")
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile hos_kv_binding.cpp into _kv.so; returns its path."""
+    newest = max(os.path.getmtime(f) for f in (BINDING_SOURCE, os.path.join(INCLUDE, "hos.h")))
+    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= newest:
+        return BINDING_PATH
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
+    tmp = BINDING_PATH + f".{os.getpid()}.tmp"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-I", INCLUDE,
+                           "-isystem", home + "/include", "-isystem", home + "/include/torch/csrc/api/include",
+                           "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda + "/include",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", tmp, BINDING_SOURCE,
+                           "-L" + home + "/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, BINDING_PATH)
+    return BINDING_PATH
+
+
 if __name__ == "__main__":
     import sys
     print(build(force=True, verbose="-v" in sys.argv, debug="--debug" in sys.argv))
+    print(build_binding(force=True))
