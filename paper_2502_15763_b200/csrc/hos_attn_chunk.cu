@@ -40,6 +40,10 @@ template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 7.
 template <typename T, int FMT, int D> struct Cfg {
     static constexpr bool Q8 = FMT != HOS_KV_SAME;
     static constexpr int THREADS = Q8 ? 512 : 384;
+    // Registers of the softmax warps and of the others: their sum must not pass what the CTA is launched with, or the wait for more
+    // would not end.
+    static constexpr int SOFTMAX_REGS = Q8 ? 184 : 200, OTHER_REGS = Q8 ? 72 : 104, LAUNCH_REGS = 65536 / THREADS / 8 * 8;
+    static_assert(256 * SOFTMAX_REGS + (THREADS - 256) * OTHER_REGS <= THREADS * LAUNCH_REGS, "");
     static constexpr int TILE_BYTES = STEP * D * 2;            // K or V of a step, 16-bit
     static constexpr int Q_BYTES = HALF * D * 2;               // one half's queries
     static constexpr int STAGES = D == 128 ? 4 : 8;
@@ -96,15 +100,25 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
-// D[128][N] (+)= A[128][16] B[N][16]^T, both in shared memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// D[128][N] (+)= A[128][16] B[N][16]^T, both in shared memory, A_STEP and B_STEP (16-byte units) past the descriptors' addresses.
+// (Added in here so that the sums of every step of a product are not kept in registers.)
+template <int A_STEP, int B_STEP> __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{ .reg .pred p; .reg .b64 x, y; setp.ne.u32 p, %4, 0; add.s64 x, %1, %5; add.s64 y, %2, %6;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "n"(A_STEP), "n"(B_STEP) : "memory");
 }
-// The same with A in tensor memory.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// The same with A in tensor memory, A_STEP columns past its address.
+template <int A_STEP, int B_STEP> __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{ .reg .pred p; .reg .b32 x; .reg .b64 y; setp.ne.u32 p, %4, 0; add.u32 x, %1, %5; add.s64 y, %2, %6;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, p; }"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "n"(A_STEP), "n"(B_STEP) : "memory");
+}
+// f(step tag) for FIRST .. END - 1
+template <int FIRST, int END, typename F> __device__ __forceinline__ void each_step(F&& f) {
+    if constexpr (FIRST < END) {
+        f(IntTag<FIRST>{});
+        each_step<FIRST + 1, END>(f);
+    }
 }
 #define HOS_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define HOS_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -281,7 +295,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 
     if (warp < 8) {
         // ================================ softmax and output ================================
-        if (C::Q8) more_registers<176>(); else more_registers<216>();
+        more_registers<C::SOFTMAX_REGS>();
         const int h = warp >> 2, row = (warp & 3) * 32 + lane;         // row of this half
         const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_tm = tmem + lane_at + h * 128, o_tm = tmem + lane_at + 256 + h * D;
@@ -520,11 +534,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
     } else {
-        if (C::Q8) {
-            fewer_registers<80>();
-        } else {
-            fewer_registers<72>();
-        }
+        fewer_registers<C::OTHER_REGS>();
         if (warp == 8) {
             // ================================ K and V by TMA ================================
             const int box = min(STEP, 1 << a.kv.page_shift), pieces = STEP / box;
@@ -570,18 +580,19 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             bool ok = true, issued = false;
             auto product_qk = [&](int h, int stage) {
                 const uint64_t qa = smem_desc(q_smem + h * C::Q_BYTES, 16), kb = smem_desc(ring + stage * C::TILE_BYTES, 16);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint64_t step = (uint64_t)(((k >> 2) * BLOCK_BYTES + (k & 3) * 32) >> 4);
-                    mma_ss(tmem + h * 128, qa + step, kb + step, QK, k > 0);
-                }
+                each_step<0, D / 16>([&](auto t) {
+                    constexpr int k = decltype(t)::value, step = ((k >> 2) * BLOCK_BYTES + (k & 3) * 32) >> 4;
+                    mma_ss<step, step>(tmem + h * 128, qa, kb, QK, k > 0);
+                });
                 tc_commit(s_full(h));
             };
-            auto product_pv = [&](int h, int stage, bool add, int part_of) {
+            auto product_pv = [&](int h, int stage, bool add, auto part_of) {
                 const uint64_t vb = smem_desc(ring + stage * C::TILE_BYTES, BLOCK_BYTES);
-#pragma unroll
-                for (int k = part_of ? FIRST_PART / 16 : 0; k < (part_of ? STEP : FIRST_PART) / 16; ++k)
-                    mma_ts(tmem + 256 + h * D, tmem + h * 128 + 8 * k, vb + (uint64_t)((k * 16 * 128) >> 4), PV, add || k > 0);
+                constexpr bool first = decltype(part_of)::value == 0;
+                each_step<first ? 0 : FIRST_PART / 16, (first ? FIRST_PART : STEP) / 16>([&](auto t) {
+                    constexpr int k = decltype(t)::value;
+                    mma_ts<8 * k, k * 16 * 128 / 16>(tmem + 256 + h * D, tmem + h * 128, vb, PV, add || k > 0);
+                });
             };
             for (; more && ok; more = list.next(cur, share)) {
                 const Segment seg = segment();
@@ -609,14 +620,14 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                         ok = bar_wait(p_half(h), p_phase[h], gave_up);
                         if (!ok) break;
                         tc_fence_after();
-                        if (elect_one()) product_pv(h, vi % C::STAGES, b > 0, 0);
+                        if (elect_one()) product_pv(h, vi % C::STAGES, b > 0, IntTag<0>{});
                         __syncwarp();
                         ok = bar_wait(p_ready(h), p_phase[h], gave_up);
                         if (!ok) break;
                         p_phase[h] ^= 1;
                         tc_fence_after();
                         if (elect_one()) {
-                            product_pv(h, vi % C::STAGES, true, 1);
+                            product_pv(h, vi % C::STAGES, true, IntTag<1>{});
                             if (more) product_qk(h, ki % C::STAGES); else tc_commit(o_done(h));
                         }
                         __syncwarp();

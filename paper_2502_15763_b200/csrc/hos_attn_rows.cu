@@ -43,7 +43,9 @@ template <typename T, int FMT, int D, int NB> struct Cfg {
     static constexpr int SMEM = WARPS * STAGES * STAGE;
 };
 constexpr int MIN_STEPS = WARPS;              // a CTA's smallest share
-constexpr int TILE_STEPS = 4;                 // what a tile's begin and end cost, in steps
+// What a tile's begin and end cost, in steps.  128 int8 decodes (1,024 tiles of about 65 steps of 32 tokens): 113 us with 4, 108 with 8, 112 with 16;
+// 16 bf16 decodes (1,024 tiles of about 127 steps of 16): 173 us with 4, 172 with 16, 170 with 24.
+template <int SUB> constexpr int TILE_STEPS = SUB == 2 ? 8 : 24;
 // A row's weights are 2^(x - (maximum - LIFT)): in fp16 the largest is 2^14, so that small ones keep their bits
 // down to 2^-28 of it.
 template <typename M> constexpr float LIFT = std::is_same<M, __half>::value ? 14.0f : 0.0f;
@@ -81,7 +83,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     using C = Cfg<T, FMT, D, NB>;
     using M = typename MatType<T, FMT>::type;
     constexpr int STEP = C::STEP, SUB = C::SUB;
-    using List = AttnList<C::ROWS, STEP, TILE_STEPS>;
+    using List = AttnList<C::ROWS, STEP, TILE_STEPS<SUB>>;
     using Cursor = typename List::Cursor;
     constexpr int ROWS = C::ROWS;
     constexpr int KS = D / 16;                 // matrix instructions along head_dim, and tiles of O^T
@@ -548,7 +550,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
         }
     }
         __syncwarp();                          // every lane has read the stage that finish() may use
-        finish(first == 0, end == cons.t.steps, lo + cons.at + TILE_STEPS + cons.t.steps);
+        finish(first == 0, end == cons.t.steps, lo + cons.at + TILE_STEPS<SUB> + cons.t.steps);
     }
     if (!open_end && threadIdx.x == 0) meta[w].last = -1;
     cp_async_wait<0>();
