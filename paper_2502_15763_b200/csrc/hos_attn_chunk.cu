@@ -240,6 +240,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     const int warp = uniform(warp_id()), lane = lane_id(), w = (int)blockIdx.x;
     const List list{a, min_rows, 0x7FFFFFFF};
     pdl_launch_dependents();
+    pdl_wait();
 
     if (warp == 0) {
         long long mine;
@@ -858,9 +859,10 @@ cudaError_t run(const AttnView& a, int min_rows, const AttnWs& ws, cudaStream_t 
     const bool o_tma = make_rows_map(&om, a, a.out, a.o_tok, a.o_head, C::OUT_PIECE / 2, 32);
     if (!make_map(&km, a.kv, a.kv.k) || !make_map(&vm, a.kv, a.kv.v)) return cudaErrorInvalidValue;
     launch_hook("k_attn_chunk", 0, st);
-    k_attn_chunk<T, FMT, D><<<ATTN_SMS, C::THREADS, C::SMEM, st>>>(a, km, vm, qm, om, q_tma, o_tma, min_rows, ws.meta, ws.state, ws.part);
+    e = launch_early(k_attn_chunk<T, FMT, D>, dim3(ATTN_SMS), C::THREADS, C::SMEM, st, a, km, vm, qm, om, q_tma, o_tma, min_rows, ws.meta, ws.state,
+                     ws.part);
     launch_hook("k_attn_chunk", 1, st);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace

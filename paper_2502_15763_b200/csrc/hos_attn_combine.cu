@@ -121,6 +121,7 @@ __device__ __forceinline__ void join_tile(const AttnView& a, const AttnWs& ws, i
 template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_constant__ AttnView a, const AttnWs rows, const int row_workers,
                                                             const AttnWs tiles) {
+    pdl_launch_dependents();
     pdl_wait();
     const int b = (int)blockIdx.x;
     if (b < row_workers) join_rows<T, D, ROWS>(a, rows, b);
@@ -129,17 +130,9 @@ __global__ void __launch_bounds__(WARPS * 32) k_attn_combine(const __grid_consta
 
 template <typename T, int D, int ROWS>
 cudaError_t run(const AttnView& a, bool chunks, const AttnWs& chunk_ws, int row_workers, const AttnWs& row_ws, cudaStream_t st) {
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(row_workers + (chunks ? ATTN_SMS * BIG_BLOCKS : 0)));
-    cfg.blockDim = dim3(WARPS * 32);
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
     launch_hook("k_attn_combine", 0, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_combine<T, D, ROWS>, a, row_ws, row_workers, chunk_ws);
+    const cudaError_t e = launch_early(k_attn_combine<T, D, ROWS>, dim3((unsigned)(row_workers + (chunks ? ATTN_SMS * BIG_BLOCKS : 0))), WARPS * 32, 0, st,
+                                       a, row_ws, row_workers, chunk_ws);
     launch_hook("k_attn_combine", 1, st);
     return e;
 }

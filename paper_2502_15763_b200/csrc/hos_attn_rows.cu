@@ -78,7 +78,7 @@ __device__ __forceinline__ float column_sum(float v) {
 
 template <typename T, int FMT, int D, int NB>
 __global__ void __launch_bounds__(WARPS * 32, Cfg<T, FMT, D, NB>::CTAS)
-k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __restrict__ meta,
+k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool beside, Partial* __restrict__ meta,
             RowState* __restrict__ state, float* __restrict__ part) {
     using C = Cfg<T, FMT, D, NB>;
     using M = typename MatType<T, FMT>::type;
@@ -92,6 +92,8 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, Partial* __r
     const int lane = lane_id(), warp = warp_id(), g = lane >> 2, t4 = lane & 3;
     const int w = (int)blockIdx.x;
     pdl_launch_dependents();
+    // Beside the chunk kernel there is nothing of it to wait for (it waited for what came before) until the end.
+    if (!beside) pdl_wait();
 
     // this CTA's share of the list
     const List list{a, 0, max_rows};
@@ -565,18 +567,8 @@ cudaError_t run(const AttnView& a, int max_rows, bool beside, const AttnWs& ws, 
     if (e != cudaSuccess) return e;
     const int ctas = 148 * C::CTAS;
     *workers = ctas;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(WARPS * 32);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = beside ? 1 : 0;
     launch_hook("k_attn_rows", 0, st);
-    e = cudaLaunchKernelEx(&cfg, k_attn_rows<T, FMT, D, NB>, a, max_rows, ws.meta, ws.state, ws.part);
+    e = launch_early(k_attn_rows<T, FMT, D, NB>, dim3((unsigned)ctas), WARPS * 32, C::SMEM, st, a, max_rows, beside, ws.meta, ws.state, ws.part);
     launch_hook("k_attn_rows", 1, st);
     return e;
 }

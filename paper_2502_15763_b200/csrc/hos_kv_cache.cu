@@ -160,6 +160,8 @@ __global__ void __launch_bounds__(WARPS * 32, APPEND_BLOCKS) k_kv_append(const _
     constexpr int AHEAD = APPEND_AHEAD, LANES = D / 16, SPAN = WARPS * 32 / LANES;           // vectors that the block moves at once
     __shared__ Place place[MOST_TOKENS];
     const Work w = block_work(c, tokens, head_shift);
+    pdl_launch_dependents();
+    pdl_wait();
     const int at = ((int)threadIdx.x % LANES) * 16, per_side = w.tokens << head_shift;
     bool known = false;
     for (int id0 = (int)threadIdx.x / LANES; id0 - (int)threadIdx.x / LANES < 2 * per_side; id0 += AHEAD * SPAN) {
@@ -204,6 +206,8 @@ __global__ void __launch_bounds__(WARPS * 32, READ_BLOCKS) k_kv_read(const __gri
     constexpr int AHEAD = READ_AHEAD, LANES = D / 16, SPAN = WARPS * 32 / LANES;
     __shared__ Place place[MOST_TOKENS];
     const Work w = block_work(c, tokens, head_shift);
+    pdl_launch_dependents();
+    pdl_wait();
     find_places(c, w, place);
     __syncthreads();
     const int at = ((int)threadIdx.x % LANES) * 16, per_side = w.tokens << head_shift;
@@ -267,10 +271,10 @@ cudaError_t append(const KvView& c, const void* k, const void* v, const long lon
     const bool wide = multiples32({address(k), address(v), 2 * st[0], 2 * st[1], 2 * st[2], 2 * st[3]}) &&
                       (FMT != HOS_KV_SAME || multiples32({address(c.k), address(c.v), 2 * c.page_stride}));
     launch_hook("k_kv_append", 0, stream);
-    k_kv_append<T, FMT, D><<<s.grid, WARPS * 32, 0, stream>>>(c, static_cast<const T*>(k), static_cast<const T*>(v), st[0], st[1], st[2], st[3],
-                                                              s.tokens, s.head_shift, wide);
+    const cudaError_t e = launch_early(k_kv_append<T, FMT, D>, s.grid, WARPS * 32, 0, stream, c, static_cast<const T*>(k), static_cast<const T*>(v), st[0],
+                                       st[1], st[2], st[3], s.tokens, s.head_shift, wide);
     launch_hook("k_kv_append", 1, stream);
-    return cudaGetLastError();
+    return e;
 }
 template <typename T, int FMT, int D>
 cudaError_t read(const KvView& c, void* k, void* v, cudaStream_t stream) {
@@ -278,9 +282,10 @@ cudaError_t read(const KvView& c, void* k, void* v, cudaStream_t stream) {
     const bool wide = multiples32({address(k), address(v)}) &&
                       (FMT != HOS_KV_SAME || multiples32({address(c.k), address(c.v), 2 * c.page_stride}));
     launch_hook("k_kv_read", 0, stream);
-    k_kv_read<T, FMT, D><<<s.grid, WARPS * 32, 0, stream>>>(c, static_cast<T*>(k), static_cast<T*>(v), s.tokens, s.head_shift, wide);
+    const cudaError_t e = launch_early(k_kv_read<T, FMT, D>, s.grid, WARPS * 32, 0, stream, c, static_cast<T*>(k), static_cast<T*>(v), s.tokens, s.head_shift,
+                                       wide);
     launch_hook("k_kv_read", 1, stream);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace
