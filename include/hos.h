@@ -384,7 +384,7 @@ int hos_kv_read(const hos_kv_cache* cache, const hos_kv_batch* batch, void* k, v
  *   x_j = sm_scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = ln sum_j exp(x_j).
  * A row that sees nothing gets out = 0, lse = -inf.  Sums, maxima and normalisers are held in 32
  * bits; the weights are rounded to 16 bits (of the output's type, fp16 with an 8-bit cache) for their
- * product with the values.  Memory past a sequence's last token may hold anything, NaN included; a
+ * product with the values, and an 8-bit cache's V scale below 2^-80 counts as 2^-80.  Memory past a sequence's last token may hold anything, NaN included; a
  * non-finite value that some new token of a sequence sees may also reach other new tokens of that sequence.
  *   q    element (token, head, d) at token * q_tok_stride + head * q_head_stride + d (16-byte multiples)
  *   out  likewise with its own strides;  lse [n_tokens][n_heads], nullable

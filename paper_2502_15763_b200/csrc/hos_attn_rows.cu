@@ -19,6 +19,12 @@
 //   - 8-bit codes become fp16 exactly; K's scale multiplies the score, V's scale joins the exponent of
 //     the weight (w_j = 2^(x_j + log2 vs_j - m), m the maximum of that), so no weight under- or overflows fp16
 //     whatever the scales are; the normaliser is sum w_j / vs_j.
+//
+// Measured on one B200, k_attn_combine included: 32,463 tokens of 64 bf16 KV heads of 128 in 16 sequences (1.06 GB) 171 us,
+// 6.2 TB/s; 265,813 tokens of 8 int8 heads in 128 sequences (566 MB) 113-119 us, 4.8-5.0 TB/s; 282,150 tokens of 8 e4m3 heads of
+// 64 in 2 sequences (307 MB) 66 us, 4.7 TB/s.  8-bit caches are bound by instruction issue (12 warps an SM, about 0.6
+// instructions a cycle and scheduler: turning codes into fp16 and the steps' fixed part), 16-bit ones by HBM.  One share a
+// warp instead of one a CTA left four times the pieces and took 125 and 83 us for the last two.
 #include "hos_attn_list.cuh"
 #include "hos_kernels.h"
 #include "hos_kv.cuh"
