@@ -20,9 +20,9 @@
 //     the weight (w_j = 2^(x_j + log2 vs_j - m), m the maximum of that), so no weight under- or overflows fp16
 //     whatever the scales are; the normaliser is sum w_j / vs_j.
 //
-// Measured on one B200, k_attn_combine included: 32,463 tokens of 64 bf16 KV heads of 128 in 16 sequences (1.06 GB) 171 us,
-// 6.2 TB/s; 265,813 tokens of 8 int8 heads in 128 sequences (566 MB) 113-119 us, 4.8-5.0 TB/s; 282,150 tokens of 8 e4m3 heads of
-// 64 in 2 sequences (307 MB) 66 us, 4.7 TB/s.  8-bit caches are bound by instruction issue (12 warps an SM, about 0.6
+// Measured on one B200, k_attn_combine included: 32,463 tokens of 64 bf16 KV heads of 128 in 16 sequences (1.06 GB) 168 us,
+// 6.3 TB/s; 265,813 tokens of 8 int8 heads in 128 sequences (566 MB) 111 us, 5.1 TB/s; 282,150 tokens of 8 e4m3 heads of
+// 64 in 2 sequences (307 MB) 62 us, 5.0 TB/s.  8-bit caches are bound by instruction issue (12 warps an SM, about 0.6
 // instructions a cycle and scheduler: turning codes into fp16 and the steps' fixed part), 16-bit ones by HBM.  One share a
 // warp instead of one a CTA left four times the pieces and took 125 and 83 us for the last two.
 #include "hos_attn_list.cuh"
@@ -157,10 +157,11 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
                 }
             }
             const uint32_t kd = ring + stage * C::STAGE, vd = kd + C::KV_BYTES;
+            int page = -1;
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) {
                 const int js = j0 + 16 * sub, row0 = js & ((1 << a.kv.page_shift) - 1);
-                const int page = __shfl_sync(FULL, pages, (js >> a.kv.page_shift) - pages_at);
+                if (sub == 0 || a.kv.page_shift == 4) page = __shfl_sync(FULL, pages, (js >> a.kv.page_shift) - pages_at);
                 const long long e = page_elem(a.kv, max(page, 0), prod.head, row0) * (C::Q8 ? 1 : 2) + lane * 16;
                 const unsigned char* ksrc = a.kv.k + e;
                 const unsigned char* vsrc = a.kv.v + e;
@@ -180,10 +181,13 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
                         cp_async16(vs + dst_of(i), vsrc + i * 512, real);
                     }
                 }
-                if (C::Q8 && lane < 8) {
-                    const long long se = scale_elem(a.kv, max(page, 0), prod.head, row0) + (lane & 3) * 4;
-                    cp_async16(vd + C::KV_BYTES + (lane < 4 ? 0 : STEP * 4) + sub * 64 + (lane & 3) * 16,
-                               (lane < 4 ? a.kv.k_scale : a.kv.v_scale) + se, page >= 0);
+            }
+            if (C::Q8) {                       // scales, four tokens a lane: K's by the first eight lanes, V's by the next
+                static_assert(!C::Q8 || SUB == 2, "");
+                const int js = j0 + (lane & 7) * 4, at = __shfl_sync(FULL, pages, (js >> a.kv.page_shift) - pages_at);
+                if (lane < 16) {
+                    const long long se = scale_elem(a.kv, max(at, 0), prod.head, js & ((1 << a.kv.page_shift) - 1));
+                    cp_async16(vd + C::KV_BYTES + lane * 16, (lane < 8 ? a.kv.k_scale : a.kv.v_scale) + se, at >= 0);
                 }
             }
             prod.step += WARPS;
