@@ -27,11 +27,13 @@ def _deps():
 
 
 def source_hash() -> str:
-    """SHA-256 over the library's sources (names and contents, in name order): what a set of
-    profiler counters was taken on."""
+    """SHA-256 over the scheduling kernels' sources (names and contents, in name order): what a set of
+    profiler counters of theirs was taken on.  The KV-cache kernels share none of that code."""
     import hashlib
     h = hashlib.sha256()
-    for path in sorted(_deps()):
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.cu*")) + glob.glob(os.path.join(CSRC, "*.h"))):
+        if os.path.basename(path).startswith(("hos_kv", "hos_attn")):
+            continue
         h.update(os.path.basename(path).encode() + b"\0")
         with open(path, "rb") as fh:
             h.update(fh.read())

@@ -31,7 +31,7 @@
 #include <cuda.h>
 
 #include "hos_attn_list.cuh"
-#include "hos_kernels.h"
+#include "hos_kv_kernels.h"
 #include "hos_kv.cuh"
 
 namespace hos {

@@ -4,7 +4,7 @@
 // in base 2), so out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i with m = max_i m_i.  Pieces are added in list
 // order.  Launched so that it may start while the attention kernel drains.  Bound by the latency of two or three dependent loads:
 // 5-7 us for the row kernel's pieces, 8 us for 294 pieces of 256 rows (40 MB).
-#include "hos_kernels.h"
+#include "hos_kv_kernels.h"
 #include "hos_kv.cuh"
 
 namespace hos {

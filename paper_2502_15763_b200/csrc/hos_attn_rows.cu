@@ -26,7 +26,7 @@
 // instructions a cycle and scheduler: turning codes into fp16 and the steps' fixed part), 16-bit ones by HBM.  One share a
 // warp instead of one a CTA left four times the pieces and took 125 and 83 us for the last two.
 #include "hos_attn_list.cuh"
-#include "hos_kernels.h"
+#include "hos_kv_kernels.h"
 #include "hos_kv.cuh"
 
 namespace hos {

@@ -1,7 +1,7 @@
 // C-ABI layer of the KV-cache calls: argument validation, workspace carving, kernel sequencing.
 #include <cmath>
 
-#include "hos_kernels.h"
+#include "hos_kv_kernels.h"
 #include "hos_kv.cuh"
 
 namespace {

@@ -10,7 +10,7 @@
 // read back from int8 (1.58 GB) 265-271 us, 5.9 TB/s.
 #include <initializer_list>
 
-#include "hos_kernels.h"
+#include "hos_kv_kernels.h"
 #include "hos_kv.cuh"
 
 namespace hos {
