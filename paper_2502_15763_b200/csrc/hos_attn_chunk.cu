@@ -27,6 +27,17 @@
 // (The first 96 of a step's 128 weights are handed over early, so that only a quarter of the second product waits for the last
 // exponentials; a third half in flight would need more tensor memory than there is.)
 //
+// Waits by parity: a barrier must not be two phases past (or short of) the one waited for.  Why none is, by barrier:
+//   kv_full    the products' warp waits in order, and a stage is refilled only after that warp has freed it; half 0's wait for V
+//              (clear_v) comes after its score of the step, and the stage is freed only after its weights of the step
+//   raw_full   the warps that convert wait in order, and the refill of a stage needs their arrivals on kv_full
+//   kv_free    the copying warp waits in order, and a stage is freed again only after it has been refilled
+//   q_full, q_free   one of each a tile, and either side needs the other's last one
+//   s_full, o_done   a half's next score needs its weights of this step; its next output needs weights that come after this output
+//   p_half, p_ready  a half's next weights need the score that is issued after the last ones were waited for
+//   scales_full      filled again only after V of the step that read it was freed, which needs all weights of that step; a
+//              half that skips tiles does not run ahead of it, since it waits for its own score first
+//
 // All waits are bounded: one that runs out sets HOS_ST_LIMIT and the CTA drains and returns.
 #include <cuda.h>
 
@@ -208,7 +219,7 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 struct Shared {                                // in the first HEAD bytes
-    uint64_t bars[40];
+    uint64_t bars[48];
     Cursor first;
     long long lo, total, active;
     int share;                                 // steps of this CTA
@@ -246,6 +257,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     auto p_half = [&](int h) { return bar1 + 80 + 8 * h; };
     const uint32_t drain = bar1 + 96;
     auto raw_full = [&](uint32_t i) { return C::Q8 ? bar1 + 104 + 8 * i : kv_full(i); };   // what the copies report to
+    auto scales_full = [&](uint32_t i) { return bar1 + 104 + 8 * (C::STAGES + i); };        // (8-bit cache) a step's scales
+    static_assert(3 * C::STAGES + 13 + C::SCALE_BUFS <= sizeof(Shared::bars) / 8, "");
     const int warp = uniform(warp_id()), lane = lane_id(), w = (int)blockIdx.x;
     const List list{a, min_rows, 0x7FFFFFFF};
     pdl_launch_dependents();
@@ -273,6 +286,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             bar_init(kv_free(i), 1);
             if (C::Q8) bar_init(raw_full(i), 1);
         }
+        if (C::Q8)
+            for (int i = 0; i < C::SCALE_BUFS; ++i) bar_init(scales_full(i), 4);
         for (int h = 0; h < 2; ++h) {
             bar_init(q_full(h), 1);
             bar_init(q_free(h), 1);
@@ -347,12 +362,11 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             for (int b = 0; b < seg.blocks; ++b, ++block) {
                 const int j0 = cur.t.k0 + (cur.step + b) * STEP;
                 const int buf = C::Q8 ? (int)(block % C::SCALE_BUFS) : 0;
-                if (C::Q8) {
-                    const uint32_t item = 2 * block;
-                    if (!bar_wait(kv_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up)) { ok = false; break; }
-                }
                 if (!bar_wait(s_full(h), s_phase, gave_up)) { ok = false; break; }
                 s_phase ^= 1;
+                // The score follows from the step's scales (its K was reported full after them), so this is no wait in time: it makes
+                // them visible.  K's own barrier would not do: its stage may be full of a later step's K by now.
+                if (C::Q8 && !bar_wait(scales_full(buf), (block / C::SCALE_BUFS) & 1, gave_up)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t s[128];
 #pragma unroll
@@ -800,6 +814,8 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc), "f"(f) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + STEP * 4), "f"(lv) : "memory");
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(sc + 2 * STEP * 4), "f"(iv) : "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(scales_full(block % C::SCALE_BUFS));
                 if (++cur.step == end_step) {
                     more = list.next(cur, share);
                     end_step = list.end_of(cur, share);

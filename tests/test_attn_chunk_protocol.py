@@ -1,0 +1,266 @@
+"""The waits of the chunk-attention kernel, as a discrete model of its roles: copies, conversion of 8-bit codes, matrix
+products (one queue, in order), two softmax halves of four warps, queries.  A parity wait passes exactly when the barrier's
+current phase has the other parity, so a barrier two phases from the expected one either lets the wait through too early
+or holds it for ever; the model raises for the first and finds the second because nothing is left to happen.  Durations
+are drawn at random over a wide range, since no order may depend on them.
+
+The model's list of waits is compared with the kernel's source, so that neither is changed alone."""
+import heapq
+import os
+import random
+import re
+
+import pytest
+
+SOURCE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_15763_b200", "csrc", "hos_attn_chunk.cu")
+
+
+class Stuck(Exception):
+    pass
+
+
+class WrongPhase(Exception):
+    pass
+
+
+class Bar:
+    def __init__(self, name, count):
+        self.name, self.count, self.have, self.done = name, count, 0, 0
+
+    def arrive(self):
+        self.have += 1
+        if self.have == self.count:
+            self.have, self.done = 0, self.done + 1
+
+
+class Model:
+    """tiles: (steps, halves) of the tiles of one CTA's share."""
+
+    def __init__(self, tiles, stages, q8, rng, slow=None, wait_for_k_stage=False):
+        self.tiles, self.stages, self.q8, self.rng, self.slow = tiles, stages, q8, rng, slow or {}
+        self.bufs, self.wait_for_k_stage = stages // 2 + 1, wait_for_k_stage
+        n = 4 if q8 else 1
+        self.kv_full = [Bar(f"kv_full{i}", n) for i in range(stages)]
+        self.kv_free = [Bar(f"kv_free{i}", 1) for i in range(stages)]
+        self.raw_full = [Bar(f"raw_full{i}", 1) for i in range(stages)] if q8 else self.kv_full
+        self.scales_full = [Bar(f"scales_full{i}", 4) for i in range(self.bufs)]
+        self.q_full, self.q_free, self.s_full, self.o_done = ([Bar(f"{k}{h}", 1) for h in (0, 1)] for k in ("q_full", "q_free", "s_full", "o_done"))
+        self.p_half, self.p_ready = ([Bar(f"{k}{h}", 4) for h in (0, 1)] for k in ("p_half", "p_ready"))
+        self.named, self.named_gen = 0, 0
+        self.scale_of, self.stage_of = [None] * self.bufs, [None] * stages
+        self.now, self.heap, self.n, self.waiting = 0.0, [], 0, []
+        self.queue_free = 0.0
+
+    # --- clockwork ---
+    def later(self, t, what):
+        self.n += 1
+        heapq.heappush(self.heap, (t, self.n, what))
+
+    def time(self, kind):
+        return self.slow.get(kind, 1.0) * self.rng.choice((0.1, 1.0, 10.0)) * self.rng.random()
+
+    def resume(self, co):
+        for step in co:
+            if step[0] == "sleep":
+                self.later(self.now + step[1], lambda co=co: self.resume(co))
+                return
+            if not self.passes(step):
+                self.waiting.append((step, co))
+                return
+
+    def passes(self, step):
+        if step[0] == "named":
+            return self.named_gen > step[1]
+        _, bar, parity, want = step
+        if (bar.done & 1) == parity:
+            return False
+        if bar.done != want:
+            raise WrongPhase(f"{bar.name}: {bar.done} phases done where {want} were meant")
+        return True
+
+    def run(self):
+        roles = [self.copies(), self.products(), self.queries(0), self.queries(1)]
+        roles += [self.softmax(h) for h in (0, 1) for _ in range(4)] + ([self.convert() for _ in range(4)] if self.q8 else [])
+        left = [len(roles)]
+
+        def counted(role):
+            yield from role
+            left[0] -= 1
+        for r in roles:
+            self.later(0.0, lambda co=counted(r): self.resume(co))
+        while self.heap:
+            self.now, _, what = heapq.heappop(self.heap)
+            what()
+            again = True
+            while again:
+                again = False
+                for i, (step, co) in enumerate(self.waiting):
+                    if self.passes(step):
+                        del self.waiting[i]
+                        self.resume(co)
+                        again = True
+                        break
+        if left[0]:
+            raise Stuck(", ".join(sorted({s[1].name for s, _ in self.waiting if s[0] == "wait"})))
+
+    def issue(self, kind, then):
+        """A matrix product or commit: runs after everything issued before it."""
+        self.queue_free = max(self.queue_free, self.now) + (self.time(kind) if kind else 0.0)
+        self.later(self.queue_free, then)
+
+    @staticmethod
+    def wait(bar, index, flipped=False):
+        """Waits for phase number `index`; flipped: for the one before (a stage that starts out free)."""
+        return ("wait", bar, (index & 1) ^ (1 if flipped else 0), index + (0 if flipped else 1))
+
+    # --- roles, in the kernel's order ---
+    def copies(self):
+        item = 0
+        for blocks, _ in self.tiles:
+            for _ in range(2 * blocks):
+                stage, rnd = item % self.stages, item // self.stages
+                yield self.wait(self.kv_free[stage], rnd, flipped=True)
+
+                def landed(stage=stage, item=item):
+                    self.stage_of[stage] = item
+                    self.raw_full[stage].arrive()
+                self.later(self.now + self.time("copy"), landed)
+                item += 1
+                yield ("sleep", self.time("issue"))
+
+    def convert(self):
+        for block in range(sum(b for b, _ in self.tiles)):
+            item = 2 * block
+            yield self.wait(self.raw_full[item % self.stages], item // self.stages)
+            yield ("sleep", self.time("scales"))
+            self.scale_of[block % self.bufs] = block
+            self.scales_full[block % self.bufs].arrive()
+            for i in (item, item + 1):
+                yield self.wait(self.raw_full[i % self.stages], i // self.stages)
+                yield ("sleep", self.time("codes"))
+                gen = self.named_gen
+                self.named += 1
+                if self.named == 4:
+                    self.named, self.named_gen = 0, gen + 1
+                yield ("named", gen)
+                yield ("sleep", self.time("codes"))
+                self.kv_full[i % self.stages].arrive()
+
+    def products(self):
+        item = tile = 0
+        block = [0, 0]
+
+        def meant(i):
+            if self.stage_of[i % self.stages] != i:
+                raise WrongPhase(f"a product of item {i} reads item {self.stage_of[i % self.stages]}")
+        for blocks, halves in self.tiles:
+            for h in (0, 1):
+                yield self.wait(self.q_full[h], tile)
+            yield self.wait(self.kv_full[item % self.stages], item // self.stages)
+            for h in range(halves):
+                self.issue("qk", lambda i=item: meant(i))
+                self.issue(None, self.s_full[h].arrive)
+            self.issue(None, self.kv_free[item % self.stages].arrive)
+            if blocks == 1:
+                for h in (0, 1):
+                    self.issue(None, self.q_free[h].arrive)
+            for b in range(blocks):
+                vi, ki, more = item + 1, item + 2, b + 1 < blocks
+                yield self.wait(self.kv_full[vi % self.stages], vi // self.stages)
+                if more:
+                    yield self.wait(self.kv_full[ki % self.stages], ki // self.stages)
+                for h in range(halves):
+                    yield self.wait(self.p_half[h], block[h])
+                    self.issue("pv", lambda i=vi: meant(i))
+                    yield self.wait(self.p_ready[h], block[h])
+                    block[h] += 1
+                    self.issue("pv", lambda i=vi: meant(i))
+                    if more:
+                        self.issue("qk", lambda i=ki: meant(i))
+                        self.issue(None, self.s_full[h].arrive)
+                    else:
+                        self.issue(None, self.o_done[h].arrive)
+                self.issue(None, self.kv_free[vi % self.stages].arrive)
+                if more:
+                    self.issue(None, self.kv_free[ki % self.stages].arrive)
+                if b + 2 == blocks:
+                    for h in (0, 1):
+                        self.issue(None, self.q_free[h].arrive)
+                item += 2
+                yield ("sleep", self.time("issue"))
+            tile += 1
+
+    def queries(self, h):
+        for tile in range(len(self.tiles)):
+            yield self.wait(self.q_free[h], tile, flipped=True)
+            yield ("sleep", self.time("queries"))
+            self.q_full[h].arrive()
+
+    def softmax(self, h):
+        block = mine = tiles = 0
+        for blocks, halves in self.tiles:
+            if h >= halves:
+                block += blocks
+                continue
+            for _ in range(blocks):
+                if self.wait_for_k_stage:
+                    yield self.wait(self.kv_full[2 * block % self.stages], 2 * block // self.stages)
+                yield self.wait(self.s_full[h], mine)
+                mine += 1
+                if self.q8 and not self.wait_for_k_stage:
+                    yield self.wait(self.scales_full[block % self.bufs], block // self.bufs)
+                if self.q8 and self.scale_of[block % self.bufs] != block:
+                    raise WrongPhase("scales of another step")
+                yield ("sleep", self.time("weights"))
+                if not self.q8 and h == 0:
+                    yield self.wait(self.kv_full[(2 * block + 1) % self.stages], (2 * block + 1) // self.stages)
+                self.p_half[h].arrive()
+                yield ("sleep", self.time("weights"))
+                if self.q8 and self.scale_of[block % self.bufs] != block:
+                    raise WrongPhase("scales of another step")
+                self.p_ready[h].arrive()
+                block += 1
+            yield self.wait(self.o_done[h], tiles)
+            tiles += 1
+            yield ("sleep", self.time("output"))
+
+
+def test_waits_of_the_source():
+    text = open(SOURCE).read()
+    marks = ["softmax and output =", "K and V by TMA =", "the products =", "queries =", "K and V of an 8-bit cache =", "tcgen05.dealloc"]
+    at = [text.index(m) for m in marks]
+    assert at == sorted(at)
+    waits = [re.findall(r"bar_wait\((\w+)\(", text[a:b]) for a, b in zip(at, at[1:])]
+    assert waits == [
+        ["kv_full", "s_full", "scales_full", "o_done"],           # kv_full: in clear_v, V of a step with hidden tokens, half 0, 16-bit
+        ["kv_free"],
+        ["q_full", "kv_full", "kv_full", "kv_full", "p_half", "p_ready"],
+        ["q_free"],
+        ["raw_full", "raw_full"],                                 # in convert; of the step's K before its scales are written
+    ]
+    convert = text[at[4]:at[5]]
+    assert convert.index("bar_arrive(scales_full(") < convert.index("!convert(item")
+    assert convert.index("fence_async_smem") < convert.index("bar_arrive(kv_full(")
+
+
+SHAPES = [[(b, 2) for b in (1, 2, 3, 4, 7, 1, 1, 5, 3)], [(3, 2)] * 12, [(1, 1)] * 9 + [(2, 2)] * 4, [(b, 1 + b % 2) for b in range(1, 12)],
+          [(20, 1), (1, 2), (9, 1), (9, 1), (1, 2), (30, 2)]]
+
+
+@pytest.mark.parametrize("stages", [4, 8])
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("slow", [{}, {"output": 100.0}, {"weights": 50.0}, {"copy": 50.0}, {"qk": 30.0, "pv": 30.0}, {"codes": 30.0},
+                                  {"queries": 60.0}, {"scales": 40.0}], ids=lambda s: "+".join(s) or "even")
+def test_no_order_depends_on_time(stages, q8, slow):
+    for seed in range(12):
+        for tiles in SHAPES:
+            Model(tiles, stages, q8, random.Random(seed), slow).run()
+
+
+def test_the_model_finds_a_wait_on_a_reused_stage():
+    """Waiting for K's stage in the softmax warps stops everything once a tile's output takes long."""
+    with pytest.raises((Stuck, WrongPhase)):
+        for seed in range(20):
+            Model([(3, 2)] * 6, 4, True, random.Random(seed), {"output": 100.0}, wait_for_k_stage=True).run()
+    with pytest.raises(Stuck):
+        Model([(3, 2)] * 6, 4, True, random.Random(0), {"output": 1e4}, wait_for_k_stage=True).run()
