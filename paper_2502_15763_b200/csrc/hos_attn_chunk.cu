@@ -261,8 +261,10 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     static_assert(3 * C::STAGES + 13 + C::SCALE_BUFS <= sizeof(Shared::bars) / 8, "");
     const int warp = uniform(warp_id()), lane = lane_id(), w = (int)blockIdx.x;
     const List list{a, min_rows, 0x7FFFFFFF};
-    pdl_launch_dependents();
+    // In this order: the row kernel of the same call starts on this signal and reads and writes at once what the kernels
+    // before this one wrote and read.
     pdl_wait();
+    pdl_launch_dependents();
 
     if (warp == 0) {
         long long mine;

@@ -98,8 +98,11 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
     const int lane = lane_id(), warp = warp_id(), g = lane >> 2, t4 = lane & 3;
     const int w = (int)blockIdx.x;
     pdl_launch_dependents();
-    // Beside the chunk kernel there is nothing of it to wait for (it waited for what came before) until the end.
-    if (!beside) pdl_wait();
+    // Beside the chunk kernel there is nothing of it to wait for until the end, and what came before is complete: that kernel
+    // lets this one start only after its own wait for it, in every CTA (it has to stay so).  The fence drops what this
+    // SM's L1 may still hold from before.
+    if (beside) __threadfence();
+    else pdl_wait();
 
     // this CTA's share of the list
     const List list{a, 0, max_rows};

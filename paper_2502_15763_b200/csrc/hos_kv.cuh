@@ -127,7 +127,9 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 }
 
 // Programmatic dependent launch: a kernel launched with the attribute may start while its predecessor
-// drains; it must not touch the predecessor's results before the wait.
+// drains.  The wait covers the direct predecessor only; that what came before it is complete as well follows
+// from the predecessor's own wait, so every kernel waits in all its threads and on every way out, and before it
+// touches memory.  The one exception is the row kernel beside the chunk kernel, which waits at its end.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
