@@ -216,6 +216,13 @@ __device__ __forceinline__ void lds_f2x2(uint32_t addr, F2& a, F2& b) {
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// Named barrier of 128 threads (whole warps); true if `mine` holds in all of them.
+__device__ __forceinline__ bool all_of_four_warps(bool mine) {
+    uint32_t all;
+    asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.and.pred q, 1, 128, p; selp.u32 %0, 1, 0, q; }"
+                 : "=r"(all) : "r"((uint32_t)mine) : "memory");
+    return all != 0;
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 struct Shared {                                // in the first HEAD bytes
@@ -771,9 +778,11 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 vs = __ldg(a.kv.v_scale + e);
                 seen = true;
             };
-            auto convert = [&](uint32_t item, int first, int end) {     // rows outside [first, end) become zeros
+            // Rows outside [first, end) become zeros.  A warp whose wait ran out still comes to the named barrier, which knows no limit:
+            // the four warps vote there and leave together.
+            auto convert = [&](uint32_t item, int first, int end, bool ok) {
                 const uint32_t stage = item % C::STAGES, at = ring + stage * C::TILE_BYTES;
-                if (!bar_wait(raw_full(stage), (item / C::STAGES) & 1, gave_up)) return false;
+                ok = ok && bar_wait(raw_full(stage), (item / C::STAGES) & 1, gave_up);
                 uint4 x[PASSES];
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
@@ -781,7 +790,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     x[i] = lds<uint4>(at + C::TILE_BYTES / 2 + r * D + sub * 16);
                     if (r < first || r >= end) x[i] = make_uint4(0, 0, 0, 0);
                 }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (!all_of_four_warps(ok)) return false;
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int r = i * PER_PASS + row0;
@@ -809,7 +818,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                 const uint32_t item = 2 * block;
                 // The buffer's last reader was done before the stage that V of this step will take was free, and K's
                 // copy was issued after that.
-                if (!bar_wait(raw_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up)) break;
+                const bool ok = bar_wait(raw_full(item % C::STAGES), (item / C::STAGES) & 1, gave_up);
                 const uint32_t sc = scales + (block % C::SCALE_BUFS) * (3 * STEP * 4) + tid * 4;
                 const float v1 = fmaxf(vs, LEAST_V_SCALE);
                 const float f = seen ? c * ks : 0.0f, lv = seen ? (vs != vs ? vs : __log2f(v1)) : -INFINITY, iv = seen ? 1.0f / v1 : 0.0f;
@@ -823,7 +832,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     end_step = list.end_of(cur, share);
                 }
                 if (more) fetch_scales();
-                if (!convert(item, first, end) || !convert(item + 1, first, end)) break;
+                if (!convert(item, first, end, ok) || !convert(item + 1, first, end, true)) break;
             }
         }
     }

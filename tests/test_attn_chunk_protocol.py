@@ -2,7 +2,8 @@
 products (one queue, in order), two softmax halves of four warps, queries.  A parity wait passes exactly when the barrier's
 current phase has the other parity, so a barrier two phases from the expected one either lets the wait through too early
 or holds it for ever; the model raises for the first and finds the second because nothing is left to happen.  Durations
-are drawn at random over a wide range, since no order may depend on them.
+are drawn at random over a wide range, since no order may depend on them.  A wait that runs out makes every role leave: each
+notices that at its next wait that does not pass, after a while of its own.
 
 The model's list of waits is compared with the kernel's source, so that neither is changed alone."""
 import heapq
@@ -36,7 +37,7 @@ class Bar:
 class Model:
     """tiles: (steps, halves) of the tiles of one CTA's share."""
 
-    def __init__(self, tiles, stages, q8, rng, slow=None, wait_for_k_stage=False):
+    def __init__(self, tiles, stages, q8, rng, slow=None, wait_for_k_stage=False, gives_up_at=None, vote=True):
         self.tiles, self.stages, self.q8, self.rng, self.slow = tiles, stages, q8, rng, slow or {}
         self.bufs, self.wait_for_k_stage = stages // 2 + 1, wait_for_k_stage
         n = 4 if q8 else 1
@@ -46,10 +47,11 @@ class Model:
         self.scales_full = [Bar(f"scales_full{i}", 4) for i in range(self.bufs)]
         self.q_full, self.q_free, self.s_full, self.o_done = ([Bar(f"{k}{h}", 1) for h in (0, 1)] for k in ("q_full", "q_free", "s_full", "o_done"))
         self.p_half, self.p_ready = ([Bar(f"{k}{h}", 4) for h in (0, 1)] for k in ("p_half", "p_ready"))
-        self.named, self.named_gen = 0, 0
+        self.named, self.named_gen, self.votes, self.outcome = 0, 0, [], {}
         self.scale_of, self.stage_of = [None] * self.bufs, [None] * stages
         self.now, self.heap, self.n, self.waiting = 0.0, [], 0, []
         self.queue_free = 0.0
+        self.gave_up, self.gives_up_at, self.vote = False, gives_up_at, vote
 
     # --- clockwork ---
     def later(self, t, what):
@@ -59,14 +61,36 @@ class Model:
     def time(self, kind):
         return self.slow.get(kind, 1.0) * self.rng.choice((0.1, 1.0, 10.0)) * self.rng.random()
 
-    def resume(self, co):
-        for step in co:
-            if step[0] == "sleep":
-                self.later(self.now + step[1], lambda co=co: self.resume(co))
-                return
-            if not self.passes(step):
-                self.waiting.append((step, co))
-                return
+    def resume(self, co, value=None):
+        try:
+            while True:
+                step = co.send(value)
+                if step[0] == "sleep":
+                    self.later(self.now + step[1], lambda: self.resume(co))
+                    return
+                if not self.passes(step):
+                    self.waiting.append((step, co))
+                    if self.gave_up:
+                        self.notice(step, co)
+                    return
+                value = True
+        except StopIteration:
+            pass
+
+    def notice(self, step, co):
+        """The waiting role sees some time later that another has given up, unless its wait has passed by then."""
+        def look():
+            for i, (s, c) in enumerate(self.waiting):
+                if s is step and c is co and s[0] == "wait":
+                    del self.waiting[i]
+                    self.resume(co, False)
+                    return
+        self.later(self.now + 20.0 * self.rng.random(), look)
+
+    def give_up(self):
+        self.gave_up = True
+        for step, co in list(self.waiting):
+            self.notice(step, co)
 
     def passes(self, step):
         if step[0] == "named":
@@ -88,6 +112,8 @@ class Model:
             left[0] -= 1
         for r in roles:
             self.later(0.0, lambda co=counted(r): self.resume(co))
+        if self.gives_up_at is not None:
+            self.later(self.gives_up_at, self.give_up)
         while self.heap:
             self.now, _, what = heapq.heappop(self.heap)
             what()
@@ -97,7 +123,7 @@ class Model:
                 for i, (step, co) in enumerate(self.waiting):
                     if self.passes(step):
                         del self.waiting[i]
-                        self.resume(co)
+                        self.resume(co, True)
                         again = True
                         break
         if left[0]:
@@ -119,7 +145,8 @@ class Model:
         for blocks, _ in self.tiles:
             for _ in range(2 * blocks):
                 stage, rnd = item % self.stages, item // self.stages
-                yield self.wait(self.kv_free[stage], rnd, flipped=True)
+                if not (yield self.wait(self.kv_free[stage], rnd, flipped=True)):
+                    return
 
                 def landed(stage=stage, item=item):
                     self.stage_of[stage] = item
@@ -131,18 +158,30 @@ class Model:
     def convert(self):
         for block in range(sum(b for b, _ in self.tiles)):
             item = 2 * block
-            yield self.wait(self.raw_full[item % self.stages], item // self.stages)
+            ok = yield self.wait(self.raw_full[item % self.stages], item // self.stages)
+            if not self.vote and not ok:
+                return
             yield ("sleep", self.time("scales"))
-            self.scale_of[block % self.bufs] = block
+            if ok:
+                self.scale_of[block % self.bufs] = block
             self.scales_full[block % self.bufs].arrive()
             for i in (item, item + 1):
-                yield self.wait(self.raw_full[i % self.stages], i // self.stages)
+                if i > item:
+                    ok = True
+                if ok:
+                    ok = yield self.wait(self.raw_full[i % self.stages], i // self.stages)
+                if not self.vote and not ok:
+                    return
                 yield ("sleep", self.time("codes"))
                 gen = self.named_gen
                 self.named += 1
+                self.votes.append(ok)
                 if self.named == 4:
+                    self.outcome[gen], self.votes = all(self.votes), []
                     self.named, self.named_gen = 0, gen + 1
                 yield ("named", gen)
+                if not self.outcome[gen]:
+                    return
                 yield ("sleep", self.time("codes"))
                 self.kv_full[i % self.stages].arrive()
 
@@ -155,8 +194,10 @@ class Model:
                 raise WrongPhase(f"a product of item {i} reads item {self.stage_of[i % self.stages]}")
         for blocks, halves in self.tiles:
             for h in (0, 1):
-                yield self.wait(self.q_full[h], tile)
-            yield self.wait(self.kv_full[item % self.stages], item // self.stages)
+                if not (yield self.wait(self.q_full[h], tile)):
+                    return
+            if not (yield self.wait(self.kv_full[item % self.stages], item // self.stages)):
+                return
             for h in range(halves):
                 self.issue("qk", lambda i=item: meant(i))
                 self.issue(None, self.s_full[h].arrive)
@@ -166,13 +207,17 @@ class Model:
                     self.issue(None, self.q_free[h].arrive)
             for b in range(blocks):
                 vi, ki, more = item + 1, item + 2, b + 1 < blocks
-                yield self.wait(self.kv_full[vi % self.stages], vi // self.stages)
+                if not (yield self.wait(self.kv_full[vi % self.stages], vi // self.stages)):
+                    return
                 if more:
-                    yield self.wait(self.kv_full[ki % self.stages], ki // self.stages)
+                    if not (yield self.wait(self.kv_full[ki % self.stages], ki // self.stages)):
+                        return
                 for h in range(halves):
-                    yield self.wait(self.p_half[h], block[h])
+                    if not (yield self.wait(self.p_half[h], block[h])):
+                        return
                     self.issue("pv", lambda i=vi: meant(i))
-                    yield self.wait(self.p_ready[h], block[h])
+                    if not (yield self.wait(self.p_ready[h], block[h])):
+                        return
                     block[h] += 1
                     self.issue("pv", lambda i=vi: meant(i))
                     if more:
@@ -192,7 +237,8 @@ class Model:
 
     def queries(self, h):
         for tile in range(len(self.tiles)):
-            yield self.wait(self.q_free[h], tile, flipped=True)
+            if not (yield self.wait(self.q_free[h], tile, flipped=True)):
+                return
             yield ("sleep", self.time("queries"))
             self.q_full[h].arrive()
 
@@ -204,23 +250,28 @@ class Model:
                 continue
             for _ in range(blocks):
                 if self.wait_for_k_stage:
-                    yield self.wait(self.kv_full[2 * block % self.stages], 2 * block // self.stages)
-                yield self.wait(self.s_full[h], mine)
+                    if not (yield self.wait(self.kv_full[2 * block % self.stages], 2 * block // self.stages)):
+                        return
+                if not (yield self.wait(self.s_full[h], mine)):
+                    return
                 mine += 1
                 if self.q8 and not self.wait_for_k_stage:
-                    yield self.wait(self.scales_full[block % self.bufs], block // self.bufs)
+                    if not (yield self.wait(self.scales_full[block % self.bufs], block // self.bufs)):
+                        return
                 if self.q8 and self.scale_of[block % self.bufs] != block:
                     raise WrongPhase("scales of another step")
                 yield ("sleep", self.time("weights"))
                 if not self.q8 and h == 0:
-                    yield self.wait(self.kv_full[(2 * block + 1) % self.stages], (2 * block + 1) // self.stages)
+                    if not (yield self.wait(self.kv_full[(2 * block + 1) % self.stages], (2 * block + 1) // self.stages)):
+                        return
                 self.p_half[h].arrive()
                 yield ("sleep", self.time("weights"))
                 if self.q8 and self.scale_of[block % self.bufs] != block:
                     raise WrongPhase("scales of another step")
                 self.p_ready[h].arrive()
                 block += 1
-            yield self.wait(self.o_done[h], tiles)
+            if not (yield self.wait(self.o_done[h], tiles)):
+                return
             tiles += 1
             yield ("sleep", self.time("output"))
 
@@ -239,6 +290,10 @@ def test_waits_of_the_source():
         ["raw_full", "raw_full"],                                 # in convert; of the step's K before its scales are written
     ]
     convert = text[at[4]:at[5]]
+    # the named barrier has no limit: all four warps come to it, whatever became of their waits, and leave on the common vote only
+    assert "bar.sync" not in convert and convert.count("all_of_four_warps(") == 1
+    loop = convert[convert.index("for (int block"):]
+    assert "break" not in loop[:loop.index("!convert(item")] and "return" not in convert[convert.index("auto convert"):convert.index("if (!all_of_four_warps")]
     assert convert.index("bar_arrive(scales_full(") < convert.index("!convert(item")
     assert convert.index("fence_async_smem") < convert.index("bar_arrive(kv_full(")
 
@@ -264,3 +319,18 @@ def test_the_model_finds_a_wait_on_a_reused_stage():
             Model([(3, 2)] * 6, 4, True, random.Random(seed), {"output": 100.0}, wait_for_k_stage=True).run()
     with pytest.raises(Stuck):
         Model([(3, 2)] * 6, 4, True, random.Random(0), {"output": 1e4}, wait_for_k_stage=True).run()
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_every_role_leaves_once_a_wait_has_run_out(q8):
+    for seed in range(150):
+        rng = random.Random(seed)
+        Model(SHAPES[seed % len(SHAPES)], rng.choice((4, 8)), q8, rng, {rng.choice(("copy", "output", "codes", "qk")): 30.0},
+              gives_up_at=rng.random() * 600.0).run()
+
+
+def test_the_model_finds_warps_that_leave_before_the_named_barrier():
+    with pytest.raises(Stuck):
+        for seed in range(300):
+            rng = random.Random(seed)
+            Model(SHAPES[seed % len(SHAPES)], 4, True, rng, {"copy": 30.0}, gives_up_at=rng.random() * 600.0, vote=False).run()
