@@ -565,7 +565,6 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             tc_fence_before();
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        if (!ok && threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status + cur.seq, HOS_ST_LIMIT);
     } else {
         fewer_registers<C::OTHER_REGS>();
         if (warp == 8) {
@@ -839,6 +838,12 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (*gave_up && threadIdx.x == 0 && a.kv.status) {
+        // whichever wait ran out: rows of any sequence in this share may be missing
+        Cursor c = sh.first;
+        do atomicOr(a.kv.status + c.seq, HOS_ST_LIMIT);
+        while (list.next(c, share));
+    }
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem));
 }
 

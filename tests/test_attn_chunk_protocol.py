@@ -334,3 +334,14 @@ def test_the_model_finds_warps_that_leave_before_the_named_barrier():
         for seed in range(300):
             rng = random.Random(seed)
             Model(SHAPES[seed % len(SHAPES)], 4, True, rng, {"copy": 30.0}, gives_up_at=rng.random() * 600.0, vote=False).run()
+
+
+def test_a_wait_that_ran_out_is_reported_whoever_waited():
+    """After all roles have met again, from the flag they share, for every sequence of the share."""
+    text = open(SOURCE).read()
+    body = text[text.index("__global__"):text.index("// Tensor map of k or v")]
+    assert len(re.findall(r"a\.kv\.status \+ \S+, HOS_ST_LIMIT", body)) == 1
+    last = body.rindex("__syncthreads();")
+    report = body.index("HOS_ST_LIMIT")
+    assert last < body.index("if (*gave_up && threadIdx.x == 0 && a.kv.status)") < report < body.index("tcgen05.dealloc")
+    assert "while (list.next(c, share));" in body[report:]
