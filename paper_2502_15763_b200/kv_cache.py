@@ -72,6 +72,8 @@ class KvCache:
         n_pages, n_kv, page, dim = k.shape
         if tuple(k.stride()[1:]) != (page * dim, dim, 1):
             raise ValueError("k, v: only the pages may be strided")
+        if n_pages > 1 and k.stride(0) < n_kv * page * dim:      # 0, an expanded page, would mean densely packed pages below
+            raise ValueError("k, v: pages must not overlap")
         scale_stride = 0
         if self.format != HOS_KV_SAME:
             for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
@@ -81,6 +83,8 @@ class KvCache:
                     raise ValueError(f"{what}: expected [n_pages][n_kv_heads][page_size], strided by pages only")
             if k_scale.stride(0) != v_scale.stride(0):
                 raise ValueError("k_scale and v_scale must have the same strides")
+            if n_pages > 1 and k_scale.stride(0) < n_kv * page:
+                raise ValueError("k_scale, v_scale: pages must not overlap")
             scale_stride = k_scale.stride(0)
         elif k_scale is not None or v_scale is not None:
             raise ValueError("scales belong to an 8-bit cache")
