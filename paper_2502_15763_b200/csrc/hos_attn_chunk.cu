@@ -365,7 +365,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             const int pos = cur.q.len - cur.q.n + tok;
             // rows past the tile see everything: no masking, and they are not written
             const int see_hi = !there ? 0x7FFFFFFF : a.causal ? min(cur.q.len, pos + 1) : cur.q.len;
-            const int see_lo = there && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+            const int see_lo = there ? first_seen(a, pos) : 0;
             float m = -INFINITY, l = 0.0f;
 #pragma unroll 1
             for (int b = 0; b < seg.blocks; ++b, ++block) {

@@ -39,7 +39,7 @@ template <int ROWS, int STEP, int START> struct AttnList {
         const int base = q.len - q.n;
         t.ke = a.causal ? min(q.len, base + by_group(a, first + t.rows - 1) + 1) : q.len;
         t.ke = max(t.ke, 0);
-        t.kb = a.window > 0 ? max(0, min(base + by_group(a, first) - a.window + 1, t.ke)) : 0;
+        t.kb = min(first_seen(a, base + by_group(a, first)), t.ke);
         t.k0 = t.kb & ~(STEP - 1);
         t.steps = max(1, (t.ke - t.k0 + STEP - 1) / STEP);
         return t;

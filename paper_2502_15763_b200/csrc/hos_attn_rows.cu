@@ -216,7 +216,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
             const int first = cons.q.len - cons.q.n + by_group(a, cons.tile * ROWS);
             const int last = cons.q.len - cons.q.n + by_group(a, cons.tile * ROWS + cons.t.rows - 1);
             all_hi = a.causal ? min(cons.q.len, first + 1) : cons.q.len;
-            all_lo = a.window > 0 ? max(0, last - a.window + 1) : 0;
+            all_lo = first_seen(a, last);
         }
 #pragma unroll
         for (int i = 0; i < KS; ++i)
@@ -271,7 +271,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
                 // columns past the tile see everything that its rows do; they are not written
                 const bool real = nb * 8 + 2 * t4 + e < cons.t.rows;
                 see_hi[nb][e] = real && a.causal ? min(cons.q.len, pos + 1) : cons.q.len;
-                see_lo[nb][e] = real && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+                see_lo[nb][e] = real ? first_seen(a, pos) : 0;
                 qmul[nb][e] = __shfl_sync(FULL, mul, (2 * t4 + e) * 4);
                 m[nb][e] = -INFINITY;
                 l[nb][e] = 0.0f;

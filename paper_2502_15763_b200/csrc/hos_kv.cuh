@@ -154,6 +154,12 @@ __device__ __forceinline__ int by_group(const AttnView& a, int n) {
     return (int)(((uint32_t)n + __umulhi((uint32_t)n, a.group_magic)) >> a.group_shift);
 }
 
+// The first token that a row at position pos sees.  Positions below 0 (more new tokens than the cache holds) see what 0 sees
+// there; so counted, the difference stays in 32 bits for every window.
+__device__ __forceinline__ int first_seen(const AttnView& a, int pos) {
+    return a.window > 0 ? max(0, max(pos, 0) - a.window + 1) : 0;
+}
+
 // Workspace of an attention call.  A worker (warp or CTA) owns a contiguous range of the call's work
 // units; a tile that crosses the range's ends is left as a partial result: slot 0 if the tile began in an
 // earlier worker's range, slot 1 if it begins here and ends later.
