@@ -71,12 +71,17 @@ template <typename T, int FMT, int D> struct Cfg {
     static constexpr int OUT_BYTES = 8 * 32 * OUT_PIECE;
     static constexpr int SCALE_BUFS = STAGES / 2 + 1;
     static constexpr int SCALES = Q8 ? SCALE_BUFS * 3 * STEP * 4 : 0;
-    static constexpr bool Q_RANGE = Q8 && !std::is_same<T, __half>::value;   // bf16 queries become fp16
+    static constexpr bool Q_RANGE = Q8 && !std::is_same<T, __half>::value;   // bf16 queries become fp16: see Q_LIFT
     static constexpr int Q_SCALES = Q_RANGE ? 2 * ROWS * 4 : 0;
     static constexpr int HEAD = 1024;                          // barriers, the cursor, the tensor memory address
     static constexpr int SMEM = 1024 /*alignment*/ + HEAD + 2 * Q_BYTES + STAGES * TILE_BYTES + OUT_BYTES + SCALES + Q_SCALES;
     static_assert(SMEM <= (int)SMEM_LIMIT, "");
 };
+// bf16 queries meet the fp16 values of an 8-bit cache, lifted by 2^9, which the scales take back: a row whose largest element is in
+// [2^-3, 2^6) then has it in [2^6, 2^15), and any other row is brought to [2^13, 2^14) by a power of two of its own, which
+// costs its warp a multiplication a score.  Elements down to 2^-23 of the row's largest are exact, smaller ones rounded to
+// within 2^-31 of it.
+constexpr int Q_LIFT = 9;
 template <typename T, int FMT> struct MatType { using type = __half; };
 template <typename T> struct MatType<T, HOS_KV_SAME> { using type = T; };
 
@@ -727,7 +732,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
                     const uint4 v = batch[i];
                     uint32_t x[4] = {v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
                     if (C::Q_RANGE) {
-                        // a row whose largest element is outside [2^-6, 2^15) is brought to [2^13, 2^14) by a power of two
+                        // rows of zeros, of nothing above 2^-100 and non-finite ones get the lift alone
                         float2 f[4];
                         float top = 0.0f;
 #pragma unroll
@@ -738,13 +743,13 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
 #pragma unroll
                         for (int d = CH / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
                         const int ex = (int)(__float_as_uint(top) >> 23);
-                        const int sh = ex >= 27 && ex < 254 && (ex < 121 || ex >= 142) ? 140 - ex : 0;
+                        const int sh = ex >= 27 && ex < 254 && (ex < 127 - 3 || ex >= 127 + 6) ? 140 - ex : Q_LIFT;
                         const float up = __uint_as_float((uint32_t)(127 + sh) << 23);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) x[k] = Pair<__half>::pack(f[k].x * up, f[k].y * up);
                         if (ch == 0)
                             asm volatile("st.shared.f32 [%0], %1;" :: "r"(q_scales + (q_buf * ROWS + h * HALF + r) * 4),
-                                         "f"(__uint_as_float((uint32_t)(127 - sh) << 23)) : "memory");
+                                         "f"(__uint_as_float((uint32_t)(127 + Q_LIFT - sh) << 23)) : "memory");
                     }
                     st_shared16(dst + (ch >> 3) * BLOCK_BYTES + r * 128 + ((ch & 7) ^ (r & 7)) * 16, make_uint4(x[0], x[1], x[2], x[3]));
                     }
@@ -762,7 +767,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             // stage with fp16 in the layout that the products read.
             constexpr int LANES = D / 16, PASSES = LANES, PER_PASS = 128 / LANES;
             const int tid = (int)threadIdx.x - 384, sub = tid % LANES, row0 = tid / LANES;
-            const float c = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
+            const float c = fabsf(a.scale_log2) * (C::Q_RANGE ? 1.0f / (1 << Q_LIFT) : 1.0f);
             float ks = 0.0f, vs = 0.0f;
             bool seen = false;
             // this thread's token's scales, on their way while the step before is converted

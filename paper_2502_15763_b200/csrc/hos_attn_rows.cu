@@ -241,8 +241,8 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
             }
             float mul = a.scale_log2;
             if (C::Q8 && !std::is_same<T, __half>::value) {
-                // bf16 queries meet fp16 keys: a power of two per row brings the row into fp16's range
-                // (exact but for elements 2^-38 of the row's largest)
+                // bf16 queries meet fp16 keys: a power of two per row brings the row into fp16's range.  Elements down to
+                // 2^-30 of the row's largest are exact, smaller ones rounded to within 2^-38 of it.
                 float top = 0.0f;
 #pragma unroll
                 for (int i2 = 0; i2 < 2 * KS; ++i2) {
@@ -252,7 +252,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
                 top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
                 const int ex = (int)(__float_as_uint(top) >> 23);            // biased; top >= 0
-                // top * 2^(140 - ex) is in [2^13, 2^14); rows of zeros, denormals or non-finite values stay
+                // top * 2^(140 - ex) is in [2^13, 2^14); rows of zeros, of nothing above 2^-100 and non-finite ones stay
                 const int sh = ex >= 27 && ex < 254 ? 140 - ex : 0;
                 const float up = __uint_as_float((uint32_t)(127 + sh) << 23);
                 mul *= __uint_as_float((uint32_t)(127 - sh) << 23);
