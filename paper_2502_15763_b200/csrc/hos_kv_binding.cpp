@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -29,8 +30,13 @@ struct Cache {
     hos_kv_cache c;
     at::ScalarType type;
     c10::DeviceIndex device;
-    int32_t* status;
-    int64_t status_len;
+    at::Tensor status;
+    cudaStream_t home;                           // that the status words were allocated on
+    int32_t* words(c10::cuda::CUDAStream st) const {
+        // their memory is not given to anyone else before a call on another stream is done with it
+        if (st.stream() != home) c10::cuda::CUDACachingAllocator::recordStream(status.storage().data_ptr(), st);
+        return status.mutable_data_ptr<int32_t>();
+    }
 };
 void drop(PyObject* capsule) { delete static_cast<Cache*>(PyCapsule_GetPointer(capsule, "hos.kv_cache")); }
 Cache* cache_of(PyObject* o) { return static_cast<Cache*>(PyCapsule_GetPointer(o, "hos.kv_cache")); }
@@ -132,20 +138,22 @@ PyObject* cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void* src = PyLong_AsVoidPtr(a[0]);
     const long device = PyLong_AsLong(a[1]);
     if (PyErr_Occurred()) return nullptr;
-    Cache* c = new Cache{*static_cast<const hos_kv_cache*>(src), at::kHalf, (c10::DeviceIndex)device, nullptr, 0};
+    Cache* c = new Cache{*static_cast<const hos_kv_cache*>(src), at::kHalf, (c10::DeviceIndex)device, at::Tensor(), nullptr};
     if (c->c.type == HOS_TYPE_BF16) c->type = at::kBFloat16;
     return PyCapsule_New(c, "hos.kv_cache", drop);
 }
 
-// set_status(handle, address, length)
+// set_status(handle, words): int32, allocated on the current stream
 PyObject* set_status(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!arity(n, 3)) return nullptr;
-    Cache* c = cache_of(a[0]);
-    if (!c) return nullptr;
-    c->status = static_cast<int32_t*>(PyLong_AsVoidPtr(a[1]));
-    c->status_len = PyLong_AsLongLong(a[2]);
-    if (PyErr_Occurred()) return nullptr;
-    Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        if (!arity(n, 2)) return nullptr;
+        Cache* c = cache_of(a[0]);
+        const at::Tensor* t = c ? tensor(a[1], "status") : nullptr;
+        if (!t) return nullptr;
+        c->status = *t;
+        c->home = c10::cuda::getCurrentCUDAStream(c->device).stream();
+        Py_RETURN_NONE;
+    });
 }
 
 // append(handle, k, v, tok_off, kv_len, page_table): error code
@@ -162,10 +170,11 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         hos_kv_batch b;
         if (!batch_of(c, a[3], a[4], a[5], k->size(0), k->size(0), &b)) return nullptr;
-        if (b.n_seq > c->status_len) return PyLong_FromLong(STATUS_TOO_SHORT);
+        if (b.n_seq > c->status.numel()) return PyLong_FromLong(STATUS_TOO_SHORT);
         const c10::cuda::CUDAGuard guard(c->device);
+        const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(c->device);
         return PyLong_FromLong(p_append(&c->c, &b, k->const_data_ptr(), v->const_data_ptr(), k->stride(0), k->stride(1), v->stride(0),
-                                        v->stride(1), c->status, c10::cuda::getCurrentCUDAStream(c->device).stream()));
+                                        v->stride(1), c->words(st), st.stream()));
     });
 }
 
@@ -183,7 +192,7 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         hos_kv_batch b;
         if (!batch_of(c, a[1], a[2], a[3], n_tok, n_tok, &b)) return nullptr;
-        if (b.n_seq > c->status_len) return Py_BuildValue("iOO", STATUS_TOO_SHORT, Py_None, Py_None);
+        if (b.n_seq > c->status.numel()) return Py_BuildValue("iOO", STATUS_TOO_SHORT, Py_None, Py_None);
         const c10::cuda::CUDAGuard guard(c->device);
         at::Tensor out[2];
         for (int i = 0; i < 2; ++i) {
@@ -199,8 +208,8 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
             }
             out[i] = *t;
         }
-        const int rc = p_read(&c->c, &b, out[0].mutable_data_ptr(), out[1].mutable_data_ptr(), c->status,
-                              c10::cuda::getCurrentCUDAStream(c->device).stream());
+        const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(c->device);
+        const int rc = p_read(&c->c, &b, out[0].mutable_data_ptr(), out[1].mutable_data_ptr(), c->words(st), st.stream());
         return Py_BuildValue("iNN", rc, THPVariable_Wrap(out[0]), THPVariable_Wrap(out[1]));
     });
 }
@@ -223,7 +232,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         hos_kv_batch b;
         if (!batch_of(c, a[2], a[3], a[4], q->size(0), max_new, &b)) return nullptr;
-        if (b.n_seq > c->status_len) return Py_BuildValue("iOO", STATUS_TOO_SHORT, Py_None, Py_None);
+        if (b.n_seq > c->status.numel()) return Py_BuildValue("iOO", STATUS_TOO_SHORT, Py_None, Py_None);
         const c10::cuda::CUDAGuard guard(c->device);
         at::Tensor out, lse, ws;
         if (a[10] == Py_None) {
@@ -251,9 +260,10 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         } else {
             ws = at::empty({need}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, c->device));
         }
+        const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(c->device);
         const int rc = p_attention(&c->c, &b, q->const_data_ptr(), q->stride(0), q->stride(1), heads, (float)scale, causal, (int)window,
                                    out.mutable_data_ptr(), out.stride(0), out.stride(1), want_lse ? lse.mutable_data_ptr<float>() : nullptr,
-                                   c->status, ws.mutable_data_ptr(), (size_t)ws.numel(), c10::cuda::getCurrentCUDAStream(c->device).stream());
+                                   c->words(st), ws.mutable_data_ptr(), (size_t)ws.numel(), st.stream());
         return Py_BuildValue("iNN", rc, THPVariable_Wrap(out), want_lse ? THPVariable_Wrap(lse) : Py_NewRef(Py_None));
     });
 }

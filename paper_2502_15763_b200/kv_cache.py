@@ -51,8 +51,9 @@ class _KvBatch(C.Structure):
 class KvCache:
     """Handle of a paged cache: its tensors, checked, and the C description of them.
 
-    `status` (int32, one word per sequence of the largest batch so far) collects the HOS_ST_* bits of the
-    calls made with this handle until `status.zero_()`."""
+    `status` (int32, one word per sequence of the largest batch so far, 1,024 or the number of pages at least)
+    collects the HOS_ST_* bits of the calls made with this handle until `status.zero_()`, on whatever streams and
+    in whatever graphs they run."""
 
     def __init__(self, k, v, k_scale, v_scale, dtype):
         torch = _torch()
@@ -90,7 +91,7 @@ class KvCache:
             raise ValueError("scales belong to an 8-bit cache")
         self.k, self.v, self.k_scale, self.v_scale, self.dtype = k, v, k_scale, v_scale, dtype
         self.n_kv_heads, self.page_size, self.head_dim, self.device = n_kv, page, dim, k.device
-        self.status, self._earlier = torch.zeros((256,), dtype=torch.int32, device=k.device), []
+        self._earlier = []                 # shorter words, which calls in flight and captured graphs may still write to
         # a page's stride means nothing where there is one page
         dense = n_kv * page * dim
         self._c = _KvCache(n_pages, page, n_kv, dim, types[dtype], self.format, k.data_ptr(), v.data_ptr(),
@@ -98,15 +99,32 @@ class KvCache:
                            v_scale.data_ptr() if v_scale is not None else None,
                            k.stride(0) if n_pages > 1 else dense, scale_stride if n_pages > 1 else 0)
         self._h = binding().cache(C.addressof(self._c), k.get_device())
-        binding().set_status(self._h, self.status.data_ptr(), self.status.shape[0])
+        self._new_status(max(1024, n_pages))
+
+    def _new_status(self, n):
+        torch = _torch()
+        self._status = torch.zeros((n,), dtype=torch.int32, device=self.device)
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()      # calls on other streams find zeros
+        binding().set_status(self._h, self._status)
 
     def _grow_status(self, n_seq):
-        # the earlier words stay allocated: calls in flight, and captured graphs, write to them
-        old = self.status
-        self._earlier.append(old)
-        self.status = old.new_zeros((max(2 * n_seq, 256),))
-        self.status[:old.shape[0]] = old
-        binding().set_status(self._h, self.status.data_ptr(), self.status.shape[0])
+        if _torch().cuda.is_current_stream_capturing():               # words made here would be zeroed by every replay
+            raise RuntimeError(f"{n_seq} sequences, status words for {self._status.shape[0]}: "
+                               "make a call with the largest batch before a graph is captured")
+        self._earlier.append(self._status)
+        self._new_status(2 * n_seq)
+
+    @property
+    def status(self):
+        if self._earlier:
+            torch = _torch()
+            torch.cuda.synchronize(self.device)
+            for old in self._earlier:
+                self._status[:old.shape[0]] |= old
+                old.zero_()
+            torch.cuda.synchronize(self.device)
+        return self._status
 
 
 def hos_kv_cache(k, v, k_scale=None, v_scale=None, dtype=None) -> KvCache:
@@ -125,7 +143,7 @@ def hos_kv_append(cache: KvCache, k, v, tok_off, kv_len, page_table):
         rc = _append(cache._h, k, v, tok_off, kv_len, page_table)
     if rc:
         raise HosError(rc, "hos_kv_append")
-    return {"status": cache.status}
+    return {"status": cache._status}
 
 
 def hos_kv_read(cache: KvCache, tok_off, kv_len, page_table, n_tokens: int, out=None):
@@ -138,7 +156,7 @@ def hos_kv_read(cache: KvCache, tok_off, kv_len, page_table, n_tokens: int, out=
         rc, k, v = _read(cache._h, tok_off, kv_len, page_table, n_tokens, ok, ov)
     if rc:
         raise HosError(rc, "hos_kv_read")
-    return {"k": k, "v": v, "status": cache.status}
+    return {"k": k, "v": v, "status": cache._status}
 
 
 def hos_paged_attention(q, cache: KvCache, tok_off, kv_len, page_table, max_new: int, sm_scale=None, causal: bool = True,
@@ -155,4 +173,4 @@ def hos_paged_attention(q, cache: KvCache, tok_off, kv_len, page_table, max_new:
         rc, o, lse = _attention(cache._h, q, tok_off, kv_len, page_table, max_new, sm_scale, causal, window, want_lse, out, ws)
     if rc:
         raise HosError(rc, "hos_paged_attention")
-    return {"out": o, "lse": lse, "status": cache.status}
+    return {"out": o, "lse": lse, "status": cache._status}
