@@ -101,6 +101,10 @@ const at::Tensor* rows(const Cache* c, PyObject* o, const char* what) {
     return t;
 }
 
+// Strides of a [tokens][heads][head_dim] tensor.  Those of a single token or head mean nothing (and torch leaves anything there).
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
+int64_t head_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : t.size(2); }
+
 bool arity(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return true;
     PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
@@ -173,8 +177,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (b.n_seq > c->status.numel()) return PyLong_FromLong(STATUS_TOO_SHORT);
         const c10::cuda::CUDAGuard guard(c->device);
         const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(c->device);
-        return PyLong_FromLong(p_append(&c->c, &b, k->const_data_ptr(), v->const_data_ptr(), k->stride(0), k->stride(1), v->stride(0),
-                                        v->stride(1), c->words(st), st.stream()));
+        return PyLong_FromLong(p_append(&c->c, &b, k->const_data_ptr(), v->const_data_ptr(), token_stride(*k), head_stride(*k),
+                                        token_stride(*v), head_stride(*v), c->words(st), st.stream()));
     });
 }
 
@@ -261,8 +265,8 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
             ws = at::empty({need}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, c->device));
         }
         const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(c->device);
-        const int rc = p_attention(&c->c, &b, q->const_data_ptr(), q->stride(0), q->stride(1), heads, (float)scale, causal, (int)window,
-                                   out.mutable_data_ptr(), out.stride(0), out.stride(1), want_lse ? lse.mutable_data_ptr<float>() : nullptr,
+        const int rc = p_attention(&c->c, &b, q->const_data_ptr(), token_stride(*q), head_stride(*q), heads, (float)scale, causal, (int)window,
+                                   out.mutable_data_ptr(), token_stride(out), head_stride(out), want_lse ? lse.mutable_data_ptr<float>() : nullptr,
                                    c->words(st), ws.mutable_data_ptr(), (size_t)ws.numel(), st.stream());
         return Py_BuildValue("iNN", rc, THPVariable_Wrap(out), want_lse ? THPVariable_Wrap(lse) : Py_NewRef(Py_None));
     });

@@ -48,6 +48,11 @@ class _KvBatch(C.Structure):
                 ("tok_off", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64)]
 
 
+def _strided(t, want):
+    """Whether t has these strides; that of a dimension of one means nothing."""
+    return all(n == 1 or s == w for n, s, w in zip(t.shape[1:], t.stride()[1:], want))
+
+
 class KvCache:
     """Handle of a paged cache: its tensors, checked, and the C description of them.
 
@@ -62,7 +67,7 @@ class KvCache:
         for t, what in ((k, "k"), (v, "v")):
             if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4):
                 raise TypeError(f"{what}: expected a CUDA tensor [n_pages][n_kv_heads][page_size][head_dim]")
-        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride() != k.stride():
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or (k.shape[0] > 1 and v.stride(0) != k.stride(0)):
             raise ValueError("k and v must agree in shape, type, device and strides")
         self.format = formats.get(k.dtype, HOS_KV_SAME)
         dtype = dtype if dtype is not None else k.dtype
@@ -71,7 +76,7 @@ class KvCache:
         if self.format == HOS_KV_SAME and k.dtype != dtype:
             raise TypeError(f"k, v: expected {dtype}, float8_e4m3fn or int8")
         n_pages, n_kv, page, dim = k.shape
-        if tuple(k.stride()[1:]) != (page * dim, dim, 1):
+        if not (_strided(k, (page * dim, dim, 1)) and _strided(v, (page * dim, dim, 1))):
             raise ValueError("k, v: only the pages may be strided")
         if n_pages > 1 and k.stride(0) < n_kv * page * dim:      # 0, an expanded page, would mean densely packed pages below
             raise ValueError("k, v: pages must not overlap")
@@ -80,9 +85,9 @@ class KvCache:
             for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
                 if not (isinstance(t, torch.Tensor) and t.device == k.device and t.dtype == torch.float32):
                     raise TypeError(f"{what}: expected a CUDA tensor of float32")
-                if tuple(t.shape) != (n_pages, n_kv, page) or tuple(t.stride()[1:]) != (page, 1):
+                if tuple(t.shape) != (n_pages, n_kv, page) or not _strided(t, (page, 1)):
                     raise ValueError(f"{what}: expected [n_pages][n_kv_heads][page_size], strided by pages only")
-            if k_scale.stride(0) != v_scale.stride(0):
+            if n_pages > 1 and k_scale.stride(0) != v_scale.stride(0):
                 raise ValueError("k_scale and v_scale must have the same strides")
             if n_pages > 1 and k_scale.stride(0) < n_kv * page:
                 raise ValueError("k_scale, v_scale: pages must not overlap")

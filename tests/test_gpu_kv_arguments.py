@@ -29,3 +29,49 @@ def test_pages_that_overlap_are_refused():
         h.hos_kv_cache(k, v, ks[:1].expand(4, -1, -1), vs[:1].expand(4, -1, -1), dtype=torch.bfloat16)
     # one page has no neighbour to overlap with
     h.hos_kv_cache(same[:1].expand(1, -1, -1, -1), same_v[:1])
+
+
+def odd_strides(x, tok, head):
+    """x [tokens][heads][d] with these strides, in a buffer of its own that begins on 16 bytes."""
+    buf = torch.full(((x.shape[0] - 1) * tok + (x.shape[1] - 1) * head + x.shape[2] + 64,), 7.0, dtype=x.dtype, device=x.device)
+    y = buf.as_strided(x.shape, (tok, head, 1))
+    y.copy_(x)
+    return y
+
+
+@pytest.mark.parametrize("n,heads,kv_heads,tok,head", [(1, 4, 4, 259, 64), (1, 1, 1, 1, 3), (5, 1, 1, 72, 5), (30, 1, 1, 64, 1), (1, 8, 2, 13, 72)])
+def test_strides_of_a_single_token_or_head_mean_nothing(n, heads, kv_heads, tok, head):
+    h = hos()
+    d, page, t, dt = 64, 16, 50, torch.bfloat16
+    off, kv_len, table, n_pages = R.make_batch([(n, t)], page, 1, 1)
+    k, v, ks, vs = make_cache(n_pages, kv_heads, page, d, dt, "int8", 2)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, nk, nv = (torch.randn((n, hd, d), generator=g, device="cuda").to(dt) for hd in (heads, kv_heads, kv_heads))
+
+    def step(odd):
+        cache = h.hos_kv_cache(*(x.clone() for x in (k, v, ks, vs)), dtype=dt)
+        a, b, c = (odd_strides(x, tok, head) if odd and x.shape[1] == q.shape[1] else x for x in (q, nk, nv))
+        out = odd_strides(torch.zeros_like(q), tok, head) if odd else None
+        h.hos_kv_append(cache, b, c, off, kv_len, table)
+        r = h.hos_paged_attention(a, cache, off, kv_len, table, n, out=out)
+        torch.cuda.synchronize()
+        assert int(cache.status.abs().sum()) == 0
+        return r["out"], cache
+    want, c1 = step(False)
+    got, c2 = step(True)
+    assert torch.equal(got, want) and torch.equal(c1.k, c2.k) and torch.equal(c1.v_scale, c2.v_scale)
+
+
+@pytest.mark.parametrize("fmt", ["same", "e4m3"])
+def test_strides_of_a_single_kv_head_or_page_mean_nothing(fmt):
+    h = hos()
+    for n_pages, strides, s_strides in ((4, (1024, 13, 64, 1), (16, 3, 1)), (1, (5, 1024, 64, 1), (9, 16, 1)), (1, (3, 1, 64, 1), (1, 1, 1))):
+        k, v, ks, vs = make_cache(n_pages, 1, 16, 64, torch.float16, fmt, 2)
+        off, kv_len, table, _ = R.make_batch([(1, 16 * n_pages - 2)], 16, 0, 1)
+        table.clamp_(0, n_pages - 1)
+        q = torch.randn((1, 2, 64), device="cuda").half()
+        want = h.hos_paged_attention(q, h.hos_kv_cache(k, v, ks, vs, dtype=torch.float16), off, kv_len, table, 1)["out"]
+        odd = h.hos_kv_cache(k.as_strided(k.shape, strides), v, None if ks is None else ks.as_strided(ks.shape, s_strides), vs, dtype=torch.float16)
+        got = h.hos_paged_attention(q, odd, off, kv_len, table, 1)["out"]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
