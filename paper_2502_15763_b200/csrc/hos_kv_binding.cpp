@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -96,6 +97,10 @@ const at::Tensor* rows(const Cache* c, PyObject* o, const char* what) {
     }
     if (t->stride(2) != 1) {
         PyErr_Format(PyExc_ValueError, "%s: the elements of a head must be dense", what);
+        return nullptr;
+    }
+    if (t->requires_grad() && c10::GradMode::is_enabled()) {     // the results would carry no graph
+        PyErr_Format(PyExc_ValueError, "%s requires grad, and there is no backward pass: detach it, or call under torch.no_grad()", what);
         return nullptr;
     }
     return t;

@@ -75,3 +75,23 @@ def test_strides_of_a_single_kv_head_or_page_mean_nothing(fmt):
         got = h.hos_paged_attention(q, odd, off, kv_len, table, 1)["out"]
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_tensors_that_require_grad():
+    """There is no backward pass: with gradients on they are refused instead of answered without a graph."""
+    h = hos()
+    off, kv_len, table, n_pages = R.make_batch([(2, 20)], 16, 0, 1)
+    cache = h.hos_kv_cache(*make_cache(n_pages, 2, 16, 64, torch.bfloat16, "same", 2))
+    q, k, v = (torch.randn((2, n, 64), device="cuda").bfloat16() for n in (4, 2, 2))
+    want = h.hos_paged_attention(q, cache, off, kv_len, table, 2)["out"]
+    g = q.clone().requires_grad_()
+    with pytest.raises(ValueError, match="q requires grad"):
+        h.hos_paged_attention(g, cache, off, kv_len, table, 2)
+    with pytest.raises(ValueError, match="k requires grad"):
+        h.hos_kv_append(cache, k.clone().requires_grad_(), v, off, kv_len, table)
+    with pytest.raises(ValueError, match="v requires grad"):
+        h.hos_kv_append(cache, k, v.clone().requires_grad_() * 1, off, kv_len, table)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            assert torch.equal(h.hos_paged_attention(g, cache, off, kv_len, table, 2)["out"], want)
+    assert torch.equal(h.hos_paged_attention(g.detach(), cache, off, kv_len, table, 2)["out"], want)
