@@ -113,8 +113,14 @@ int hos_kv_read(const hos_kv_cache* c, const hos_kv_batch* b, void* k, void* v, 
     int rc = check_cache(c);
     if (rc) return rc;
     if ((rc = check_kv_batch(c, b))) return rc;
-    if (b->n_seq == 0 || b->n_tokens == 0) return HOS_OK;
+    if (b->n_tokens == 0) return HOS_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return HOS_E_INVALID;
+    if (b->n_seq == 0) {                              // tokens of no sequence have no place, and read as zero
+        const size_t bytes = (size_t)b->n_tokens * c->n_kv_heads * c->head_dim * 2;
+        for (void* p : {k, v})
+            if ((rc = cuda_rc(cudaMemsetAsync(p, 0, bytes, static_cast<cudaStream_t>(stream))))) return rc;
+        return HOS_OK;
+    }
     return cuda_rc(launch_kv_read(view(c, b, status), c->type, c->format, k, v, static_cast<cudaStream_t>(stream)));
 }
 

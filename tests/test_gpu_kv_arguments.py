@@ -95,3 +95,19 @@ def test_tensors_that_require_grad():
         with mode():
             assert torch.equal(h.hos_paged_attention(g, cache, off, kv_len, table, 2)["out"], want)
     assert torch.equal(h.hos_paged_attention(g.detach(), cache, off, kv_len, table, 2)["out"], want)
+
+
+def test_tokens_of_no_sequence_read_as_zero():
+    h = hos()
+    for d, fmt in ((64, "same"), (128, "int8")):
+        cache = h.hos_kv_cache(*make_cache(3, 2, 16, d, torch.float16, fmt, 2), dtype=torch.float16)
+        empty = [torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((1,), (0,), (0, 2))]
+        out = [torch.full((7, 2, d), 5.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+        r = h.hos_kv_read(cache, *empty, 7, out=out)
+        assert bool((r["k"] == 0).all()) and bool((r["v"] == 0).all())
+        # a batch whose sequences begin after the first token and end before the last
+        off = torch.tensor([2, 4], dtype=torch.int32, device="cuda")
+        kv_len, table = torch.tensor([20], dtype=torch.int32, device="cuda"), torch.tensor([[2, 0]], dtype=torch.int32, device="cuda")
+        r = h.hos_kv_read(cache, off, kv_len, table, 7, out=[t.fill_(5.0) for t in out])
+        for x in (r["k"], r["v"]):
+            assert bool((x[[0, 1, 4, 5, 6]] == 0).all()) and bool((x[2:4] != 0).any())
