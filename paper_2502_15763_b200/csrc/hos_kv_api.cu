@@ -64,7 +64,12 @@ KvView view(const hos_kv_cache* c, const hos_kv_batch* b, int32_t* status) {
     return v;
 }
 
-inline int cuda_rc(cudaError_t e) { return e == cudaSuccess ? HOS_OK : HOS_E_CUDA; }
+// An error is reported once: the runtime would hand it to the next call that asks for its last one, too.
+inline int cuda_rc(cudaError_t e) {
+    if (e == cudaSuccess) return HOS_OK;
+    cudaGetLastError();
+    return HOS_E_CUDA;
+}
 
 struct AttnSpace {
     AttnWs rows, chunks;
@@ -103,6 +108,7 @@ int hos_kv_append(const hos_kv_cache* c, const hos_kv_batch* b, const void* k, c
     if ((rc = check_kv_batch(c, b))) return rc;
     if (b->n_seq == 0 || b->n_tokens == 0) return HOS_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return HOS_E_INVALID;
+    if (c->n_kv_heads > KV_MOST_HEADS) return HOS_E_UNSUPPORTED;
     const long long st[4] = {k_tok_stride, k_head_stride, v_tok_stride, v_head_stride};
     for (long long s : st)
         if (!multiple16(s, 2)) return HOS_E_INVALID;
@@ -115,6 +121,7 @@ int hos_kv_read(const hos_kv_cache* c, const hos_kv_batch* b, void* k, void* v, 
     if ((rc = check_kv_batch(c, b))) return rc;
     if (b->n_tokens == 0) return HOS_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return HOS_E_INVALID;
+    if (c->n_kv_heads > KV_MOST_HEADS) return HOS_E_UNSUPPORTED;
     if (b->n_seq == 0) {                              // tokens of no sequence have no place, and read as zero
         const size_t bytes = (size_t)b->n_tokens * c->n_kv_heads * c->head_dim * 2;
         for (void* p : {k, v})

@@ -16,7 +16,7 @@
 namespace hos {
 namespace {
 
-constexpr int WARPS = 8, MOST_TOKENS = 16, APPEND_TOKENS = 4, MOST_HEADS = 16;
+constexpr int WARPS = 8, MOST_TOKENS = 16, APPEND_TOKENS = 4, MOST_HEADS = KV_HEADS_A_BLOCK;
 // Vectors that a thread has on the way at once; blocks an SM.  Few and many: reading 31,896 tokens of 64 int8 heads (1.6 GB) takes
 // 331 us with 4 vectors and 4 blocks, 305 with 2 and 5, 265 with 1 and 7; appending 6,634 tokens of 64 heads as e4m3 (329 MB)
 // took 66, 62 and 63 us (62 with the magnitudes compared two at a time and the final shape).

@@ -33,6 +33,8 @@ struct AttnWs {
     RowState* state;
     float* part;
 };
+// Append and read take up to 16 heads a block, and a grid's second dimension ends at 65,535.
+constexpr int KV_HEADS_A_BLOCK = 16, KV_MOST_HEADS = 65535 * KV_HEADS_A_BLOCK;
 cudaError_t launch_kv_append(const KvView& c, int type, int format, const void* k, const void* v,
                              const long long (&strides)[4], cudaStream_t st);
 cudaError_t launch_kv_read(const KvView& c, int type, int format, void* k, void* v, cudaStream_t st);
