@@ -65,27 +65,34 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
 
 # The Python module behind kv_cache.py: host code only, against the interpreter's and torch's headers.
 BINDING_SOURCE = os.path.join(CSRC, "hos_kv_binding.cpp")
-BINDING_PATH = os.path.join(_PKG, "_kv.so")
+
+
+def binding_path() -> str:
+    """Where the module for this interpreter and torch is: one built against other headers is never loaded."""
+    import importlib.metadata
+    import sysconfig
+    return os.path.join(_PKG, f"_kv.torch-{importlib.metadata.version('torch')}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
 
 def build_binding(force: bool = False) -> str:
-    """Compile hos_kv_binding.cpp into _kv.so; returns its path."""
+    """Compile hos_kv_binding.cpp into the module of binding_path(); returns that."""
+    path = binding_path()
     newest = max(os.path.getmtime(f) for f in (BINDING_SOURCE, os.path.join(INCLUDE, "hos.h")))
-    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= newest:
-        return BINDING_PATH
+    if not force and os.path.exists(path) and os.path.getmtime(path) >= newest:
+        return path
     import sysconfig
 
     import torch
     home = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
-    tmp = BINDING_PATH + f".{os.getpid()}.tmp"
+    tmp = path + f".{os.getpid()}.tmp"
     subprocess.check_call([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-I", INCLUDE,
                            "-isystem", home + "/include", "-isystem", home + "/include/torch/csrc/api/include",
                            "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda + "/include",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", tmp, BINDING_SOURCE,
                            "-L" + home + "/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
-    os.replace(tmp, BINDING_PATH)
-    return BINDING_PATH
+    os.replace(tmp, path)
+    return path
 
 
 if __name__ == "__main__":

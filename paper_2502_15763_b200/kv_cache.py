@@ -21,7 +21,7 @@ _binding = _append = _read = _attention = None
 
 
 def binding():
-    """The compiled half of this module (_kv.so, built first if its source is newer), tied to the loaded library."""
+    """The compiled half of this module (_kv, built first if its source is newer), tied to the loaded library."""
     global _binding, _append, _read, _attention
     if _binding is None:
         from . import _build
