@@ -253,6 +253,10 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                 PyErr_SetString(PyExc_ValueError, "out must have the shape of q");
                 return nullptr;
             }
+            if ((t->size(0) > 1 && t->stride(0) == 0) || (t->size(1) > 1 && t->stride(1) == 0)) {
+                PyErr_SetString(PyExc_ValueError, "out: several rows in one place (an expanded tensor)");
+                return nullptr;
+            }
             out = *t;
         }
         const int heads = (int)q->size(1);

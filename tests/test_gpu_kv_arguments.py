@@ -111,3 +111,20 @@ def test_tokens_of_no_sequence_read_as_zero():
         r = h.hos_kv_read(cache, off, kv_len, table, 7, out=[t.fill_(5.0) for t in out])
         for x in (r["k"], r["v"]):
             assert bool((x[[0, 1, 4, 5, 6]] == 0).all()) and bool((x[2:4] != 0).any())
+
+
+def test_an_expanded_output_is_refused():
+    """Its rows would be written to one place by several blocks at once; the check comes before any launch."""
+    h = hos()
+    off, kv_len, table, n_pages = R.make_batch([(2, 20)], 16, 0, 1)
+    cache = h.hos_kv_cache(*make_cache(n_pages, 2, 16, 64, torch.bfloat16, "same", 2))
+    q = torch.randn((2, 4, 64), device="cuda").bfloat16()
+    for out in (torch.zeros_like(q[:1]).expand(2, 4, 64), torch.zeros_like(q[:, :1]).expand(2, 4, 64)):
+        with pytest.raises(ValueError, match="expanded"):
+            h.hos_paged_attention(q, cache, off, kv_len, table, 2, out=out)
+    one = torch.zeros((1, 1, 64), dtype=q.dtype, device="cuda").expand(1, 4, 64)
+    with pytest.raises(ValueError, match="expanded"):
+        h.hos_paged_attention(q[:1], cache, off, kv_len, table, 2, out=one)
+    wide = q[:1].expand(2, 4, 64)                                # an expanded query is fine
+    got = h.hos_paged_attention(wide, cache, off, kv_len, table, 2)["out"]
+    assert torch.equal(got, h.hos_paged_attention(wide.contiguous(), cache, off, kv_len, table, 2)["out"])
