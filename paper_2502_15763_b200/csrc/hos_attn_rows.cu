@@ -578,7 +578,7 @@ cudaError_t run(const AttnView& a, int max_rows, bool beside, const AttnWs& ws, 
     static_assert(C::CTAS <= ATTN_WORKERS_PER_SM && C::CTAS * C::ROWS <= ATTN_ROWS_PER_SM && C::STAGES >= 2, "");
     cudaError_t e = allow_max_dynamic_smem(reinterpret_cast<const void*>(&k_attn_rows<T, FMT, D, NB>));
     if (e != cudaSuccess) return e;
-    const int ctas = 148 * C::CTAS;
+    const int ctas = ATTN_SMS * C::CTAS;
     *workers = ctas;
     launch_hook("k_attn_rows", 0, st);
     e = launch_early(k_attn_rows<T, FMT, D, NB>, dim3((unsigned)ctas), WARPS * 32, C::SMEM, st, a, max_rows, beside, ws.meta, ws.state, ws.part);
