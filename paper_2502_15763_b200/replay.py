@@ -86,8 +86,8 @@ def replay(p, o, recs, queue, batch_cap, kv_budget, heads=64, kv_heads=8, head_d
     cache = hos_kv_cache(k, v, ks, vs, dtype=dt)
     pool, running, most_pages = PagePool(n_pages, page), [], 0          # running: [request, tokens in the cache, steps left, pages]
     gen = torch.Generator(device="cuda").manual_seed(seed)
-    longest = int(max(p[queue]))
-    qkv = torch.randn((max(batch_cap, 1) * longest if len(queue) else 1, heads + 2 * kv_heads, head_dim), generator=gen, device="cuda", dtype=dt)
+    longest = int(p[queue].max()) if len(queue) else 1
+    qkv = torch.randn((max(batch_cap, 1) * longest, heads + 2 * kv_heads, head_dim), generator=gen, device="cuda", dtype=dt)
     us, out = [], []
     for it, rec in enumerate(recs if max_iters is None else recs[:max_iters]):
         prefill = bool(rec["kind_n"] >> 31)
@@ -130,8 +130,8 @@ def replay(p, o, recs, queue, batch_cap, kv_budget, heads=64, kv_heads=8, head_d
     torch.cuda.synchronize()
     if int(cache.status.abs().sum()):
         raise RuntimeError("the cache calls reported a problem: status bits set")
-    kind, n, tokens = (np.array(c) for c in zip(*out))
-    return dict(prefill=kind.astype(bool), n=n, tokens=tokens, us=np.array(us), most_pages=most_pages, n_pages=n_pages)
+    kind, n, tokens = np.array(out, dtype=np.int64).reshape(-1, 3).T
+    return dict(prefill=kind.astype(bool), n=n, tokens=tokens, us=np.array(us, dtype=float), most_pages=most_pages, n_pages=n_pages)
 
 
 def fit(r, layers):

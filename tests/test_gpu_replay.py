@@ -37,3 +37,21 @@ def test_replay_notices_a_wrong_trace():
     recs["tokens"][5] += 1
     with pytest.raises(RuntimeError, match="iteration 5"):
         R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=2, kv_heads=1, head_dim=64, fmt="same", max_iters=10, repeat=0)
+
+
+def test_a_client_without_requests():
+    """Nothing to run is no error: empty arrays, no fit."""
+    from paper_2502_15763_b200 import ITER_REC_DTYPE, replay as R
+    from workload import workload
+    w = workload("c0")
+    p, o = (x[0] for x in w.lengths())
+    none = np.zeros(0, dtype=ITER_REC_DTYPE)
+    for queue, most in ((np.zeros(0, dtype=np.int64), None), (np.arange(3), 0)):
+        r = R.replay(p, o, none, queue, w.batch_cap, w.kv_budget, heads=2, kv_heads=1, head_dim=64, fmt="same", max_iters=most, repeat=0)
+        assert len(r["us"]) == len(r["n"]) == len(r["tokens"]) == 0 and r["most_pages"] == 0
+        f = R.fit(r, 80)
+        assert f["iterations"] == 0 and f["median_decode_us"] is None and "decode_kv_div" not in f
+    # a workload of one request on four clients leaves three of them without any
+    recs, queue = R.client_schedule(p[:1], o[:1], w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 3)
+    r = R.replay(p[:1], o[:1], recs, queue, w.batch_cap, w.kv_budget, heads=2, kv_heads=1, head_dim=64, fmt="same", repeat=0)
+    assert len(r["us"]) == len(recs)
