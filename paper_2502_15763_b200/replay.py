@@ -5,8 +5,9 @@ The scheduler's cost model has a term in the prompt tokens of a prefill and one 
 workload (offline packing, online simulation), takes the iteration trace of one client, and runs every iteration's KV
 work for real: requests are admitted into a paged cache, their prompts' keys and values are appended and attended to in one
 ragged call, decode rounds append and attend with one token per running request, retired requests give their pages back.
-Every iteration is held against its trace record and timed (the two calls as a graph of several repetitions: they write the
-same places again, and the host's side stays out of the figures), and the times are fitted by least squares.
+Every iteration is held against its trace record and timed (the two calls as a graph of several layers, each with a cache of its
+own as in a model, so that a layer's keys and values come from memory and not from what the layer before left on the chip; the
+host's side stays out of the figures), and the times are fitted by least squares.
 
     python -m paper_2502_15763_b200.replay --workload c0 --client 0 --heads 64 --kv-heads 8 --format int8 --layers 80
 """
@@ -54,13 +55,13 @@ class PagePool:
         self.free.extend(pages)
 
 
-def device_us(step, repeat):
-    """Device time of one `step`, from a graph of `repeat` of them."""
+def device_us(steps):
+    """Device time of one of `steps`, from a graph of them."""
     import torch
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        for _ in range(repeat):
+        for step in steps:
             step()
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     graph.replay()
@@ -68,22 +69,34 @@ def device_us(step, repeat):
     graph.replay()
     end.record()
     torch.cuda.synchronize()
-    return start.elapsed_time(end) * 1000.0 / repeat
+    return start.elapsed_time(end) * 1000.0 / len(steps)
+
+
+def cache_bytes(batch_cap, kv_budget, kv_heads, head_dim, page, fmt):
+    """Memory of one layer's cache in replay()."""
+    vector = 2 * head_dim if fmt == "same" else head_dim + 4
+    return 2 * (-(-kv_budget // page) + batch_cap) * kv_heads * page * vector
 
 
 def replay(p, o, recs, queue, batch_cap, kv_budget, heads=64, kv_heads=8, head_dim=128, page=128, fmt="int8", max_iters=None,
-           repeat=8, seed=0):
+           repeat=8, seed=0, watch=None):
     """Runs the records' KV work; returns per-iteration arrays (kind, n, tokens, us) and the pages' high-water mark.  The times
-    are device times of one of `repeat` repetitions; repeat = 0 runs every iteration once, untimed."""
+    are device times of one of `repeat` layers, each with a cache of its own (of the same pages); repeat = 0 runs every
+    iteration once, untimed.  watch(iteration, requests, x, cache, tok_off, kv_len, page_table, out): called after each
+    iteration with what one layer got ([token][queries, keys, values]) and gave."""
     import torch
     dt = torch.bfloat16
     # every running request may leave one page part empty
     n_pages = -(-kv_budget // page) + batch_cap
     shape = (n_pages, kv_heads, page, head_dim)
     store = {"same": dt, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[fmt]
-    k, v = (torch.zeros(shape, dtype=torch.uint8 if fmt != "same" else dt, device="cuda").view(store) for _ in range(2))
-    ks, vs = (torch.zeros(shape[:3], device="cuda") if fmt != "same" else None for _ in range(2))
-    cache = hos_kv_cache(k, v, ks, vs, dtype=dt)
+
+    def layer():
+        k, v = (torch.zeros(shape, dtype=torch.uint8 if fmt != "same" else dt, device="cuda").view(store) for _ in range(2))
+        ks, vs = (torch.zeros(shape[:3], device="cuda") if fmt != "same" else None for _ in range(2))
+        return hos_kv_cache(k, v, ks, vs, dtype=dt)
+
+    caches = [layer() for _ in range(max(repeat, 1))]
     pool, running, most_pages = PagePool(n_pages, page), [], 0          # running: [request, tokens in the cache, steps left, pages]
     gen = torch.Generator(device="cuda").manual_seed(seed)
     longest = int(p[queue].max()) if len(queue) else 1
@@ -113,12 +126,14 @@ def replay(p, o, recs, queue, batch_cap, kv_budget, heads=64, kv_heads=8, head_d
         kv_len = torch.tensor([b[1] for b in batch], dtype=torch.int32).cuda()
         x = qkv[:sum(new)]
 
-        def step():
+        def step(cache=caches[0]):
             hos_kv_append(cache, x[:, heads:heads + kv_heads], x[:, heads + kv_heads:], off, kv_len, table)
-            hos_paged_attention(x[:, :heads], cache, off, kv_len, table, max(new))
+            return hos_paged_attention(x[:, :heads], cache, off, kv_len, table, max(new))["out"]
 
-        step()
-        us.append(device_us(step, repeat) if repeat else 0.0)
+        got = step()
+        us.append(device_us([lambda c=c: step(c) for c in caches]) if repeat else 0.0)
+        if watch is not None:
+            watch(it, [b[0] for b in batch], x, caches[0], off, kv_len, table, got)
         out.append((prefill, n, seen))
         if not prefill:
             done = [b for b in running if (b.__setitem__(2, b[2] - 1) or b[2] == 0)]
@@ -128,7 +143,7 @@ def replay(p, o, recs, queue, batch_cap, kv_budget, heads=64, kv_heads=8, head_d
                 pool.give(b[3])
             running = [b for b in running if b[2] > 0]
     torch.cuda.synchronize()
-    if int(cache.status.abs().sum()):
+    if any(int(c.status.abs().sum()) for c in caches):
         raise RuntimeError("the cache calls reported a problem: status bits set")
     kind, n, tokens = np.array(out, dtype=np.int64).reshape(-1, 3).T
     return dict(prefill=kind.astype(bool), n=n, tokens=tokens, us=np.array(us, dtype=float), most_pages=most_pages, n_pages=n_pages)
@@ -155,6 +170,7 @@ def fit(r, layers):
 
 
 def main(argv=None):
+    import torch
     from workload import workload
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--workload", default="c0")
@@ -165,14 +181,16 @@ def main(argv=None):
     ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--page", type=int, default=128)
     ap.add_argument("--format", default="int8", choices=("same", "e4m3", "int8"))
-    ap.add_argument("--layers", type=int, default=80)
+    ap.add_argument("--layers", type=int, default=80, help="layers of the model; as many as fit are run and timed")
     ap.add_argument("--iters", type=int, default=None)
     a = ap.parse_args(argv)
     w = workload(a.workload).subset(a.instance, 1)
     p, o = (x[0] for x in w.lengths())
     recs, queue = client_schedule(p, o, w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, a.client)
-    r = replay(p, o, recs, queue, w.batch_cap, w.kv_budget, a.heads, a.kv_heads, a.head_dim, a.page, a.format, a.iters)
-    print(json.dumps({"workload": a.workload, "client": a.client, "layers": a.layers, **fit(r, a.layers)}))
+    one = cache_bytes(w.batch_cap, w.kv_budget, a.kv_heads, a.head_dim, a.page, a.format)
+    run = max(1, min(a.layers, int(0.6 * torch.cuda.mem_get_info()[0]) // one))
+    r = replay(p, o, recs, queue, w.batch_cap, w.kv_budget, a.heads, a.kv_heads, a.head_dim, a.page, a.format, a.iters, repeat=run)
+    print(json.dumps({"workload": a.workload, "client": a.client, "layers": a.layers, "layers_run": run, **fit(r, a.layers)}))
 
 
 if __name__ == "__main__":

@@ -55,3 +55,28 @@ def test_a_client_without_requests():
     recs, queue = R.client_schedule(p[:1], o[:1], w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 3)
     r = R.replay(p[:1], o[:1], recs, queue, w.batch_cap, w.kv_budget, heads=2, kv_heads=1, head_dim=64, fmt="same", repeat=0)
     assert len(r["us"]) == len(recs)
+
+
+@pytest.mark.parametrize("fmt", ["same", "int8"])
+def test_every_timed_layer_has_a_cache_of_its_own(fmt, monkeypatch):
+    """The layers of a timed iteration must not find each other's keys and values on the chip; all of them hold the same."""
+    import torch
+    from paper_2502_15763_b200 import replay as R
+    from workload import workload
+    made, make = [], R.hos_kv_cache
+
+    def recorded(*args, **kw):
+        made.append(make(*args, **kw))
+        return made[-1]
+    monkeypatch.setattr(R, "hos_kv_cache", recorded)
+    w = workload("c0")
+    p, o = (x[0] for x in w.lengths())
+    recs, queue = R.client_schedule(p, o, w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 1)
+    r = R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=8, kv_heads=2, head_dim=64, page=32, fmt=fmt, max_iters=6, repeat=5)
+    assert (r["us"] > 0).all() and len(made) == 5
+    assert len({c.k.data_ptr() for c in made}) == 5
+    one = R.cache_bytes(w.batch_cap, w.kv_budget, 2, 64, 32, fmt)
+    for c in made:
+        assert sum(t.numel() * t.element_size() for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None) == one
+        assert torch.equal(c.k.view(torch.uint8), made[0].k.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), made[0].v.view(torch.uint8))
+    assert bool(made[0].k.view(torch.uint8).any())
