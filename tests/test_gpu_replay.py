@@ -80,3 +80,46 @@ def test_every_timed_layer_has_a_cache_of_its_own(fmt, monkeypatch):
         assert sum(t.numel() * t.element_size() for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None) == one
         assert torch.equal(c.k.view(torch.uint8), made[0].k.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), made[0].v.view(torch.uint8))
     assert bool(made[0].k.view(torch.uint8).any())
+
+
+@pytest.mark.parametrize("fmt,heads,kv_heads,d,page", [("int8", 8, 2, 64, 32), ("e4m3", 8, 8, 128, 128), ("same", 4, 1, 64, 16)])
+def test_replay_holds_and_attends_to_what_was_appended(fmt, heads, kv_heads, d, page):
+    """After prefills and decode rounds, what the pages of the running requests hold is what was appended, bit for bit, and the outputs
+    are the formulas' on that (bounds as in the tests of attention, with the unit roundoffs of bf16 and of the weights)."""
+    import math
+    import torch
+    from paper_2502_15763_b200 import replay as R
+    from tests import kv_reference as K
+    from tests.test_gpu_kv_cache import CODES
+    from workload import workload
+    w = workload("c0")
+    p, o = (x[0] for x in w.lengths())
+    recs, queue = R.client_schedule(p, o, w.n_clients, w.batch_cap, w.kv_budget, w.cost_model, 1)
+    held, checked = {}, []                                        # request -> its appended keys and values, call by call
+
+    def watch(it, requests, x, cache, off, kv_len, table, out):
+        starts = off.tolist()
+        for s, r in enumerate(requests):
+            mine = x[starts[s]:starts[s + 1]]
+            held.setdefault(r, []).append((mine[:, heads:heads + kv_heads], mine[:, heads + kv_heads:]))
+        prefill = bool(recs[it]["kind_n"] >> 31)
+        if not (prefill and len(checked) % 2 == 0 or not prefill and it % 7 == 0):
+            return
+        checked.append(prefill)
+        lengths = kv_len.tolist()
+        assert lengths == [sum(len(k) for k, _ in held[r]) for r in requests]
+        for s, r in enumerate(requests):
+            for i, (store, scale) in enumerate(((cache.k, cache.k_scale), (cache.v, cache.v_scale))):
+                new = torch.cat([kv[i] for kv in held[r]])
+                want = new.double() if CODES[fmt] is None else K.values(*K.quantise(new, CODES[fmt]))
+                assert torch.equal(K.sequence(store, scale, table[s], lengths[s], page), want)
+        pairs = [(b - a, t) for a, b, t in zip(starts, starts[1:], lengths)]
+        want, _, mag, dot = K.attention(x[:, :heads], cache.k, cache.v, cache.k_scale, cache.v_scale, pairs, off, table, page, 1 / math.sqrt(d), True, 0)
+        u, uw = 2.0 ** -8, 2.0 ** -8 if fmt == "same" else 2.0 ** -11
+        e = (d + 4) * 2.0 ** -24 * dot
+        bound = u * want.abs() + (uw + 2.0 ** -18 + 2 * e[..., None]) * (1 + u) * mag + 2.0 ** -24
+        assert float(((out.double() - want).abs() / bound).max()) <= 1.0, it
+
+    R.replay(p, o, recs, queue, w.batch_cap, w.kv_budget, heads=heads, kv_heads=kv_heads, head_dim=d, page=page, fmt=fmt, max_iters=60, repeat=0,
+             watch=watch)
+    assert any(checked) and not all(checked)
