@@ -335,7 +335,8 @@ enum { HOS_KV_SAME = 0, HOS_KV_E4M3 = 1, HOS_KV_INT8 = 2 };
 /* HOST struct; DEVICE arrays.  k, v: [n_pages][n_kv_heads][page_size][head_dim], pages page_stride
  * elements apart (0: densely packed); k_scale, v_scale (8-bit formats only, else NULL):
  * [n_pages][n_kv_heads][page_size], pages scale_page_stride elements apart (0: densely packed).
- * head_dim 64 or 128; page_size 16, 32, 64, 128 or 256; all bases and page strides multiples of 16 bytes. */
+ * head_dim 64 or 128; page_size 16, 32, 64, 128 or 256; all bases and page strides multiples of 16 bytes;
+ * append and read take up to 1,048,560 KV heads. */
 typedef struct hos_kv_cache {
     int32_t n_pages, page_size, n_kv_heads, head_dim, type, format;
     void *k, *v;
@@ -384,13 +385,17 @@ int hos_kv_read(const hos_kv_cache* cache, const hos_kv_batch* batch, void* k, v
  *   x_j = sm_scale * <q, k_j>,   out = sum_j softmax(x)_j v_j,   lse = ln sum_j exp(x_j).
  * A row that sees nothing gets out = 0, lse = -inf.  Sums, maxima and normalisers are held in 32
  * bits; the weights are rounded to 16 bits (of the output's type, fp16 with an 8-bit cache) for their
- * product with the values, and an 8-bit cache's V scale below 2^-80 counts as 2^-80.  Memory past a sequence's last token may hold anything, NaN included; a
- * non-finite value that some new token of a sequence sees may also reach other new tokens of that sequence.
+ * product with the values, while their sum is of the unrounded ones.  With an 8-bit cache a V scale below 2^-80
+ * counts as 2^-80 (hos_kv_read takes it as it is), and bf16 queries enter the products as fp16 numbers times a power of
+ * two: elements below 2^-23 of a row's largest are rounded to within 2^-31 of that.
+ * Memory past a sequence's last token may hold anything, NaN included; a non-finite value that some new token of a
+ * sequence sees may also reach other new tokens of that sequence.  Rows of tokens that no sequence owns are not written.
  *   q    element (token, head, d) at token * q_tok_stride + head * q_head_stride + d (16-byte multiples)
  *   out  likewise with its own strides;  lse [n_tokens][n_heads], nullable
  *   status [n_seq], nullable, OR-ed into: HOS_ST_INVALID (offsets, length or page number out of
  *   range: the sequence's rows are undefined, nothing outside the given arrays is touched),
- *   HOS_ST_LIMIT (a bounded wait inside a kernel ran out; cannot happen on a working device)
+ *   HOS_ST_LIMIT (a wait inside a kernel, bounded to two seconds, ran out: rows of the sequence may be missing; every
+ *   such wait ends on a device that makes progress)
  */
 int hos_paged_attention(const hos_kv_cache* cache, const hos_kv_batch* batch, const void* q,
                         int64_t q_tok_stride, int64_t q_head_stride, int n_heads, float sm_scale, int causal,

@@ -18,14 +18,14 @@
 // An 8-bit cache's K scale multiplies the score, its V scale joins the exponent: y_j = x_j + log2 vs_j, the weights 2^(y_j - m)
 // meet the bare codes and are safe in fp16 whatever the scales are, and l = sum 2^(y_j - m) / vs_j.
 //
-// Measured on one B200, k_attn_combine included: 4,096 tokens, 64 heads of 128, bf16, causal: 290 us when cool, 345 us under the
-// power cap (800-950 TFLOP/s); 509 tokens, 64 heads over 8, behind 15,991 in an e4m3 cache: 325-350 us; 32 prompts of 129
-// tokens, 64 heads over 8, fp16: 69 us.  What bounds it: a half's chain of scores -> maximum -> exponentials -> products, which two
+// Measured on one B200, k_attn_combine included: 4,096 tokens, 64 heads of 128, bf16, causal: 334-344 us under the power cap
+// (810 TFLOP/s); 509 tokens, 64 heads over 8, behind 15,991 in an e4m3 cache: 343-347 us; 32 prompts of 129
+// tokens, 64 heads over 8, fp16: 69-71 us.  What bounds it: a half's chain of scores -> maximum -> exponentials -> products, which two
 // halves hide from one another only in part: a step of 2 x 128 rows takes about 3,300 cycles, of which the tensor cores need 2,048 and
 // the exponentials (16 a cycle and SM) 2,048; with an 8-bit cache about 5,300, since every thread reads three vectors
 // of 128 scales from shared memory.  Work that short prompts cannot hide: a tile's queries in, its first score and its result out.
 // (The first 96 of a step's 128 weights are handed over early, so that only a quarter of the second product waits for the last
-// exponentials; a third half in flight would need more tensor memory than there is.)
+// exponentials; with head_dim 128 a third half in flight would need more tensor memory than there is.)
 //
 // Waits by parity: a barrier must not be two phases past (or short of) the one waited for.  Why none is, by barrier:
 //   kv_full    the products' warp waits in order, and a stage is refilled only after that warp has freed it; half 0's wait for V

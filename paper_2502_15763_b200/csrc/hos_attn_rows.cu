@@ -22,8 +22,8 @@
 //
 // Measured on one B200, k_attn_combine included: 32,463 tokens of 64 bf16 KV heads of 128 in 16 sequences (1.06 GB) 168 us,
 // 6.3 TB/s; 265,813 tokens of 8 int8 heads in 128 sequences (566 MB) 111 us, 5.1 TB/s; 282,150 tokens of 8 e4m3 heads of
-// 64 in 2 sequences (307 MB) 62 us, 5.0 TB/s.  8-bit caches are bound by instruction issue (12 warps an SM, about 0.6
-// instructions a cycle and scheduler: turning codes into fp16 and the steps' fixed part), 16-bit ones by HBM.  One share a
+// 64 in 2 sequences (307 MB) 62 us, 5.0 TB/s.  16-bit caches are bound by HBM, 8-bit ones by the work of a step (turning codes into
+// fp16, the reductions) that 12 warps an SM hide only in part: 56 % of the issue slots are used.  One share a
 // warp instead of one a CTA left four times the pieces and took 125 and 83 us for the last two.
 #include "hos_attn_list.cuh"
 #include "hos_kv_kernels.h"
@@ -588,7 +588,8 @@ cudaError_t run(const AttnView& a, int max_rows, bool beside, const AttnWs& ws, 
 
 }  // namespace
 
-// `beside`: the chunk kernel of the same call was launched just before, and this one may start while that runs.
+// `beside`: the chunk kernel of the same call was launched just before, and this one may start while that runs (a CTA of it fits on
+// an SM once the chunk kernel's has left it, so it fills that kernel's tail).
 cudaError_t launch_attn_rows(const AttnView& a, int type, int format, int tile_rows, int max_rows, bool beside, const AttnWs& ws, int* workers,
                              cudaStream_t st) {
     return kv_dispatch(type, format, a.kv.head_dim, [&](auto t, auto f, auto d) {

@@ -1,5 +1,8 @@
 """Binding of the KV-cache calls: keys and values in pages, written, read back and attended to.
 
+The calls have no backward pass: tensors that require grad are refused while gradients are on.  They are plain
+functions, not registered operators, so dispatch modes and tracing do not see them.
+
 `hos_kv_cache` checks a cache's tensors once and returns the handle that the other calls take.  The
 batch is the same three device tensors everywhere (int32): `tok_off` [n_seq + 1], the packed new
 tokens of every sequence; `kv_len` [n_seq], its tokens in the cache, the new ones included;
