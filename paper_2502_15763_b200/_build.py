@@ -27,11 +27,12 @@ def _deps():
 
 
 def source_hash() -> str:
-    """SHA-256 over the scheduling kernels' sources (names and contents, in name order): what a set of
-    profiler counters of theirs was taken on.  The KV-cache kernels share none of that code."""
+    """SHA-256 over the scheduling kernels' sources (names and contents, in name order), the headers that the
+    KV-cache kernels share with them included: what a set of profiler counters of theirs was taken on.  Only
+    the KV-cache kernels' own files do not count."""
     import hashlib
     h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(CSRC, "*.cu*")) + glob.glob(os.path.join(CSRC, "*.h"))):
+    for path in sorted(_deps()):
         if os.path.basename(path).startswith(("hos_kv", "hos_attn")):
             continue
         h.update(os.path.basename(path).encode() + b"\0")
