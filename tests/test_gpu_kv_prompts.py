@@ -47,3 +47,29 @@ def test_whole_prompts_again_and_again(fmt):
     assert int(cache.status.abs().sum()) == 0
     for o in outs:
         assert torch.equal(o.view(torch.int16), first.view(torch.int16))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_beside_other_traffic(fmt, d):
+    """Copies on another stream make loads and stores slow: same outputs, no status."""
+    import torch
+    import paper_2502_15763_b200 as hos
+    from tests import kv_reference as R
+    from tests.test_gpu_kv_cache import make_cache
+    pairs = [(384, 384)] * 6 + [(100, 900)] * 6 + [(640, 640)] * 4
+    off, kv_len, table, n_pages = R.make_batch(pairs, 32, 0, 3)
+    cache = hos.hos_kv_cache(*make_cache(n_pages, 32, 32, d, torch.bfloat16, fmt, 4), dtype=torch.bfloat16)
+    q = torch.randn((sum(n for n, _ in pairs), 32, d), device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).bfloat16()
+    first = hos.hos_paged_attention(q, cache, off, kv_len, table, 640)["out"]
+    a, b = (torch.empty(1 << 30, dtype=torch.uint8, device="cuda") for _ in range(2))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(60):
+            b.copy_(a)
+    outs = [hos.hos_paged_attention(q, cache, off, kv_len, table, 640)["out"] for _ in range(40)]
+    torch.cuda.synchronize()
+    assert int(cache.status.abs().sum()) == 0
+    for o in outs:
+        assert torch.equal(o.view(torch.int16), first.view(torch.int16))
