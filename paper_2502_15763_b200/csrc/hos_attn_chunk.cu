@@ -556,9 +556,7 @@ k_attn_chunk(const __grid_constant__ AttnView a, const __grid_constant__ CUtenso
             }
             if (there) {
                 if (whole) {
-                    if (a.lse)
-                        a.lse[(long long)(cur.q.off + tok) * a.n_heads + hd] =
-                            l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+                    if (a.lse) a.lse[(long long)(cur.q.off + tok) * a.n_heads + hd] = row_lse<!C::Q8>(m, l);
                 } else {
                     state[(long long)slot * ROWS + h * HALF + row] = RowState{m, l};
                 }

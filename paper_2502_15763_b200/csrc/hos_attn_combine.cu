@@ -72,7 +72,7 @@ __device__ __forceinline__ void join_rows(const AttnView& a, const AttnWs& ws, i
         reinterpret_cast<uint2*>(dst)[lane] = make_uint2(Pair<T>::pack(o.x * by, o.y * by), Pair<T>::pack(o.z * by, o.w * by));
     }
     if (a.lse && lane == 0)
-        a.lse[(long long)tok * a.n_heads + hd] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+        a.lse[(long long)tok * a.n_heads + hd] = row_lse(m, l);
 }
 
 // A quarter of a tile of 256 rows, mostly of two or three pieces, which hold four columns of every row together: a warp takes four
@@ -116,7 +116,7 @@ __device__ __forceinline__ void join_tile(const AttnView& a, const AttnWs& ws, i
     for (int e = 0; e < PER; ++e)
         reinterpret_cast<uint2*>(dst)[g + 8 * e] = make_uint2(Pair<T>::pack(o[e].x * by, o[e].y * by), Pair<T>::pack(o[e].z * by, o[e].w * by));
     if (a.lse && g == 0)
-        a.lse[(long long)tok * a.n_heads + hd] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+        a.lse[(long long)tok * a.n_heads + hd] = row_lse(m, l);
 }
 
 template <typename T, int D, int ROWS>

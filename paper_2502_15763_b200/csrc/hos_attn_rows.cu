@@ -383,8 +383,7 @@ k_attn_rows(const __grid_constant__ AttnView a, const int max_rows, const bool b
                     if (OWN == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(v[0], v[OWN - 1]);
                     else *reinterpret_cast<uint32_t*>(dst) = v[0];
                     if (a.lse && g == 0 && warp == 0)
-                        a.lse[(long long)tok * a.n_heads + hd] =
-                            norm[nb][e] == 0.0f ? -INFINITY : (ref[nb][e] + log2f(norm[nb][e])) * 0.69314718055994530942f;
+                        a.lse[(long long)tok * a.n_heads + hd] = row_lse(ref[nb][e], norm[nb][e]);
                 } else {
                     const long long r = (long long)slot * ROWS + in_tile;
                     float* dst = part + r * D + d0;

@@ -168,6 +168,19 @@ struct Partial {                              // per worker, what slot 1 holds
 };
 struct RowState { float m, l; };              // of one row: what its exponents (base 2) are relative to, and the sum of its weights
 
+// A row's lse from its state.  The power of two of l joins m first: with an 8-bit cache m holds the lift and the log2 of V's scale, and
+// log2 l as much with the other sign, so that their sum would keep the rounding of numbers around 20.  SMALL: m holds no scale and a
+// lift of 7 at most, which costs no such bits (32 short prompts, fp16, in the chunk kernel: 70.9 us so, 71.5 otherwise).
+template <bool SMALL = false> __device__ __forceinline__ float row_lse(float m, float l) {
+    constexpr float LN2 = 0.69314718055994530942f;
+    if (l == 0.0f) return -INFINITY;
+    if (SMALL) return (m + log2f(l)) * LN2;
+    const uint32_t bits = __float_as_uint(l);
+    const int biased = (int)(bits >> 23);
+    if (biased < 1 || biased > 254) return (m + log2f(l)) * LN2;          // denormal, infinite, NaN
+    return ((m + (float)(biased - 127)) + log2f(__uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u))) * LN2;
+}
+
 // The smallest V scale that the attention kernels tell from zero (a vector of values below 1e-21).
 constexpr float LEAST_V_SCALE = 8.2718061e-25f;                       // 2^-80
 
