@@ -58,9 +58,10 @@ enum {
                                  T_i >= 2^32, assignment outside [0, n_clients), or a queue key
                                  p_i + o_est_i too long to sit beside the client number in 32
                                  bits: bit_width(max p + o_est) + bit_width(n_clients - 1) > 32) */
-    HOS_ST_RANGE   = 8        /* a lower bound of this instance does not fit 64 bits (products of
+    HOS_ST_RANGE   = 8,       /* a lower bound of this instance does not fit 64 bits (products of
                                  coefficients and token sums that are each inside their limits);
                                  its hos_lb is zeroed, everything else is unaffected             */
+    HOS_ST_PAGES   = 16       /* too few free pages: the sequence keeps its length (hos_kv_resize) */
 };
 
 enum { HOS_QUEUE_SORTED = 0, HOS_QUEUE_FCFS = 1 };
@@ -329,7 +330,7 @@ int hos_trace_offsets(const hos_client_result* cres, int64_t n_units, int64_t* t
  *   Q = 448 or 127, each operation rounded to 32 bits;  the value of a code is code * scale.
  * A vector that holds a NaN or an infinity reads back as NaN.
  */
-enum { HOS_TYPE_BF16 = 0, HOS_TYPE_FP16 = 1 };
+enum { HOS_TYPE_BF16 = 0, HOS_TYPE_FP16 = 1, HOS_TYPE_FP32 = 2 /* probabilities only */ };
 enum { HOS_KV_SAME = 0, HOS_KV_E4M3 = 1, HOS_KV_INT8 = 2 };
 
 /* HOST struct; DEVICE arrays.  k, v: [n_pages][n_kv_heads][page_size][head_dim], pages page_stride
@@ -402,6 +403,113 @@ int hos_paged_attention(const hos_kv_cache* cache, const hos_kv_batch* batch, co
                         int window, void* out, int64_t out_tok_stride, int64_t out_head_stride, float* lse,
                         int32_t* status, void* ws, size_t ws_bytes, void* stream);
 size_t hos_paged_attention_workspace_bytes(const hos_kv_cache* cache, const hos_kv_batch* batch, int n_heads);
+
+/*
+ * Whose pages are whose.  refs[p] is the number of page-table entries, over all sequences, that hold page p;
+ * a page with refs[p] = 0 is free.  Sequence s holds the first ceil(kv_len[s] / page_size) entries of its row;
+ * the entries after those mean nothing.  A pool begins as zeros: all pages free, all sequences of length 0.
+ * The calls below take the state in `in` and leave the new one in `out`, which may be other memory or, where
+ * they say so, the same (array by array); a row of `out` is max_pages entries, -1 after its pages.  In place,
+ * entries that a sequence held neither before nor after stay as they are.
+ * page_size may be any positive number here; max_pages * page_size < 2^31 - 256, n_seq <= 262,144,
+ * n_pages <= 16,777,216.  Counts and numbers are whole and every page is chosen by its number, so results
+ * do not depend on timing.  Page numbers outside [0, n_pages) in entries that a sequence holds are carried
+ * along and counted nowhere (HOS_ST_INVALID; in hos_kv_resize only for entries given up or grown from).
+ *   status [n_seq of out], nullable, written
+ */
+typedef struct hos_kv_pages {    /* HOST struct; DEVICE arrays */
+    int32_t n_pages, page_size, n_seq, max_pages;
+    int32_t* refs;               /* [n_pages] */
+    int32_t* kv_len;             /* [n_seq] */
+    int32_t* page_table;         /* [n_seq][table_stride] */
+    int64_t table_stride;
+} hos_kv_pages;
+
+/* Page copies to be made, DEVICE arrays: page src[i] to page dst[i] for i < *count; -1 after those.  No page
+ * is in both lists, none twice in dst. */
+typedef struct hos_kv_moves {    /* HOST struct */
+    int32_t *src, *dst, *count;  /* [n_seq] for hos_kv_resize, [n_pages] for hos_kv_compact; [1] */
+} hos_kv_moves;
+
+/*
+ * Sequence s gets the length new_len[s]: admission (from 0), decode rounds (by the tokens to be appended),
+ * taking drafts back, freeing (to 0), as if these were done one after the other:
+ *   1. sequences that shrink give up the pages past their new end;
+ *   2. the sequences that grow, in order: if it grows from inside a page that others hold, too
+ *      (refs > 1), it gets a page of its own for that one, to be copied (`moves`, in order of sequences);
+ *      then one page for each that it lacks.  Pages are taken in order of their numbers, lowest first,
+ *      from those that are free after 1.  The first sequence whose pages are not there, and every
+ *      growing one after it, keeps its length and pages (HOS_ST_PAGES).
+ * A length outside [0, max_pages * page_size], old or new: the sequence stays as it is, with its whole row
+ * (HOS_ST_INVALID).  A page that is given up more often than it is held: HOS_ST_INVALID.
+ * `out` may be `in`, as a whole or array by array.  The copies have to be made before the new tokens are
+ * appended, and before the next call of these.
+ */
+int hos_kv_resize(const hos_kv_pages* in, const int32_t* new_len, const hos_kv_pages* out, const hos_kv_moves* moves,
+                  int32_t* status, void* ws, size_t ws_bytes, void* stream);
+size_t hos_kv_resize_workspace_bytes(const hos_kv_pages* in);
+
+/*
+ * Sequence i of `out` (out->n_seq of them) gets the pages and the length of sequence parent[i] of `in`; -1: none,
+ * length 0.  Sequences of `in` that are nobody's parent give up their pages, those with several children share
+ * them.  So prompts are sampled several times, beams reordered, finished sequences dropped.
+ * out->refs may be in->refs; page_table and kv_len must be other memory.  HOS_ST_INVALID: parent[i] outside
+ * [-1, n_seq), or its length out of range; i is then empty (and that parent's pages are neither shared nor given up).
+ */
+int hos_kv_fork(const hos_kv_pages* in, const int32_t* parent, const hos_kv_pages* out, int32_t* status, void* ws,
+                size_t ws_bytes, void* stream);
+size_t hos_kv_fork_workspace_bytes(const hos_kv_pages* in);
+
+/*
+ * Moves the pages in use to the front: with n of them, the k-th page numbered n or more that is in use goes
+ * to the k-th free page below n (`moves`), and refs and the table follow.  The table must hold all sequences
+ * that hold pages.  `out` may be `in`; kv_len is only read (out->kv_len is not used).  HOS_ST_INVALID: a page that
+ * the sequence holds and refs says is free, or a length out of range (the row is left as it is).
+ */
+int hos_kv_compact(const hos_kv_pages* in, const hos_kv_pages* out, const hos_kv_moves* moves, int32_t* status, void* ws,
+                   size_t ws_bytes, void* stream);
+size_t hos_kv_compact_workspace_bytes(const hos_kv_pages* in);
+
+/*
+ * Copies whole pages, keys, values and scales as they are: page src_page[i] of from[l] to page dst_page[i] of to[l],
+ * for i < n_moves, or i < *count if that is less (count DEVICE, nullable), and for all n_layers caches (HOST
+ * arrays of structs; `from` may be `to`).  All have one shape and format; n_pages and page strides may differ.  A page must not be
+ * written twice in a call, nor written and read.
+ *   status [n_moves], nullable, OR-ed into: HOS_ST_INVALID where a page number is out of range (not copied)
+ */
+int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_layers, const int32_t* src_page,
+                      const int32_t* dst_page, const int32_t* count, int n_moves, int32_t* status, void* stream);
+
+/*
+ * Which of a round's drafted tokens the target keeps, and the token that follows them, from given random numbers.
+ * The batch is that of the round's attention call: sequence s owns the n_s packed tokens from tok_off[s] on,
+ * tokens[r] = the one it had, then k = n_s - 1 drafts.  Row r of target [n_tokens][vocab] is the target's
+ * distribution after token r, row r of draft (nullable) the one that tokens[r+1] was drawn from; without it the
+ * drafts were not drawn (q = 1 at the draft, 0 elsewhere).  With p, q the rows of r and d = tokens[r+1]:
+ *   the draft is accepted if those before it are and  u_accept[r] * q(d) < p(d)   (exact in 64 bits);
+ *   next = the least v with  sum_{x <= v} w(x) > u_sample[s] * sum_x w(x),  w and its sums in 64 bits, where
+ *     w = max(p - q, 0) at the first draft that is not accepted (p, if that is zero everywhere),
+ *     w = p of the last row if all are.
+ * Rows need not sum to one.  Entries that are negative, infinite or NaN count as zero, and so does a u_sample
+ * that is negative or NaN; from 1 on u_sample gives the last v with w(v) > 0.
+ *   target, draft  one type (HOS_TYPE_*), element (row, v) at row * stride + v, any alignment that the type has
+ *   accepted [n_seq], next [n_seq], out_tokens [n_tokens]: the accepted drafts, next, then -1; rows of no sequence
+ *     are not written (offsets that descend may give a row to two: it holds what either has)
+ *   kv_len, new_len [n_seq], both or neither: new_len = kv_len - k + accepted (the length to cut the cache to)
+ *   status [n_seq], nullable, written: HOS_ST_INVALID where offsets are out of range (accepted 0, next -1, nothing
+ *     else), the first draft that is not accepted is outside [0, vocab), or w is zero everywhere (next -1)
+ * A sequence without tokens: accepted 0, next -1.
+ */
+typedef struct hos_drafts {      /* HOST struct; DEVICE arrays */
+    int32_t n_seq, n_tokens, vocab, type;
+    const int32_t *tok_off, *tokens;          /* [n_seq + 1], [n_tokens] */
+    const void *target, *draft;
+    int64_t target_stride, draft_stride;
+    const float *u_accept, *u_sample;         /* [n_tokens], [n_seq] */
+    const int32_t* kv_len;                    /* [n_seq], nullable */
+    int32_t *accepted, *next, *out_tokens, *new_len, *status;
+} hos_drafts;
+int hos_verify_drafts(const hos_drafts* d, void* stream);
 
 size_t hos_offline_workspace_bytes(const hos_batch* batch, int n_copies, int ls_rounds);
 size_t hos_offline_multifit_workspace_bytes(const hos_batch* batch, int ls_rounds);

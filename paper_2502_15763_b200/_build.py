@@ -33,7 +33,7 @@ def source_hash() -> str:
     import hashlib
     h = hashlib.sha256()
     for path in sorted(_deps()):
-        if os.path.basename(path).startswith(("hos_kv", "hos_attn")):
+        if os.path.basename(path).startswith(("hos_kv", "hos_attn", "hos_pages", "hos_drafts", "hos_cluster")):
             continue
         h.update(os.path.basename(path).encode() + b"\0")
         with open(path, "rb") as fh:

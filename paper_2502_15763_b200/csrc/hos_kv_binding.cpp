@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <vector>
 
 #include "hos.h"
 
@@ -24,6 +25,14 @@ decltype(&hos_kv_append) p_append;
 decltype(&hos_kv_read) p_read;
 decltype(&hos_paged_attention) p_attention;
 decltype(&hos_paged_attention_workspace_bytes) p_workspace;
+decltype(&hos_kv_resize) p_resize;
+decltype(&hos_kv_resize_workspace_bytes) p_resize_workspace;
+decltype(&hos_kv_fork) p_fork;
+decltype(&hos_kv_fork_workspace_bytes) p_fork_workspace;
+decltype(&hos_kv_compact) p_compact;
+decltype(&hos_kv_compact_workspace_bytes) p_compact_workspace;
+decltype(&hos_kv_copy_pages) p_copy_pages;
+decltype(&hos_verify_drafts) p_verify;
 
 constexpr int STATUS_TOO_SHORT = 1;              // not an error of the library: the caller lengthens its status words and calls again
 
@@ -128,16 +137,23 @@ template <typename F> PyObject* guarded(F&& f) {
     return nullptr;
 }
 
-// init(append, read, attention, workspace_bytes): addresses of the C entry points
+// init(addresses of the C entry points, in the order below)
+template <typename P> void set(P& entry, PyObject* address) { entry = reinterpret_cast<P>(PyLong_AsVoidPtr(address)); }
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!arity(n, 4)) return nullptr;
-    void* p[4];
-    for (int i = 0; i < 4; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!arity(n, 12)) return nullptr;
+    set(p_append, a[0]);
+    set(p_read, a[1]);
+    set(p_attention, a[2]);
+    set(p_workspace, a[3]);
+    set(p_resize, a[4]);
+    set(p_resize_workspace, a[5]);
+    set(p_fork, a[6]);
+    set(p_fork_workspace, a[7]);
+    set(p_compact, a[8]);
+    set(p_compact_workspace, a[9]);
+    set(p_copy_pages, a[10]);
+    set(p_verify, a[11]);
     if (PyErr_Occurred()) return nullptr;
-    p_append = reinterpret_cast<decltype(p_append)>(p[0]);
-    p_read = reinterpret_cast<decltype(p_read)>(p[1]);
-    p_attention = reinterpret_cast<decltype(p_attention)>(p[2]);
-    p_workspace = reinterpret_cast<decltype(p_workspace)>(p[3]);
     Py_RETURN_NONE;
 }
 
@@ -281,9 +297,259 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the pages of a cache ------------------------------------------------------------------------------------------
+
+// A dense int32 (or float32) tensor of one dimension on `device` (-1: any CUDA device) with `size` elements (-1: any).
+const at::Tensor* vector(PyObject* o, const char* what, at::ScalarType type, int device, int64_t size) {
+    const at::Tensor* t = tensor(o, what);
+    if (!t) return nullptr;
+    if (t->scalar_type() != type || !t->is_cuda() || (device >= 0 && t->get_device() != device)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a CUDA tensor of %s%s", what, type == at::kInt ? "int32" : "float32",
+                     device >= 0 ? " on the same device as the others" : "");
+        return nullptr;
+    }
+    if (t->dim() != 1 || !t->is_contiguous() || (size >= 0 && t->size(0) != size)) {
+        if (size >= 0) PyErr_Format(PyExc_ValueError, "%s: expected one dense dimension of %lld", what, (long long)size);
+        else PyErr_Format(PyExc_ValueError, "%s: expected one dense dimension", what);
+        return nullptr;
+    }
+    if (t->size(0) > INT32_MAX) {
+        PyErr_SetString(PyExc_ValueError, "sizes beyond 32 bits");
+        return nullptr;
+    }
+    return t;
+}
+
+// refs, page_table and kv_len; device -1 and n_seq -1: whatever the first of them has.
+bool state_of(PyObject* refs_o, PyObject* table_o, PyObject* len_o, long long page_size, int device, int64_t n_pages, int64_t n_seq, int64_t width,
+              hos_kv_pages* p) {
+    const at::Tensor* refs = vector(refs_o, "refs", at::kInt, device, n_pages);
+    if (!refs) return false;
+    const at::Tensor* len = vector(len_o, "kv_len", at::kInt, refs->get_device(), n_seq);
+    const at::Tensor* table = len ? tensor(table_o, "page_table") : nullptr;
+    if (!table) return false;
+    if (table->scalar_type() != at::kInt || !table->is_cuda() || table->get_device() != refs->get_device()) {
+        PyErr_SetString(PyExc_TypeError, "page_table: expected a CUDA tensor of int32 on the same device as the others");
+        return false;
+    }
+    if (table->dim() != 2 || table->size(0) != len->size(0) || (width >= 0 && table->size(1) != width) || (table->size(1) > 1 && table->stride(1) != 1)) {
+        PyErr_SetString(PyExc_ValueError, "page_table: expected [n_seq][pages] with dense rows");
+        return false;
+    }
+    if (table->size(0) > 1 && table->stride(0) < table->size(1)) {
+        PyErr_SetString(PyExc_ValueError, "page_table: rows must not overlap");
+        return false;
+    }
+    if (table->size(1) > INT32_MAX || page_size > INT32_MAX || page_size < 1) {
+        PyErr_SetString(PyExc_ValueError, "sizes beyond 32 bits, or no page size");
+        return false;
+    }
+    *p = hos_kv_pages{(int32_t)refs->size(0), (int32_t)page_size, (int32_t)len->size(0), (int32_t)table->size(1), refs->mutable_data_ptr<int32_t>(),
+                      len->mutable_data_ptr<int32_t>(), table->mutable_data_ptr<int32_t>(), table->size(0) > 1 ? table->stride(0) : table->size(1)};
+    return true;
+}
+
+at::Tensor words(at::IntArrayRef sizes, int device) {
+    return at::empty(sizes, at::TensorOptions().dtype(at::kInt).device(at::kCUDA, (c10::DeviceIndex)device));
+}
+
+enum { RESIZE, FORK, COMPACT };
+// a: refs, page_table, kv_len, new_len or parent or None, page_size, out or None.
+// (error code, refs, page_table, kv_len, status), and but for FORK src, dst, count
+PyObject* pages(int kind, PyObject* const* a) {
+    const long long page_size = PyLong_AsLongLong(a[4]);
+    if (PyErr_Occurred()) return nullptr;
+    hos_kv_pages in, out;
+    if (!state_of(a[0], a[1], a[2], page_size, -1, -1, -1, -1, &in)) return nullptr;
+    const int device = THPVariable_Unpack(a[0]).get_device();
+    const at::Tensor* change = nullptr;
+    if (kind != COMPACT && !(change = vector(a[3], kind == RESIZE ? "new_len" : "parent", at::kInt, device, kind == RESIZE ? in.n_seq : -1))) return nullptr;
+    const int64_t n_out = kind == FORK ? change->size(0) : in.n_seq;
+    const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
+    at::Tensor refs, table, len, moves, count;
+    if (a[5] == Py_None) {
+        refs = words({in.n_pages}, device);
+        table = words({n_out, in.max_pages}, device);
+        len = kind == COMPACT ? THPVariable_Unpack(a[2]) : words({n_out}, device);
+        out = hos_kv_pages{in.n_pages, in.page_size, (int32_t)n_out, in.max_pages, refs.mutable_data_ptr<int32_t>(), len.mutable_data_ptr<int32_t>(),
+                           table.mutable_data_ptr<int32_t>(), in.max_pages};
+    } else {
+        if (!PyTuple_Check(a[5]) || PyTuple_GET_SIZE(a[5]) != 3) {
+            PyErr_SetString(PyExc_TypeError, "out: expected a tuple (refs, page_table, kv_len)");
+            return nullptr;
+        }
+        PyObject* const o[3] = {PyTuple_GET_ITEM(a[5], 0), PyTuple_GET_ITEM(a[5], 1), PyTuple_GET_ITEM(a[5], 2)};
+        if (!state_of(o[0], o[1], o[2], page_size, device, in.n_pages, n_out, in.max_pages, &out)) return nullptr;
+        refs = THPVariable_Unpack(o[0]);
+        table = THPVariable_Unpack(o[1]);
+        len = THPVariable_Unpack(o[2]);
+    }
+    const int64_t n_moves = kind == RESIZE ? in.n_seq : in.n_pages;
+    hos_kv_moves m = {nullptr, nullptr, nullptr};
+    at::Tensor src, dst;
+    if (kind != FORK) {
+        src = words({n_moves}, device);
+        dst = words({n_moves}, device);
+        count = words({1}, device);
+        // an empty tensor has no address, and nothing is written to it
+        m = hos_kv_moves{n_moves ? src.mutable_data_ptr<int32_t>() : count.mutable_data_ptr<int32_t>(),
+                         n_moves ? dst.mutable_data_ptr<int32_t>() : count.mutable_data_ptr<int32_t>(), count.mutable_data_ptr<int32_t>()};
+    }
+    at::Tensor status = words({n_out}, device);
+    const auto need = kind == RESIZE ? p_resize_workspace : kind == FORK ? p_fork_workspace : p_compact_workspace;
+    at::Tensor ws = at::empty({(int64_t)need(&in)}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)device));
+    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device);
+    void* w = ws.mutable_data_ptr();
+    const size_t bytes = (size_t)ws.numel();
+    int32_t* s = status.mutable_data_ptr<int32_t>();
+    const int rc = kind == RESIZE ? p_resize(&in, change->const_data_ptr<int32_t>(), &out, &m, s, w, bytes, st.stream())
+                 : kind == FORK ? p_fork(&in, change->const_data_ptr<int32_t>(), &out, s, w, bytes, st.stream())
+                                : p_compact(&in, &out, &m, s, w, bytes, st.stream());
+    if (kind == FORK) return Py_BuildValue("iNNNN", rc, THPVariable_Wrap(refs), THPVariable_Wrap(table), THPVariable_Wrap(len), THPVariable_Wrap(status));
+    return Py_BuildValue("iNNNNNNN", rc, THPVariable_Wrap(refs), THPVariable_Wrap(table), THPVariable_Wrap(len), THPVariable_Wrap(status),
+                         THPVariable_Wrap(src), THPVariable_Wrap(dst), THPVariable_Wrap(count));
+}
+
+// resize, fork, compact(refs, page_table, kv_len, new_len | parent | None, page_size, out or None)
+template <int KIND> PyObject* pages_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* { return arity(n, 6) ? pages(KIND, a) : nullptr; });
+}
+
+// copy_pages(list of handles, list of source handles, src, dst, count or None): error code
+PyObject* copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (!arity(n, 5)) return nullptr;
+        if (!PyList_Check(a[0]) || !PyList_Check(a[1]) || PyList_GET_SIZE(a[0]) != PyList_GET_SIZE(a[1]) || PyList_GET_SIZE(a[0]) < 1) {
+            PyErr_SetString(PyExc_ValueError, "as many source caches as caches, and one at least");
+            return nullptr;
+        }
+        const Py_ssize_t layers = PyList_GET_SIZE(a[0]);
+        std::vector<hos_kv_cache> to, from;
+        to.reserve(layers);
+        from.reserve(layers);
+        const Cache* first = nullptr;
+        for (Py_ssize_t l = 0; l < layers; ++l) {
+            const Cache* c = cache_of(PyList_GET_ITEM(a[0], l));
+            const Cache* f = c ? cache_of(PyList_GET_ITEM(a[1], l)) : nullptr;
+            if (!f) return nullptr;
+            if (!first) first = c;
+            for (const Cache* x : {c, f})
+                if (x->device != first->device) {
+                    PyErr_SetString(PyExc_ValueError, "the caches must be on one device");
+                    return nullptr;
+                }
+            for (const Cache* x : {c, f})
+                if (x->c.n_kv_heads != first->c.n_kv_heads || x->c.page_size != first->c.page_size || x->c.head_dim != first->c.head_dim ||
+                    x->c.type != first->c.type || x->c.format != first->c.format) {
+                    PyErr_SetString(PyExc_ValueError, "the caches must have the same heads, page size, head_dim, dtype and format");
+                    return nullptr;
+                }
+            to.push_back(c->c);
+            from.push_back(f->c);
+        }
+        for (Py_ssize_t l = 0; l < layers; ++l)
+            if (to[l].n_pages != to[0].n_pages || from[l].n_pages != from[0].n_pages) {
+                PyErr_SetString(PyExc_ValueError, "all layers must have the same number of pages");
+                return nullptr;
+            }
+        const at::Tensor* src = vector(a[2], "src", at::kInt, first->device, -1);
+        const at::Tensor* dst = src ? vector(a[3], "dst", at::kInt, first->device, src->size(0)) : nullptr;
+        if (!dst) return nullptr;
+        const at::Tensor* count = nullptr;
+        if (a[4] != Py_None && !(count = vector(a[4], "count", at::kInt, first->device, 1))) return nullptr;
+        if (src->size(0) > first->status.numel()) return PyLong_FromLong(STATUS_TOO_SHORT);
+        const c10::cuda::CUDAGuard guard(first->device);
+        const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream(first->device);
+        return PyLong_FromLong(p_copy_pages(to.data(), from.data(), (int)layers, src->const_data_ptr<int32_t>(), dst->const_data_ptr<int32_t>(),
+                                            count ? count->const_data_ptr<int32_t>() : nullptr, (int)src->size(0), first->words(st), st.stream()));
+    });
+}
+
+// A [n_tokens][vocab] tensor of probabilities.
+const at::Tensor* probabilities(PyObject* o, const char* what, const at::Tensor* like) {
+    const at::Tensor* t = tensor(o, what);
+    if (!t) return nullptr;
+    const at::ScalarType k = t->scalar_type();
+    if (!t->is_cuda() || (k != at::kFloat && k != at::kHalf && k != at::kBFloat16) ||
+        (like && (k != like->scalar_type() || t->get_device() != like->get_device()))) {
+        PyErr_Format(PyExc_TypeError, like ? "%s: expected a tensor of target's dtype on its device" : "%s: expected a CUDA tensor of float32, float16 or bfloat16", what);
+        return nullptr;
+    }
+    if (t->dim() != 2 || t->size(1) < 1 || (t->size(1) > 1 && t->stride(1) != 1) || (like && t->sizes() != like->sizes())) {
+        PyErr_Format(PyExc_ValueError, "%s: expected [n_tokens][vocab] with dense rows", what);
+        return nullptr;
+    }
+    if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) {
+        PyErr_SetString(PyExc_ValueError, "sizes beyond 32 bits");
+        return nullptr;
+    }
+    if (t->requires_grad() && c10::GradMode::is_enabled()) {
+        PyErr_Format(PyExc_ValueError, "%s requires grad, and there is no backward pass: detach it, or call under torch.no_grad()", what);
+        return nullptr;
+    }
+    return t;
+}
+
+// verify(tokens, target, draft or None, tok_off, u_accept, u_sample, kv_len or None): (error code, accepted, next, tokens, new_len or None, status)
+PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (!arity(n, 7)) return nullptr;
+        const at::Tensor* target = probabilities(a[1], "target", nullptr);
+        if (!target) return nullptr;
+        const at::Tensor* draft = nullptr;
+        if (a[2] != Py_None && !(draft = probabilities(a[2], "draft", target))) return nullptr;
+        const int device = target->get_device();
+        const int64_t n_tok = target->size(0);
+        const at::Tensor* tokens = vector(a[0], "tokens", at::kInt, device, n_tok);
+        const at::Tensor* off = tokens ? vector(a[3], "tok_off", at::kInt, device, -1) : nullptr;
+        if (!off) return nullptr;
+        if (off->size(0) < 1) {
+            PyErr_SetString(PyExc_ValueError, "tok_off must have n_seq + 1 entries");
+            return nullptr;
+        }
+        const int64_t n_seq = off->size(0) - 1;
+        const at::Tensor* ua = vector(a[4], "u_accept", at::kFloat, device, n_tok);
+        const at::Tensor* us = ua ? vector(a[5], "u_sample", at::kFloat, device, n_seq) : nullptr;
+        if (!us) return nullptr;
+        const at::Tensor* len = nullptr;
+        if (a[6] != Py_None && !(len = vector(a[6], "kv_len", at::kInt, device, n_seq))) return nullptr;
+        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
+        at::Tensor accepted = words({n_seq}, device), next = words({n_seq}, device), out = words({n_tok}, device), status = words({n_seq}, device), now;
+        if (len) now = words({n_seq}, device);
+        hos_drafts d = {};
+        d.n_seq = (int32_t)n_seq;
+        d.n_tokens = (int32_t)n_tok;
+        d.vocab = (int32_t)target->size(1);
+        d.type = target->scalar_type() == at::kFloat ? HOS_TYPE_FP32 : target->scalar_type() == at::kHalf ? HOS_TYPE_FP16 : HOS_TYPE_BF16;
+        d.tok_off = off->const_data_ptr<int32_t>();
+        d.tokens = tokens->const_data_ptr<int32_t>();
+        d.target = target->const_data_ptr();
+        d.target_stride = n_tok > 1 ? target->stride(0) : d.vocab;
+        if (draft) {
+            d.draft = draft->const_data_ptr();
+            d.draft_stride = n_tok > 1 ? draft->stride(0) : d.vocab;
+        }
+        d.u_accept = ua->const_data_ptr<float>();
+        d.u_sample = us->const_data_ptr<float>();
+        d.accepted = accepted.mutable_data_ptr<int32_t>();
+        d.next = next.mutable_data_ptr<int32_t>();
+        d.out_tokens = out.mutable_data_ptr<int32_t>();
+        d.status = status.mutable_data_ptr<int32_t>();
+        if (len) {
+            d.kv_len = len->const_data_ptr<int32_t>();
+            d.new_len = now.mutable_data_ptr<int32_t>();
+        }
+        const int rc = p_verify(&d, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream());
+        return Py_BuildValue("iNNNNN", rc, THPVariable_Wrap(accepted), THPVariable_Wrap(next), THPVariable_Wrap(out),
+                             len ? THPVariable_Wrap(now) : Py_NewRef(Py_None), THPVariable_Wrap(status));
+    });
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"init", FAST(init)}, {"cache", FAST(cache)}, {"set_status", FAST(set_status)}, {"append", FAST(append)},
-                         {"read", FAST(read)}, {"attention", FAST(attention)}, {nullptr, nullptr, 0, nullptr}};
+                         {"read", FAST(read)}, {"attention", FAST(attention)}, {"resize", FAST(pages_call<RESIZE>)},
+                         {"fork", FAST(pages_call<FORK>)}, {"compact", FAST(pages_call<COMPACT>)}, {"copy_pages", FAST(copy_pages)},
+                         {"verify", FAST(verify)}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
