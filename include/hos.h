@@ -456,9 +456,7 @@ size_t hos_kv_resize_workspace_bytes(const hos_kv_pages* in);
  * out->refs may be in->refs; page_table and kv_len must be other memory.  HOS_ST_INVALID: parent[i] outside
  * [-1, n_seq), or its length out of range; i is then empty (and that parent's pages are neither shared nor given up).
  */
-int hos_kv_fork(const hos_kv_pages* in, const int32_t* parent, const hos_kv_pages* out, int32_t* status, void* ws,
-                size_t ws_bytes, void* stream);
-size_t hos_kv_fork_workspace_bytes(const hos_kv_pages* in);
+int hos_kv_fork(const hos_kv_pages* in, const int32_t* parent, const hos_kv_pages* out, int32_t* status, void* stream);
 
 /*
  * Moves the pages in use to the front: with n of them, the k-th page numbered n or more that is in use goes
@@ -487,11 +485,11 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
  * distribution after token r, row r of draft (nullable) the one that tokens[r+1] was drawn from; without it the
  * drafts were not drawn (q = 1 at the draft, 0 elsewhere).  With p, q the rows of r and d = tokens[r+1]:
  *   the draft is accepted if those before it are and  u_accept[r] * q(d) < p(d)   (exact in 64 bits);
- *   next = the least v with  sum_{x <= v} w(x) > u_sample[s] * sum_x w(x),  w and its sums in 64 bits, where
+ *   next = the least v with  sum_{x <= v} w(x) > u_sample[s] * sum_x w(x),  sums good to 2^-40 of the whole, where
  *     w = max(p - q, 0) at the first draft that is not accepted (p, if that is zero everywhere),
  *     w = p of the last row if all are.
- * Rows need not sum to one.  Entries that are negative, infinite or NaN count as zero, and so does a u_sample
- * that is negative or NaN; from 1 on u_sample gives the last v with w(v) > 0.
+ * Rows need not sum to one.  Entries of target that are negative, infinite or NaN count as zero, and so do entries of
+ * draft that are negative or NaN, and a u_sample that is; from 1 on u_sample gives the last v with w(v) > 0.
  *   target, draft  one type (HOS_TYPE_*), element (row, v) at row * stride + v, any alignment that the type has
  *   accepted [n_seq], next [n_seq], out_tokens [n_tokens]: the accepted drafts, next, then -1; rows of no sequence
  *     are not written (offsets that descend may give a row to two: it holds what either has)

@@ -91,7 +91,7 @@ def build_binding(force: bool = False) -> str:
                            "-isystem", home + "/include", "-isystem", home + "/include/torch/csrc/api/include",
                            "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda + "/include",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", tmp, BINDING_SOURCE,
-                           "-L" + home + "/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+                           "-L" + home + "/lib", "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     os.replace(tmp, path)
     return path
 

@@ -34,7 +34,7 @@ _SYMBOLS = ("hos_offline_pack", "hos_local_search", "hos_lower_bound", "hos_onli
             "hos_lower_bound_static", "hos_trace_fill", "hos_online_simulate_steal",
             "hos_offline_pack_multifit", "hos_debug_bounds_violations", "hos_offline_multifit_workspace_bytes",
             "hos_kv_append", "hos_kv_read", "hos_paged_attention", "hos_paged_attention_workspace_bytes",
-            "hos_kv_resize", "hos_kv_resize_workspace_bytes", "hos_kv_fork", "hos_kv_fork_workspace_bytes",
+            "hos_kv_resize", "hos_kv_resize_workspace_bytes", "hos_kv_fork",
             "hos_kv_compact", "hos_kv_compact_workspace_bytes", "hos_kv_copy_pages", "hos_verify_drafts")
 
 LAUNCH_HOOK = C.CFUNCTYPE(None, C.c_char_p, C.c_int, C.c_void_p, C.c_void_p)
@@ -81,7 +81,7 @@ def lib():
         for name in ("hos_offline_workspace_bytes", "hos_lower_bound_workspace_bytes",
                      "hos_online_workspace_bytes", "hos_offline_multifit_workspace_bytes",
                      "hos_paged_attention_workspace_bytes", "hos_kv_resize_workspace_bytes",
-                     "hos_kv_fork_workspace_bytes", "hos_kv_compact_workspace_bytes"):
+                     "hos_kv_compact_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.hos_strerror.restype = C.c_char_p
         for name in ("hos_offline_pack", "hos_local_search", "hos_lower_bound",
@@ -96,11 +96,11 @@ def lib():
         L.hos_paged_attention.argtypes = [p, p, p, i64, i64, i32, C.c_float, i32, i32, p, i64, i64, p, p, p, C.c_size_t, p]
         L.hos_paged_attention_workspace_bytes.argtypes = [p, p, i32]
         L.hos_kv_resize.argtypes = [p, p, p, p, p, p, C.c_size_t, p]
-        L.hos_kv_fork.argtypes = [p, p, p, p, p, C.c_size_t, p]
+        L.hos_kv_fork.argtypes = [p, p, p, p, p]
         L.hos_kv_compact.argtypes = [p, p, p, p, p, C.c_size_t, p]
         L.hos_kv_copy_pages.argtypes = [p, p, i32, p, p, p, i32, p, p]
         L.hos_verify_drafts.argtypes = [p, p]
-        for name in ("hos_kv_resize", "hos_kv_fork", "hos_kv_compact"):
+        for name in ("hos_kv_resize", "hos_kv_compact"):
             getattr(L, name + "_workspace_bytes").argtypes = [p]
         _lib = L
     return _lib

@@ -16,18 +16,33 @@
 namespace hos {
 namespace {
 
-constexpr int THREADS = 512, WARPS = THREADS / 32, MOST_BLOCKS = 16;
+constexpr int THREADS = 512, WARPS = THREADS / 32;
 
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-// What a probability counts for: nothing, unless it is positive and finite.
-__device__ __forceinline__ float counted(float x) { return x > 0.0f && x < __int_as_float(0x7F800000) ? x : 0.0f; }
+__device__ __forceinline__ bool counts(float x) { return x > 0.0f && x < __int_as_float(0x7F800000); }
+// What a probability of the target counts for: nothing, unless it is positive and finite; of the draft: nothing, if it is negative or NaN.
+__device__ __forceinline__ float target_of(float x) { return counts(x) ? x : 0.0f; }
+__device__ __forceinline__ float draft_of(float x) { return fmaxf(x, 0.0f); }
 
-__device__ __forceinline__ double warp_sum_double(double v) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(FULL, v, d);
-    return v;
+// 16 bytes of a row.
+template <typename T> struct Vec {
+    static constexpr int N = 16 / sizeof(T);
+    uint4 w;
+    __device__ __forceinline__ float at(int i) const;
+};
+template <> __device__ __forceinline__ float Vec<float>::at(int i) const {
+    return __uint_as_float(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w);
+}
+__device__ __forceinline__ uint32_t pair_of(const uint4& w, int i) { return i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w; }
+template <> __device__ __forceinline__ float Vec<__half>::at(int i) const {
+    const float2 f = Pair<__half>::unpack(pair_of(w, i));
+    return i & 1 ? f.y : f.x;
+}
+template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::at(int i) const {
+    const float2 f = Pair<__nv_bfloat16>::unpack(pair_of(w, i));
+    return i & 1 ? f.y : f.x;
 }
 
 // The weights that the next token is drawn by: of entry v, max(p - q, 0) in 64 bits; q null: p, but nothing at `banned`.
@@ -35,11 +50,80 @@ template <typename T> struct Weights {
     const T *p, *q;
     int banned;
     __device__ __forceinline__ double at(int v) const {
-        const double x = counted(as_float(p[v]));
+        const double x = target_of(as_float(__ldg(p + v)));
         if (!q) return v == banned ? 0.0 : x;
-        return fmax(x - (double)counted(as_float(q[v])), 0.0);
+        return fmax(x - (double)draft_of(as_float(__ldg(q + v))), 0.0);
+    }
+    // Sum over [a, b) by one warp; where they can be read 16 bytes at a time from `a` on, in both rows.  A difference x - y > 0 is
+    // d + e exactly, d rounded to 32 bits and e = (x - d) - y (Dekker, 1971).  The d are added up in 64 bits; the e, below 2^-24 of
+    // them, 16 or 32 in 32 bits first, which leaves 2^-43 of the sum.  So a conversion and a 64-bit sum are left of two and three
+    // (they go at a fraction of the others' rate).
+    template <bool Q> __device__ __forceinline__ double sum_wide(int a, int b) const {
+        constexpr int N = Vec<T>::N, AHEAD = 4;
+        double s[2] = {0.0, 0.0};
+        const int whole = a + (b - a) / N * N;
+        for (int i0 = a + lane_id() * N; i0 < whole; i0 += 32 * N * AHEAD) {
+            Vec<T> x[AHEAD], y[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = i0 + k * 32 * N;
+                x[k].w = y[k].w = make_uint4(0, 0, 0, 0);
+                if (i < whole) {
+                    x[k].w = __ldg(reinterpret_cast<const uint4*>(p + i));
+                    if (Q) y[k].w = __ldg(reinterpret_cast<const uint4*>(q + i));
+                }
+            }
+            float small = 0.0f;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int out = banned - (i0 + k * 32 * N);        // which of these is the banned one
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float v = x[k].at(j);
+                    if (Q) {
+                        const float u = draft_of(y[k].at(j)), d = v - u, e = (v - d) - u;
+                        const bool some = counts(d);
+                        s[j & 1] += (double)(some ? d : 0.0f);
+                        small += some ? e : 0.0f;
+                    } else {
+                        s[j & 1] += (double)(counts(v) && j != out ? v : 0.0f);
+                    }
+                }
+            }
+            if (Q) s[0] += (double)small;
+        }
+        const int i = whole + lane_id();
+        if (i < b) s[0] += at(i);
+        return s[0] + s[1];
+    }
+    __device__ __forceinline__ double sum(int a, int b, bool wide) const {
+        if (wide) return q ? sum_wide<true>(a, b) : sum_wide<false>(a, b);
+        double s = 0.0;
+#pragma unroll 8
+        for (int i = a + lane_id(); i < b; i += 32) s += at(i);
+        return s;
     }
 };
+
+__device__ __forceinline__ double warp_sum_double(double v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(FULL, v, d);
+    return v;
+}
+__device__ __forceinline__ double warp_sum_upto(double v) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double o = __shfl_up_sync(FULL, v, d);
+        if (lane_id() >= d) v += o;
+    }
+    return v;
+}
+// The first lane whose sum `upto` is beyond t; if there is none (rounding, or a t that is the whole sum), the last one that has
+// anything itself; -1: nobody has.
+__device__ __forceinline__ int first_beyond(double upto, double own, double t) {
+    const unsigned beyond = __ballot_sync(FULL, own > 0.0 && upto > t), some = __ballot_sync(FULL, own > 0.0);
+    return beyond ? __ffs(beyond) - 1 : 31 - __clz(some);
+}
 
 struct Verdict {
     int off, n, accepted, flags;                     // the sequence's tokens; drafts accepted; status bits
@@ -64,8 +148,8 @@ template <typename T> __device__ __forceinline__ Verdict judge(const hos_drafts&
             const float u = __ldg(d.u_accept + row);
             strange = (unsigned)token >= (unsigned)d.vocab;
             if (!strange) {
-                const float p = counted(as_float(static_cast<const T*>(d.target)[row * d.target_stride + token]));
-                const float q = d.draft ? counted(as_float(static_cast<const T*>(d.draft)[row * d.draft_stride + token])) : 1.0f;
+                const float p = target_of(as_float(static_cast<const T*>(d.target)[row * d.target_stride + token]));
+                const float q = d.draft ? draft_of(as_float(static_cast<const T*>(d.draft)[row * d.draft_stride + token])) : 1.0f;
                 good = (double)u * (double)q < (double)p;
             }
         }
@@ -83,9 +167,9 @@ template <typename T> __device__ __forceinline__ Verdict judge(const hos_drafts&
     return r;
 }
 
-template <typename T> __global__ void __launch_bounds__(THREADS) k_verify_drafts(const __grid_constant__ hos_drafts d) {
+template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_drafts(const __grid_constant__ hos_drafts d) {
     __shared__ Verdict verdict;
-    __shared__ double sums[WARPS], before[MOST_BLOCKS * WARPS + 1];
+    __shared__ double sums[WARPS], total;
     pdl_launch_dependents();
     pdl_wait();
     const int blocks = cluster_size(), rank = cluster_rank(), s = (int)blockIdx.x / blocks;
@@ -96,122 +180,107 @@ template <typename T> __global__ void __launch_bounds__(THREADS) k_verify_drafts
     __syncthreads();
     const Verdict v = verdict;
     const int k = v.n - 1;
-    const bool rejected = v.accepted < k;
-    int next = -1;
-    if (v.n > 0) {                                     // the same for the whole cluster
-        const long long row = v.off + v.accepted;
-        Weights<T> w{static_cast<const T*>(d.target) + row * d.target_stride, nullptr, -1};
-        if (rejected && d.draft) w.q = static_cast<const T*>(d.draft) + row * d.draft_stride;
-        if (rejected && !d.draft) w.banned = __ldg(d.tokens + row + 1);
-        const int each = (d.vocab + blocks * WARPS - 1) / (blocks * WARPS);
-        const long long first = (long long)(rank * WARPS + warp_id()) * each;
-        const int a = (int)min(first, (long long)d.vocab), b = (int)min(first + each, (long long)d.vocab);
-        double all = 0.0;
-        for (int pass = 0; pass < 2; ++pass) {         // a second one only if nothing is left of p - q
-            double sum = 0.0;
-#pragma unroll 8
-            for (int i = a + lane_id(); i < b; i += 32) sum += w.at(i);
-            sum = warp_sum_double(sum);
-            if (lane_id() == 0) sums[warp_id()] = sum;
-            cluster_sync();
-            if (warp_id() == 0) {                      // sums of the segments before each, in order
-                double base = 0.0;
-                for (int i0 = 0; i0 < blocks * WARPS; i0 += 32) {
-                    const int i = i0 + lane_id();
-                    const double mine = i < blocks * WARPS ? __longlong_as_double((long long)read_of_block(sums + i % WARPS, i / WARPS)) : 0.0;
-                    double x = mine;
-#pragma unroll
-                    for (int dd = 1; dd < 32; dd <<= 1) {
-                        const double o = __shfl_up_sync(FULL, x, dd);
-                        if (lane_id() >= dd) x += o;
-                    }
-                    if (i < blocks * WARPS) before[i + 1] = base + x;
-                    base += __shfl_sync(FULL, x, 31);
-                }
-                if (lane_id() == 0) before[0] = 0.0;
-            }
-            __syncthreads();
-            all = before[blocks * WARPS];
-            cluster_sync();                            // nobody's sums are written or gone before all have been read
-            if (all > 0.0 || !rejected || pass == 1) break;
-            w.q = nullptr;
-            w.banned = -1;
+    if (rank == 0) {
+        for (int i = (int)threadIdx.x; i < v.n; i += THREADS)
+            if (i != v.accepted) d.out_tokens[v.off + i] = i < v.accepted ? __ldg(d.tokens + v.off + i + 1) : -1;
+        if (threadIdx.x == 0) {
+            d.accepted[s] = v.accepted;
+            if (d.new_len) d.new_len[s] = __ldg(d.kv_len + s) - (k > 0 ? k - v.accepted : 0);
+            if (v.n == 0) d.next[s] = -1;
+            if (d.status) d.status[s] = v.flags;
         }
-        if (all > 0.0) {
-            const float u = __ldg(d.u_sample + s);
-            const double t = u > 0.0f ? (double)u * all : 0.0;
-            // the first segment whose end is beyond t; if rounding or a u from 1 on leaves none, the last one that has anything
-            const int mine = rank * WARPS + warp_id();
-            int segment = -1, last = 0;
-            for (int i0 = 0; i0 < blocks * WARPS && segment < 0; i0 += 32) {
-                const int i = i0 + lane_id();
-                const bool in = i < blocks * WARPS;
-                const unsigned beyond = __ballot_sync(FULL, in && before[i + 1] > t), some = __ballot_sync(FULL, in && before[i + 1] > before[i]);
-                if (beyond) segment = i0 + __ffs(beyond) - 1;
-                else if (some) last = i0 + 31 - __clz(some);
-            }
-            if (segment < 0) segment = last;
-            if (segment == mine) {
-                double c = before[mine];
-                int pick = -1, positive = -1;
-                for (int i0 = a; i0 < b && pick < 0; i0 += 32) {
-                    const int i = i0 + lane_id();
-                    const double x = i < b ? w.at(i) : 0.0;
-                    double sum = x;
-#pragma unroll
-                    for (int dd = 1; dd < 32; dd <<= 1) {
-                        const double o = __shfl_up_sync(FULL, sum, dd);
-                        if (lane_id() >= dd) sum += o;
-                    }
-                    const unsigned beyond = __ballot_sync(FULL, x > 0.0 && c + sum > t), some = __ballot_sync(FULL, x > 0.0);
-                    if (beyond) pick = i0 + __ffs(beyond) - 1;
-                    else if (some) positive = i0 + 31 - __clz(some);
-                    c += __shfl_sync(FULL, sum, 31);
-                }
-                next = pick >= 0 ? pick : positive;
-                if (lane_id() == 0) {
-                    d.next[s] = next;
-                    d.out_tokens[row] = next;
-                }
-            }
-        }
-        if (rank == 0) {
-            if (!(all > 0.0) && threadIdx.x == 0) {
-                d.next[s] = -1;
-                d.out_tokens[row] = -1;
-            }
-            for (int i = (int)threadIdx.x; i < v.n; i += THREADS)
-                if (i != v.accepted) d.out_tokens[v.off + i] = i < v.accepted ? __ldg(d.tokens + v.off + i + 1) : -1;
-        }
-        if (rank == 0 && threadIdx.x == 0 && d.status) d.status[s] = v.flags | (all > 0.0 ? 0 : HOS_ST_INVALID);
-    } else if (rank == 0 && threadIdx.x == 0) {
-        d.next[s] = -1;
-        if (d.status) d.status[s] = v.flags;
     }
-    if (rank == 0 && threadIdx.x == 0) {
-        d.accepted[s] = v.accepted;
-        if (d.new_len) d.new_len[s] = __ldg(d.kv_len + s) - (k > 0 ? k - v.accepted : 0);
+    if (v.n == 0) return;                              // the whole cluster
+    const bool rejected = v.accepted < k;
+    const long long row = v.off + v.accepted;
+    Weights<T> w{static_cast<const T*>(d.target) + row * d.target_stride, nullptr, -1};
+    if (rejected && d.draft) w.q = static_cast<const T*>(d.draft) + row * d.draft_stride;
+    if (rejected && !d.draft) w.banned = __ldg(d.tokens + row + 1);
+    // segments begin on 16 bytes of p, the first at 0, and end with the row
+    constexpr int N = Vec<T>::N;
+    const int head = (int)((16 - (reinterpret_cast<uintptr_t>(w.p) & 15)) & 15) / (int)sizeof(T);
+    const bool wide = !w.q || ((reinterpret_cast<uintptr_t>(w.p) ^ reinterpret_cast<uintptr_t>(w.q)) & 15) == 0;
+    const long long each = ((d.vocab + blocks * WARPS - 1) / (blocks * WARPS) + N - 1) / N * N;
+    auto edge = [&](int i) { return i == 0 ? 0 : (int)min(head + i * each, (long long)d.vocab); };
+    const int segment = rank * WARPS + warp_id(), a = edge(segment), b = edge(segment + 1);
+    const float u = __ldg(d.u_sample + s);
+    for (int pass = 0;; ++pass) {                      // a second one only if nothing is left of p - q
+        const int from = min(b, max(a, head));
+        double sum = w.sum(from, b, wide);
+        if (a + lane_id() < from) sum += w.at(a + lane_id());
+        sum = warp_sum_double(sum);
+        if (lane_id() == 0) sums[warp_id()] = sum;
+        __syncthreads();
+        double own = lane_id() < WARPS ? sums[lane_id()] : 0.0, upto = warp_sum_upto(own);
+        if (threadIdx.x == 31) total = upto;
+        cluster_or_block_sync();
+        const double of_block = lane_id() < blocks ? read_of_block(&total, lane_id()) : 0.0;
+        const double upto_block = warp_sum_upto(of_block);
+        if (blocks > 1) cluster_arrive();
+        const double all = __shfl_sync(FULL, upto_block, 31);
+        if (!(all > 0.0)) {
+            if (blocks > 1) cluster_wait();
+            else __syncthreads();
+            if (rejected && pass == 0) {
+                w.q = nullptr;
+                w.banned = -1;
+                continue;
+            }
+            if (rank == 0 && threadIdx.x == 0) {
+                d.next[s] = d.out_tokens[row] = -1;
+                if (d.status) d.status[s] = v.flags | HOS_ST_INVALID;
+            }
+            return;
+        }
+        const double t = u > 0.0f ? (double)u * all : 0.0;
+        const int block = first_beyond(upto_block, of_block, t);
+        if (block == rank) {
+            double left = t - __shfl_sync(FULL, upto_block - of_block, block);
+            const int warp = first_beyond(upto, own, left);
+            left -= __shfl_sync(FULL, upto - own, warp);
+            // the segment of that warp, by the whole block: a run of neighbours each
+            const int i = rank * WARPS + warp, first = edge(i), last = edge(i + 1);
+            const int run = (last - first + THREADS - 1) / THREADS, c = min(first + (int)threadIdx.x * run, last), e = min(c + run, last);
+            double mine = 0.0;
+            for (int x = c; x < e; ++x) mine += w.at(x);
+            __syncthreads();
+            const double upto_lane = warp_sum_upto(mine);
+            if (lane_id() == 31) sums[warp_id()] = upto_lane;
+            __syncthreads();
+            own = lane_id() < WARPS ? sums[lane_id()] : 0.0;
+            upto = warp_sum_upto(own);
+            const int in = first_beyond(upto, own, left);
+            if (warp_id() == in) {
+                left -= __shfl_sync(FULL, upto - own, in);
+                const int lane = first_beyond(upto_lane, mine, left);
+                if (lane_id() == lane) {
+                    left -= upto_lane - mine;
+                    int pick = -1;
+                    double sofar = 0.0;
+                    for (int x = c; x < e; ++x) {
+                        const double y = w.at(x);
+                        sofar += y;
+                        if (y > 0.0) {
+                            pick = x;
+                            if (sofar > left) break;
+                        }
+                    }
+                    d.next[s] = d.out_tokens[row] = pick;
+                }
+            }
+        }
+        if (blocks > 1) cluster_wait();
+        return;
     }
 }
 
+// As many blocks a sequence as there are room for at once (two of 512 threads an SM, and as good as all SMs even), up to 8, with
+// 2,048 entries each at least.  One, 2, 4, 8, 16, us: one sequence of 32,000 32-bit entries 8.6, 6.6, 5.6, 5.6, 5.8; 33 of 50,257
+// bf16 ones 12.7, 10.7, 8.9, 10.1, 20.6; 128 of 128,000 32-bit ones 44, 30, 33, 41, 73.
 template <typename T> cudaError_t verify(const hos_drafts& d, cudaStream_t st) {
-    const int blocks = 1;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)blocks;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(d.n_seq * blocks));
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    launch_hook("k_verify_drafts", 0, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_verify_drafts<T>, d);
-    launch_hook("k_verify_drafts", 1, st);
-    return e;
+    int blocks = 8;
+    while (blocks > 1 && ((long long)d.n_seq * blocks > 256 || d.vocab < 2048 * blocks)) blocks >>= 1;
+    return launch_clusters("k_verify_drafts", k_verify_drafts<T>, d.n_seq * blocks, blocks, THREADS, st, d);
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
@@ -28,7 +29,6 @@ decltype(&hos_paged_attention_workspace_bytes) p_workspace;
 decltype(&hos_kv_resize) p_resize;
 decltype(&hos_kv_resize_workspace_bytes) p_resize_workspace;
 decltype(&hos_kv_fork) p_fork;
-decltype(&hos_kv_fork_workspace_bytes) p_fork_workspace;
 decltype(&hos_kv_compact) p_compact;
 decltype(&hos_kv_compact_workspace_bytes) p_compact_workspace;
 decltype(&hos_kv_copy_pages) p_copy_pages;
@@ -140,7 +140,7 @@ template <typename F> PyObject* guarded(F&& f) {
 // init(addresses of the C entry points, in the order below)
 template <typename P> void set(P& entry, PyObject* address) { entry = reinterpret_cast<P>(PyLong_AsVoidPtr(address)); }
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!arity(n, 12)) return nullptr;
+    if (!arity(n, 11)) return nullptr;
     set(p_append, a[0]);
     set(p_read, a[1]);
     set(p_attention, a[2]);
@@ -148,11 +148,10 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     set(p_resize, a[4]);
     set(p_resize_workspace, a[5]);
     set(p_fork, a[6]);
-    set(p_fork_workspace, a[7]);
-    set(p_compact, a[8]);
-    set(p_compact_workspace, a[9]);
-    set(p_copy_pages, a[10]);
-    set(p_verify, a[11]);
+    set(p_compact, a[7]);
+    set(p_compact_workspace, a[8]);
+    set(p_copy_pages, a[9]);
+    set(p_verify, a[10]);
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
@@ -349,13 +348,64 @@ bool state_of(PyObject* refs_o, PyObject* table_o, PyObject* len_o, long long pa
     return true;
 }
 
-at::Tensor words(at::IntArrayRef sizes, int device) {
-    return at::empty(sizes, at::TensorOptions().dtype(at::kInt).device(at::kCUDA, (c10::DeviceIndex)device));
+// The int32 results of a call and its workspace, cut from one allocation: with eight of their own the allocations took longer than
+// the kernel.  (Whoever keeps one of the results keeps the workspace: 12 bytes a page at most.)
+class Words {
+  public:
+    explicit Words(int device) : device_(device) {}
+    // Room for a result of this many words; returns where it will be.
+    int64_t add(int64_t words) {
+        const int64_t at = total_;
+        total_ += (words + 63) & ~(int64_t)63;
+        return at;
+    }
+    void allocate() { whole_ = at::detail::empty_cuda({total_}, at::kInt, at::Device(at::kCUDA, (c10::DeviceIndex)device_), std::nullopt); }
+    int32_t* address(int64_t at) const { return static_cast<int32_t*>(whole_.mutable_data_ptr()) + at; }
+    PyObject* tensor(int64_t at, at::IntArrayRef sizes) const {
+        at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole_.storage()), whole_.key_set(), whole_.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(at);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+        return THPVariable_Wrap(t);
+    }
+
+  private:
+    int device_;
+    int64_t total_ = 0;
+    at::TensorBase whole_;
+};
+
+// A dict of results; a value that is missing (an error) leaves none.
+class Results {
+  public:
+    Results() : dict_(PyDict_New()) {}
+    ~Results() { Py_XDECREF(dict_); }
+    void add(PyObject* name, PyObject* value) {
+        if (!value || !dict_ || PyDict_SetItem(dict_, name, value)) Py_CLEAR(dict_);
+        Py_XDECREF(value);
+    }
+    PyObject* take() {
+        PyObject* d = dict_;
+        dict_ = nullptr;
+        if (!d && !PyErr_Occurred()) PyErr_NoMemory();
+        return d;
+    }
+
+  private:
+    PyObject* dict_;
+};
+struct Names {
+    PyObject *refs, *page_table, *kv_len, *status, *src, *dst, *count, *accepted, *next, *tokens, *new_len;
+};
+const Names& names() {
+    static const Names n = {PyUnicode_InternFromString("refs"), PyUnicode_InternFromString("page_table"), PyUnicode_InternFromString("kv_len"),
+                            PyUnicode_InternFromString("status"), PyUnicode_InternFromString("src"), PyUnicode_InternFromString("dst"),
+                            PyUnicode_InternFromString("count"), PyUnicode_InternFromString("accepted"), PyUnicode_InternFromString("next"),
+                            PyUnicode_InternFromString("tokens"), PyUnicode_InternFromString("new_len")};
+    return n;
 }
 
 enum { RESIZE, FORK, COMPACT };
-// a: refs, page_table, kv_len, new_len or parent or None, page_size, out or None.
-// (error code, refs, page_table, kv_len, status), and but for FORK src, dst, count
+// a: refs, page_table, kv_len, new_len or parent or None, page_size, out or None.  Error code, or the results.
 PyObject* pages(int kind, PyObject* const* a) {
     const long long page_size = PyLong_AsLongLong(a[4]);
     if (PyErr_Occurred()) return nullptr;
@@ -364,50 +414,41 @@ PyObject* pages(int kind, PyObject* const* a) {
     const int device = THPVariable_Unpack(a[0]).get_device();
     const at::Tensor* change = nullptr;
     if (kind != COMPACT && !(change = vector(a[3], kind == RESIZE ? "new_len" : "parent", at::kInt, device, kind == RESIZE ? in.n_seq : -1))) return nullptr;
-    const int64_t n_out = kind == FORK ? change->size(0) : in.n_seq;
+    const int64_t n_out = kind == FORK ? change->size(0) : in.n_seq, n_moves = kind == RESIZE ? in.n_seq : kind == COMPACT ? in.n_pages : 0;
+    const bool given = a[5] != Py_None;
+    if (given && (!PyTuple_Check(a[5]) || PyTuple_GET_SIZE(a[5]) != 3)) {
+        PyErr_SetString(PyExc_TypeError, "out: expected a tuple (refs, page_table, kv_len)");
+        return nullptr;
+    }
+    PyObject* const* o = given ? &PyTuple_GET_ITEM(a[5], 0) : nullptr;
+    if (given && !state_of(o[0], o[1], o[2], page_size, device, in.n_pages, n_out, in.max_pages, &out)) return nullptr;
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
-    at::Tensor refs, table, len, moves, count;
-    if (a[5] == Py_None) {
-        refs = words({in.n_pages}, device);
-        table = words({n_out, in.max_pages}, device);
-        len = kind == COMPACT ? THPVariable_Unpack(a[2]) : words({n_out}, device);
-        out = hos_kv_pages{in.n_pages, in.page_size, (int32_t)n_out, in.max_pages, refs.mutable_data_ptr<int32_t>(), len.mutable_data_ptr<int32_t>(),
-                           table.mutable_data_ptr<int32_t>(), in.max_pages};
-    } else {
-        if (!PyTuple_Check(a[5]) || PyTuple_GET_SIZE(a[5]) != 3) {
-            PyErr_SetString(PyExc_TypeError, "out: expected a tuple (refs, page_table, kv_len)");
-            return nullptr;
-        }
-        PyObject* const o[3] = {PyTuple_GET_ITEM(a[5], 0), PyTuple_GET_ITEM(a[5], 1), PyTuple_GET_ITEM(a[5], 2)};
-        if (!state_of(o[0], o[1], o[2], page_size, device, in.n_pages, n_out, in.max_pages, &out)) return nullptr;
-        refs = THPVariable_Unpack(o[0]);
-        table = THPVariable_Unpack(o[1]);
-        len = THPVariable_Unpack(o[2]);
-    }
-    const int64_t n_moves = kind == RESIZE ? in.n_seq : in.n_pages;
-    hos_kv_moves m = {nullptr, nullptr, nullptr};
-    at::Tensor src, dst;
+    const size_t need = kind == RESIZE ? p_resize_workspace(&in) : kind == COMPACT ? p_compact_workspace(&in) : 0;
+    Words w(device);
+    const int64_t scratch = w.add((int64_t)(need / 4)), status = w.add(n_out), src = w.add(n_moves), dst = w.add(n_moves), count = w.add(kind != FORK),
+                  refs = w.add(given ? 0 : in.n_pages), table = w.add(given ? 0 : n_out * in.max_pages), len = w.add(given || kind == COMPACT ? 0 : n_out);
+    w.allocate();
+    if (!given)
+        out = hos_kv_pages{in.n_pages, in.page_size, (int32_t)n_out, in.max_pages, w.address(refs), kind == COMPACT ? in.kv_len : w.address(len),
+                           w.address(table), in.max_pages};
+    void* st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+    const hos_kv_moves m = {w.address(src), w.address(dst), w.address(count)};
+    const int rc = kind == RESIZE ? p_resize(&in, change->const_data_ptr<int32_t>(), &out, &m, w.address(status), w.address(scratch), need, st)
+                 : kind == FORK ? p_fork(&in, change->const_data_ptr<int32_t>(), &out, w.address(status), st)
+                                : p_compact(&in, &out, &m, w.address(status), w.address(scratch), need, st);
+    if (rc) return PyLong_FromLong(rc);
+    const Names& n = names();
+    Results r;
+    r.add(n.refs, given ? Py_NewRef(o[0]) : w.tensor(refs, {in.n_pages}));
+    r.add(n.page_table, given ? Py_NewRef(o[1]) : w.tensor(table, {n_out, in.max_pages}));
+    r.add(n.kv_len, given ? Py_NewRef(o[2]) : kind == COMPACT ? Py_NewRef(a[2]) : w.tensor(len, {n_out}));
+    r.add(n.status, w.tensor(status, {n_out}));
     if (kind != FORK) {
-        src = words({n_moves}, device);
-        dst = words({n_moves}, device);
-        count = words({1}, device);
-        // an empty tensor has no address, and nothing is written to it
-        m = hos_kv_moves{n_moves ? src.mutable_data_ptr<int32_t>() : count.mutable_data_ptr<int32_t>(),
-                         n_moves ? dst.mutable_data_ptr<int32_t>() : count.mutable_data_ptr<int32_t>(), count.mutable_data_ptr<int32_t>()};
+        r.add(n.src, w.tensor(src, {n_moves}));
+        r.add(n.dst, w.tensor(dst, {n_moves}));
+        r.add(n.count, w.tensor(count, {1}));
     }
-    at::Tensor status = words({n_out}, device);
-    const auto need = kind == RESIZE ? p_resize_workspace : kind == FORK ? p_fork_workspace : p_compact_workspace;
-    at::Tensor ws = at::empty({(int64_t)need(&in)}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)device));
-    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device);
-    void* w = ws.mutable_data_ptr();
-    const size_t bytes = (size_t)ws.numel();
-    int32_t* s = status.mutable_data_ptr<int32_t>();
-    const int rc = kind == RESIZE ? p_resize(&in, change->const_data_ptr<int32_t>(), &out, &m, s, w, bytes, st.stream())
-                 : kind == FORK ? p_fork(&in, change->const_data_ptr<int32_t>(), &out, s, w, bytes, st.stream())
-                                : p_compact(&in, &out, &m, s, w, bytes, st.stream());
-    if (kind == FORK) return Py_BuildValue("iNNNN", rc, THPVariable_Wrap(refs), THPVariable_Wrap(table), THPVariable_Wrap(len), THPVariable_Wrap(status));
-    return Py_BuildValue("iNNNNNNN", rc, THPVariable_Wrap(refs), THPVariable_Wrap(table), THPVariable_Wrap(len), THPVariable_Wrap(status),
-                         THPVariable_Wrap(src), THPVariable_Wrap(dst), THPVariable_Wrap(count));
+    return r.take();
 }
 
 // resize, fork, compact(refs, page_table, kv_len, new_len | parent | None, page_size, out or None)
@@ -490,7 +531,7 @@ const at::Tensor* probabilities(PyObject* o, const char* what, const at::Tensor*
     return t;
 }
 
-// verify(tokens, target, draft or None, tok_off, u_accept, u_sample, kv_len or None): (error code, accepted, next, tokens, new_len or None, status)
+// verify(tokens, target, draft or None, tok_off, u_accept, u_sample, kv_len or None): error code, or the results
 PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         if (!arity(n, 7)) return nullptr;
@@ -514,8 +555,9 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* len = nullptr;
         if (a[6] != Py_None && !(len = vector(a[6], "kv_len", at::kInt, device, n_seq))) return nullptr;
         const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
-        at::Tensor accepted = words({n_seq}, device), next = words({n_seq}, device), out = words({n_tok}, device), status = words({n_seq}, device), now;
-        if (len) now = words({n_seq}, device);
+        Words w(device);
+        const int64_t accepted = w.add(n_seq), next = w.add(n_seq), out = w.add(n_tok), status = w.add(n_seq), now = w.add(len ? n_seq : 0);
+        w.allocate();
         hos_drafts d = {};
         d.n_seq = (int32_t)n_seq;
         d.n_tokens = (int32_t)n_tok;
@@ -531,17 +573,24 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         d.u_accept = ua->const_data_ptr<float>();
         d.u_sample = us->const_data_ptr<float>();
-        d.accepted = accepted.mutable_data_ptr<int32_t>();
-        d.next = next.mutable_data_ptr<int32_t>();
-        d.out_tokens = out.mutable_data_ptr<int32_t>();
-        d.status = status.mutable_data_ptr<int32_t>();
+        d.accepted = w.address(accepted);
+        d.next = w.address(next);
+        d.out_tokens = w.address(out);
+        d.status = w.address(status);
         if (len) {
             d.kv_len = len->const_data_ptr<int32_t>();
-            d.new_len = now.mutable_data_ptr<int32_t>();
+            d.new_len = w.address(now);
         }
         const int rc = p_verify(&d, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream());
-        return Py_BuildValue("iNNNNN", rc, THPVariable_Wrap(accepted), THPVariable_Wrap(next), THPVariable_Wrap(out),
-                             len ? THPVariable_Wrap(now) : Py_NewRef(Py_None), THPVariable_Wrap(status));
+        if (rc) return PyLong_FromLong(rc);
+        const Names& name = names();
+        Results r;
+        r.add(name.accepted, w.tensor(accepted, {n_seq}));
+        r.add(name.next, w.tensor(next, {n_seq}));
+        r.add(name.tokens, w.tensor(out, {n_tok}));
+        r.add(name.new_len, len ? w.tensor(now, {n_seq}) : Py_NewRef(Py_None));
+        r.add(name.status, w.tensor(status, {n_seq}));
+        return r.take();
     });
 }
 

@@ -1,5 +1,6 @@
 // The pages of a cache: who holds which, and their contents from one place to another.
 #include <algorithm>
+#include <atomic>
 
 #include "hos_cluster.cuh"
 #include "hos_kv_kernels.h"
@@ -10,40 +11,6 @@ namespace hos {
 namespace {
 
 constexpr int THREADS = 1024, WARPS = THREADS / 32;
-
-// Sum of `v` over the threads before this one in the block, and over all of it.  Contains barriers.
-__device__ __forceinline__ unsigned long long block_before(unsigned long long v, unsigned long long* scratch, unsigned long long* all) {
-    unsigned long long s = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long o = __shfl_up_sync(FULL, s, d);
-        if (lane_id() >= d) s += o;
-    }
-    __syncthreads();
-    if (lane_id() == 31) scratch[warp_id()] = s;
-    __syncthreads();
-    unsigned long long w = scratch[lane_id()];
-    const unsigned long long mine = w;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long o = __shfl_up_sync(FULL, w, d);
-        if (lane_id() >= d) w += o;
-    }
-    *all = __shfl_sync(FULL, w, 31);
-    return s - v + __shfl_sync(FULL, w - mine, warp_id());
-}
-
-// Sums of a value of every block: of those before this one, and of all.  `mine` is in shared memory, written by one thread
-// of each block before the last cluster_sync.
-struct Shares { unsigned long long before, all; };
-__device__ __forceinline__ Shares shares_of(const unsigned long long* mine) {
-    Shares s{0, 0};
-    const int rank = cluster_rank(), n = cluster_size();
-    const unsigned long long v = lane_id() < n ? read_of_block(mine, lane_id()) : 0;
-    s.all = warp_sum_u64(v);
-    s.before = warp_sum_u64(lane_id() < rank ? v : 0);
-    return s;
-}
 
 struct Range { int first, last; };
 // The part of n things that falls to this block.
@@ -58,301 +25,511 @@ __device__ __forceinline__ Range warp_part(Range block) {
 }
 __device__ __forceinline__ unsigned lanes_before() { return (1u << lane_id()) - 1u; }
 
+// Numbers of pages are added up in 32 bits.  What sequences ask for may be more than that holds; every sum stops at PLENTY, which no pool has
+// (min(a + b, PLENTY) is associative for numbers from 0 to PLENTY, and 32 of them are below 2^31).
+constexpr int PLENTY = 1 << 25;
+__device__ __forceinline__ int sum_of_warp(int v) { return (int)__reduce_add_sync(FULL, (unsigned)v); }
+__device__ __forceinline__ int sum_before_lane(int v) {
+    int s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(FULL, s, d);
+        if (lane_id() >= d) s = min(s + o, PLENTY);
+    }
+    s = __shfl_up_sync(FULL, s, 1);
+    return lane_id() == 0 ? 0 : s;
+}
+
+// What the blocks tell one another: each writes `mine`, in shared memory, by one thread before a barrier of the cluster.  One warp of a
+// block reads what the others have written (all 32 of all 16 blocks at once took 2 us).
+struct Shares { int4 before, all; };
+__device__ __forceinline__ Shares shares_of(const int4* mine, Shares* board) {
+    const int rank = cluster_rank(), n = cluster_size();
+    if (n == 1) return Shares{make_int4(0, 0, 0, 0), *mine};
+    if (warp_id() == 0) {
+        Shares s;
+        const int4 v = lane_id() < n ? read_of_block(mine, lane_id()) : make_int4(0, 0, 0, 0);
+        const bool b = lane_id() < rank;
+        s.all = make_int4(min(sum_of_warp(v.x), PLENTY), sum_of_warp(v.y), sum_of_warp(v.z), sum_of_warp(v.w));
+        s.before = make_int4(min(sum_of_warp(b ? v.x : 0), PLENTY), sum_of_warp(b ? v.y : 0), sum_of_warp(b ? v.z : 0), sum_of_warp(b ? v.w : 0));
+        if (lane_id() == 0) *board = s;
+    }
+    __syncthreads();
+    return *board;
+}
+
 __device__ __forceinline__ bool is_page(const PagesView& p, int page) { return (unsigned)page < (unsigned)p.n_pages; }
 __device__ __forceinline__ bool is_length(const PagesView& p, int len) { return len >= 0 && len <= (long long)p.max_pages * p.page_size; }
-__device__ __forceinline__ int pages_of(const PagesView& p, int len) { return (int)(((long long)len + p.page_size - 1) / p.page_size); }
+__device__ __forceinline__ int pages_of(const PagesView& p, int len) { return (int)(((unsigned)len + (unsigned)p.page_size - 1u) / (unsigned)p.page_size); }
 __device__ __forceinline__ void flag(const PagesView& p, int s) {
     if (p.status) atomicOr(p.status + s, HOS_ST_INVALID);
 }
 
-// Rows are gone through in pieces of PIECE entries, one a warp.
-constexpr int PIECE = 128;
-template <typename F> __device__ __forceinline__ void for_each_piece(const PagesView& p, Range rows, F&& f) {
-    const int pieces = max(1, (p.max_pages + PIECE - 1) / PIECE);
-    const long long n = (long long)(rows.last - rows.first) * pieces;
-    for (long long i = warp_id(); i < n; i += WARPS) {
-        const int s = rows.first + (int)(i / pieces), first = (int)(i % pieces) * PIECE;
-        f(s, first, min(first + PIECE, p.max_pages));
+// A warp's pages, 32 at a time, as masks of those whose count is zero.  The loads of AHEAD groups are on their way at once; the masks
+// of the first 32 groups stay with the lanes for a second pass (a pool of up to 32,768 pages a block is read once).
+constexpr int AHEAD = 8;
+struct FreeMasks {
+    Range part;
+    unsigned kept;                                     // of group lane_id()
+    template <typename F> __device__ __forceinline__ void first_pass(const int32_t* refs, F&& f) {
+        kept = 0;
+        for (int g0 = 0; part.first + 32 * g0 < part.last; g0 += AHEAD) {
+            int r[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = part.first + 32 * (g0 + k) + lane_id();
+                r[k] = i < part.last ? __ldcg(refs + i) : 1;
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const unsigned m = __ballot_sync(FULL, r[k] == 0);
+                if (g0 + k == lane_id()) kept = m;
+                f(part.first + 32 * (g0 + k), m);
+            }
+        }
+    }
+    // f(first page of the group, mask) until it returns false
+    template <typename F> __device__ __forceinline__ void again(const int32_t* refs, F&& f) const {
+        for (int g = 0; part.first + 32 * g < part.last; ++g) {
+            const int i0 = part.first + 32 * g, i = i0 + lane_id();
+            const unsigned m = g < 32 ? __shfl_sync(FULL, kept, g) : __ballot_sync(FULL, i < part.last && __ldcg(refs + i) == 0);
+            if (!f(i0, m)) return;
+        }
+    }
+    __device__ __forceinline__ unsigned there(int i0) const { return part.last - i0 >= 32 ? FULL : (1u << (part.last - i0)) - 1u; }
+};
+
+__device__ __forceinline__ void copy_counts(const PagesView& p, Range pages) {
+    if (p.refs == p.refs_in) return;
+    for (int i0 = pages.first + (int)threadIdx.x; i0 < pages.last; i0 += AHEAD * THREADS) {
+        int r[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * THREADS < pages.last) r[k] = p.refs_in[i0 + k * THREADS];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * THREADS < pages.last) p.refs[i0 + k * THREADS] = r[k];
+    }
+}
+
+// 32 x EACH entries of a row from `first` on, by a warp: all loads before the stores (the compiler cannot know that the tables are apart).
+constexpr int EACH = 8, PIECE = 32 * EACH;
+struct Piece { int e[EACH]; };
+__device__ __forceinline__ Piece load_piece(const int32_t* row, int first, int last) {
+    Piece x;
+    const int left = last - first - lane_id();
+    const int32_t* at = row + (first + lane_id());
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) x.e[k] = 32 * k < left ? at[32 * k] : -1;
+    return x;
+}
+__device__ __forceinline__ void store_piece(int32_t* row, int first, int last, const Piece& x) {
+    const int left = last - first - lane_id();
+    int32_t* at = row + (first + lane_id());
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (32 * k < left) at[32 * k] = x.e[k];
+}
+
+// Part of a row to be gone through: of sequence `seq`, entries first to last - 1.
+struct RowWork { int seq, first, last, from; };
+// A list of row parts that the threads of a block make together and its warps go through, piece by piece: the next piece's entries
+// are on their way while one is worked on, the first already before a barrier of the blocks where there is one in between.
+struct RowList {
+    RowWork row[THREADS];
+    int n, pieces;                                     // row parts; pieces of the longest (at least)
+
+    __device__ __forceinline__ void begin(int at_least) {
+        if (threadIdx.x == 0) n = 0, pieces = at_least;
+        __syncthreads();
+    }
+    __device__ __forceinline__ void add(const RowWork& r) {
+        row[atomicAdd(&n, 1)] = r;
+        const int need = (r.last - r.first + PIECE - 1) / PIECE;
+        if (need > 1) atomicMax(&pieces, need);
+    }
+};
+struct Cursor { int r, c; Piece next; };               // of a warp: its next piece, c of row part r
+// load(row part, first entry)
+template <typename L> __device__ __forceinline__ Cursor first_piece(const RowList& list, L&& load) {
+    __syncthreads();
+    Cursor at;
+    const int pieces = list.pieces;
+    at.r = pieces ? warp_id() / pieces : list.n;
+    at.c = warp_id() - at.r * pieces;
+    if (at.r < list.n) at.next = load(list.row[at.r], list.row[at.r].first + at.c * PIECE);
+    return at;
+}
+// work(row part, first entry, piece)
+template <typename L, typename W> __device__ __forceinline__ void all_pieces(const RowList& list, Cursor at, L&& load, W&& work) {
+    const int rows = list.n, pieces = list.pieces;
+    if (at.r >= rows) return;
+    const int step_rows = WARPS / pieces, step = WARPS - step_rows * pieces;
+    RowWork now = list.row[at.r];
+    while (true) {
+        const int j = now.first + at.c * PIECE;
+        const RowWork then = now;
+        const Piece x = at.next;
+        at.r += step_rows;
+        at.c += step;
+        if (at.c >= pieces) at.c -= pieces, ++at.r;
+        const bool more = at.r < rows;
+        if (more) {
+            now = list.row[at.r];
+            at.next = load(now, now.first + at.c * PIECE);
+        }
+        work(then, j, x);
+        if (!more) return;
     }
 }
 
 // ---- resize ------------------------------------------------------------------------------------------------------------
-constexpr unsigned long long GROWS = 1ull << 63, SPLITS = 1ull << 62, ONE_SPLIT = 1ull << 43, TAKES = ONE_SPLIT - 1;
+constexpr int GROWS = 1 << 30, SPLITS = 1 << 29, TAKES = SPLITS - 1;
 
-struct Change { int old, now; bool valid; };
+struct Change {
+    int old, now;
+    bool valid;
+    int page;                  // that the sequence grows from the inside of; -1: none, -2: none that exists
+};
 __device__ __forceinline__ Change change_of(const PagesView& p, int s) {
     Change c;
     c.old = p.len_in[s];
     c.now = p.change[s];
     c.valid = is_length(p, c.old) && is_length(p, c.now);
+    c.page = -1;
+    if (c.valid && c.now > c.old) {
+        const unsigned at = (unsigned)c.old / (unsigned)p.page_size;
+        if (at * (unsigned)p.page_size != (unsigned)c.old) {
+            c.page = p.table_in[(long long)s * p.in_stride + at];
+            if (!is_page(p, c.page)) c.page = -2;
+        }
+    }
     return c;
-}
-// The page that a sequence grows from the inside of; -1: none.
-__device__ __forceinline__ int grown_page(const PagesView& p, int s, const Change& c) {
-    if (!c.valid || c.now <= c.old || c.old % p.page_size == 0) return -1;
-    const int page = p.table_in[(long long)s * p.in_stride + c.old / p.page_size];
-    return is_page(p, page) ? page : -2;
 }
 
 __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant__ PagesView p) {
-    __shared__ unsigned long long scratch[WARPS], mine[2], warp_free[WARPS];
+    __shared__ int4 mine;
+    __shared__ Shares board;
+    __shared__ int of_warp[3][WARPS];
+    __shared__ RowList stay, go;
     pdl_launch_dependents();
     pdl_wait();
     const Range seqs = block_part(p.n_seq), pages = block_part(p.n_pages);
-    const Range part = warp_part(pages);
     const int tid = (int)threadIdx.x;
-    // the new counts begin as the old ones; what is known of pages that are grown from, as nothing
-    if (p.refs != p.refs_in)
-        for (int i = pages.first + tid; i < pages.last; i += THREADS) p.refs[i] = p.refs_in[i];
-    for (int s = seqs.first + tid; s < seqs.last; s += THREADS) {
-        const Change c = change_of(p, s);
-        p.src[s] = p.dst[s] = -1;
-        const int page = grown_page(p, s, c);
-        if (page >= 0) p.growers[page] = 0, p.latest[page] = -1;
-        if (p.status) p.status[s] = c.valid && page != -2 ? 0 : HOS_ST_INVALID;
-    }
-    cluster_sync();
-    // pages given up; how many sequences grow from the inside of a page, and the last of them
-    for (int s = seqs.first + warp_id(); s < seqs.last; s += WARPS) {
-        const Change c = change_of(p, s);
-        if (!c.valid) continue;
-        for (int j = pages_of(p, c.now) + lane_id(); j < pages_of(p, c.old); j += 32) {
-            const int page = p.table_in[(long long)s * p.in_stride + j];
-            if (!is_page(p, page) || atomicSub(p.refs + page, 1) <= 0) flag(p, s);
+    const bool in_place = p.table == p.table_in;
+    auto old_row = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.seq * p.in_stride, j, r.last); };
+    auto keep = [&](const RowWork& r, int j, const Piece& x) { store_piece(p.table + (long long)r.seq * p.out_stride, j, p.max_pages, x); };
+    auto give_up = [&](const RowWork& r, int j, const Piece& x) {
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (32 * k < r.last - j - lane_id()) bad |= !is_page(p, x.e[k]) || atomicSub(p.refs + x.e[k], 1) <= 0;
+        if (bad) flag(p, r.seq);
+        if (in_place) store_piece(p.table + (long long)r.seq * p.out_stride, j, r.last, Piece{{-1, -1, -1, -1, -1, -1, -1, -1}});
+    };
+    auto list_of_gone = [&](const Change& c, int s) {
+        if (c.valid && c.now < c.old) {
+            const int have = pages_of(p, c.old), need = pages_of(p, c.now);
+            if (need < have) go.add(RowWork{s, need, have, 0});
         }
-        const int page = lane_id() == 0 ? grown_page(p, s, c) : -1;
-        if (page >= 0) {
-            atomicAdd(p.growers + page, 1);
-            atomicMax(p.latest + page, s);
+    };
+    // the new counts begin as the old ones; what is known of shared pages that are grown from, as nothing; rows of tables apart are copied
+    // as far as they stay
+    Change first = {};                                 // of this thread's first sequence
+    if (seqs.first + tid < seqs.last) first = change_of(p, seqs.first + tid);
+    copy_counts(p, pages);
+    go.begin(1);
+    for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
+        stay.begin((p.max_pages + PIECE - 1) / PIECE);
+        const int s = s0 + tid;
+        const Change c = s0 == seqs.first ? first : s < seqs.last ? change_of(p, s) : Change{};
+        if (s < seqs.last) {
+            if (!in_place) stay.add(RowWork{s, 0, c.valid ? pages_of(p, min(c.old, c.now)) : p.max_pages, 0});
+            if (s0 == seqs.first) list_of_gone(c, s);
+            p.src[s] = p.dst[s] = -1;
         }
+        if (!in_place) all_pieces(stay, first_piece(stay, old_row), old_row, keep);
+        if (s < seqs.last) {
+            if (p.status) p.status[s] = c.valid && c.page != -2 ? 0 : HOS_ST_INVALID;
+            if (c.page >= 0 && p.refs_in[c.page] > 1) p.growers[c.page] = 0, p.latest[c.page] = -1;
+        }
+        if (s0 + THREADS < seqs.last) __syncthreads();
     }
-    cluster_sync();
-    // what each sequence takes, with sums in order; how many pages are free
-    unsigned long long sum = 0;
+    Cursor gone = first_piece(go, old_row);
+    cluster_or_block_sync();
+    // pages given up; how many sequences grow from the inside of a shared page, and the last of them
     for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
         const int s = s0 + tid;
-        unsigned long long takes = 0, flags = 0;
-        ResizePlan plan{0, 0, 0};
+        if (s0 > seqs.first) {
+            __syncthreads();
+            go.begin(1);
+        }
         if (s < seqs.last) {
-            const Change c = change_of(p, s);
-            plan.have = c.valid ? pages_of(p, c.old) : p.max_pages;
-            plan.need = c.valid ? pages_of(p, c.now) : p.max_pages;
+            const Change c = s0 == seqs.first ? first : change_of(p, s);
+            if (c.page >= 0 && __ldcg(p.refs_in + c.page) > 1) {
+                atomicAdd(p.growers + c.page, 1);
+                atomicMax(p.latest + c.page, s);
+            }
+            if (s0 > seqs.first) list_of_gone(c, s);
+        }
+        if (s0 > seqs.first) gone = first_piece(go, old_row);
+        all_pieces(go, gone, old_row, give_up);
+    }
+    cluster_or_block_sync();
+    // how many pages are free; what each sequence takes, with sums in order
+    FreeMasks masks{warp_part(pages), 0};
+    int n_free = 0;
+    masks.first_pass(p.refs, [&](int, unsigned m) { n_free += __popc(m); });
+    if (lane_id() == 0) of_warp[2][warp_id()] = n_free;
+    int sum_takes = 0, sum_splits = 0;
+    ResizePlan of_first = {0, 0, 0};
+    for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
+        const int s = s0 + tid;
+        ResizePlan plan = {0, 0, 0};
+        if (s < seqs.last) {
+            const Change c = s0 == seqs.first ? first : change_of(p, s);
             if (c.valid && c.now > c.old) {
-                flags = GROWS;
-                takes = min(plan.need - plan.have, p.n_pages + 1);
-                const int page = grown_page(p, s, c);
-                if (page >= 0) {
-                    const int refs = __ldcg(p.refs + page);
-                    if (refs > 1 && !(__ldcg(p.growers + page) == refs && __ldcg(p.latest + page) == s)) {
-                        flags |= SPLITS;
-                        takes += ONE_SPLIT + 1;
-                    }
+                plan.takes = GROWS | min(pages_of(p, c.now) - pages_of(p, c.old), PLENTY - 1);
+                if (c.page >= 0) {
+                    const int refs = __ldcg(p.refs + c.page);
+                    if (refs > 1 && !(__ldcg(p.growers + c.page) == refs && __ldcg(p.latest + c.page) == s)) plan.takes = (plan.takes + 1) | SPLITS;
                 }
             }
         }
-        unsigned long long all;
-        plan.before = sum + block_before(takes, scratch, &all) + flags;
-        if (s < seqs.last) p.plan[s] = plan;
-        sum += all;
+        const unsigned split = __ballot_sync(FULL, plan.takes & SPLITS);
+        const int before = sum_before_lane(plan.takes & TAKES), all = min(before + (plan.takes & TAKES), PLENTY);
+        if (lane_id() == 31) of_warp[0][warp_id()] = all, of_warp[1][warp_id()] = __popc(split);
+        __syncthreads();
+        const int t = of_warp[0][lane_id()], u = of_warp[1][lane_id()];
+        const bool b = lane_id() < warp_id();
+        plan.before = min(sum_takes + min(sum_of_warp(b ? t : 0), PLENTY) + before, PLENTY);
+        plan.splits_before = sum_splits + sum_of_warp(b ? u : 0) + __popc(split & lanes_before());
+        sum_takes = min(sum_takes + min(sum_of_warp(t), PLENTY), PLENTY);
+        sum_splits += sum_of_warp(u);
+        if (s0 == seqs.first) of_first = plan;
+        else if (s < seqs.last) p.plan[s] = plan;
+        if (s0 + THREADS < seqs.last) __syncthreads();
     }
-    unsigned n_free = 0;
-    for (int i0 = part.first; i0 < part.last; i0 += 32) {
-        const int i = i0 + lane_id();
-        n_free += __popc(__ballot_sync(FULL, i < part.last && __ldcg(p.refs + i) == 0));
-    }
-    if (lane_id() == 0) warp_free[warp_id()] = n_free;
     __syncthreads();
+    const int free_of_lane = of_warp[2][lane_id()];
     if (warp_id() == 0) {
-        const unsigned long long all = warp_sum_u64(warp_free[lane_id()]);
-        if (lane_id() == 0) mine[0] = sum, mine[1] = all;
+        const int all = sum_of_warp(free_of_lane);
+        if (lane_id() == 0) mine = make_int4(sum_takes, sum_splits, all, 0);
     }
-    cluster_sync();
-    const Shares takes = shares_of(mine), free = shares_of(mine + 1);
+    cluster_or_block_sync();
+    const Shares shares = shares_of(&mine, &board);
+    const int wanted = shares.all.x, free = shares.all.z;
+    if (tid == 0 && cluster_rank() == 0 && wanted <= free) *p.count = shares.all.y;
     // the free pages in order, as many as are taken
-    const unsigned long long wanted = takes.all & TAKES;
-    unsigned long long at = free.before + warp_sum_u64(lane_id() < warp_id() ? warp_free[lane_id()] : 0);
-    for (int i0 = part.first; i0 < part.last && at < wanted; i0 += 32) {
-        const int i = i0 + lane_id();
-        const bool is_free = i < part.last && __ldcg(p.refs + i) == 0;
-        const unsigned m = __ballot_sync(FULL, is_free);
-        const unsigned long long k = at + __popc(m & lanes_before());
-        if (is_free && k < wanted) p.queue[k] = i;
-        at += __popc(m);
+    int at = shares.before.z + sum_of_warp(lane_id() < warp_id() ? free_of_lane : 0);
+    if (at < wanted)
+        masks.again(p.refs, [&](int i0, unsigned m) {
+            const int k = at + __popc(m & lanes_before());
+            if ((m >> lane_id() & 1u) && k < wanted) p.queue[k] = i0 + lane_id();
+            at += __popc(m);
+            return at < wanted;
+        });
+    cluster_or_block_sync();
+    // lengths, and the pages that rows get
+    auto taken = [&](const RowWork& r, int j) { return load_piece(p.queue + r.from, j, r.last); };
+    for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
+        go.begin(1);
+        const int s = s0 + tid;
+        if (s < seqs.last) {
+            const Change c = s0 == seqs.first ? first : change_of(p, s);
+            const ResizePlan plan = s0 == seqs.first ? of_first : p.plan[s];
+            const int base = min(shares.before.x + plan.before, PLENTY), takes = plan.takes & TAKES, splits = shares.before.y + plan.splits_before;
+            const bool short_of = (plan.takes & GROWS) && base + takes > free;
+            if (short_of) {
+                // the first sequence whose pages are not there: the splits before it are those that are made
+                if (base <= free) *p.count = splits;
+                if (p.status) atomicOr(p.status + s, HOS_ST_PAGES);
+            } else if (takes) {
+                const int split = (plan.takes & SPLITS) != 0, have = pages_of(p, c.old);
+                go.add(RowWork{s, have - split, pages_of(p, c.now), base - (have - split)});
+                if (split) {
+                    atomicSub(p.refs + c.page, 1);
+                    p.src[splits] = c.page;
+                    p.dst[splits] = __ldcg(p.queue + base);
+                }
+            }
+            p.len[s] = c.valid && !short_of ? c.now : c.old;
+        }
+        all_pieces(go, first_piece(go, taken), taken, [&](const RowWork& r, int j, const Piece& x) {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (x.e[k] >= 0) p.refs[x.e[k]] = 1;
+            store_piece(p.table + (long long)r.seq * p.out_stride, j, r.last, x);
+        });
+        if (s0 + THREADS < seqs.last) __syncthreads();
     }
-    cluster_sync();
-    // rows
-    const bool in_place = p.table == p.table_in;
-    if (tid == 0 && cluster_rank() == 0 && (takes.all & TAKES) <= free.all) *p.count = (int)(takes.all >> 43);
-    for_each_piece(p, seqs, [&](int s, int first, int last) {
-        const ResizePlan plan = p.plan[s];
-        const unsigned long long before = takes.before + (plan.before & ~(GROWS | SPLITS)), base = before & TAKES;
-        const int split = (plan.before & SPLITS) != 0;
-        const unsigned long long mine = plan.before & GROWS ? (unsigned long long)min(plan.need - plan.have, p.n_pages + 1) + split : 0;
-        const bool short_of = (plan.before & GROWS) && base + mine > free.all;
-        const int have = plan.have, need = short_of ? have : plan.need, kept = min(have, need), splits_at = split && !short_of ? have - 1 : -1;
-        const int32_t* in = p.table_in + (long long)s * p.in_stride;
-        int32_t* out = p.table + (long long)s * p.out_stride;
-        int a = first, b = last;
-        if (in_place) a = max(a, splits_at >= 0 ? splits_at : kept), b = min(b, max(have, need));
-        for (int j = a + lane_id(); j < b; j += 32) {
-            int e = -1;
-            if (j == splits_at || (j >= have && j < need)) {
-                e = __ldcg(p.queue + base + (j == splits_at ? 0 : split + j - have));
-                p.refs[e] = 1;
-            } else if (j < kept) {
-                e = in[j];
-            }
-            if (j == splits_at) {
-                const int k = (int)(before >> 43), page = in[j];
-                atomicSub(p.refs + page, 1);
-                p.src[k] = page;
-                p.dst[k] = e;
-            }
-            out[j] = e;
-        }
-        if (first == 0 && lane_id() == 0) {
-            // the first sequence whose pages are not there: the splits before it are those that are made
-            if (short_of && base <= free.all) *p.count = (int)(before >> 43);
-            if (short_of && p.status) atomicOr(p.status + s, HOS_ST_PAGES);
-            if (!(plan.before & GROWS) || !short_of) {
-                const Change c = change_of(p, s);
-                p.len[s] = c.valid ? c.now : c.old;
-            } else if (p.len != p.len_in) {
-                p.len[s] = p.len_in[s];
-            }
-        }
-    });
 }
 
 // ---- fork --------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ int parent_of(const PagesView& p, int i) {
+__device__ __forceinline__ int parent_of(const PagesView& p, int i, int* len) {
     const int s = p.change[i];
-    return s >= 0 && s < p.n_seq && is_length(p, p.len_in[s]) ? s : s == -1 ? -1 : -2;
+    *len = 0;
+    if (s == -1) return -1;
+    if (s < 0 || s >= p.n_seq) return -2;
+    const int n = p.len_in[s];
+    if (!is_length(p, n)) return -2;
+    *len = n;
+    return s;
 }
 
 __global__ void __launch_bounds__(THREADS, 1) k_kv_fork(const __grid_constant__ PagesView p) {
+    __shared__ int children[THREADS];
+    __shared__ RowList list, held;
     pdl_launch_dependents();
     pdl_wait();
-    const Range seqs = block_part(p.n_seq), outs = block_part(p.n_out), pages = block_part(p.n_pages);
+    const Range seqs = block_part(p.n_seq), outs = block_part(p.n_out);
     const int tid = (int)threadIdx.x;
-    if (p.refs != p.refs_in)
-        for (int i = pages.first + tid; i < pages.last; i += THREADS) p.refs[i] = p.refs_in[i];
-    for (int s = seqs.first + tid; s < seqs.last; s += THREADS) p.children[s] = 0;
-    for (int i = outs.first + tid; i < outs.last; i += THREADS) {
-        const int s = parent_of(p, i);
-        p.len[i] = s >= 0 ? p.len_in[s] : 0;
-        if (p.status) p.status[i] = s == -2 ? HOS_ST_INVALID : 0;
-    }
-    cluster_sync();
-    for (int i = outs.first + tid; i < outs.last; i += THREADS) {
-        const int s = parent_of(p, i);
-        if (s >= 0) atomicAdd(p.children + s, 1);
-    }
-    for_each_piece(p, outs, [&](int i, int first, int last) {
-        const int s = parent_of(p, i), have = s >= 0 ? pages_of(p, p.len_in[s]) : 0;
-        for (int j = first + lane_id(); j < last; j += 32) {
-            int e = -1;
-            if (j < have) {
-                e = p.table_in[(long long)s * p.in_stride + j];
-                if (!is_page(p, e)) flag(p, i);
-            }
-            p.table[(long long)i * p.out_stride + j] = e;
+    auto row_of_parent = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.from * p.in_stride, j, r.last); };
+    auto row = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.seq * p.in_stride, j, r.last); };
+    copy_counts(p, block_part(p.n_pages));
+    for (int i0 = outs.first; i0 < outs.last; i0 += THREADS) {
+        list.begin((p.max_pages + PIECE - 1) / PIECE);
+        const int i = i0 + tid;
+        if (i < outs.last) {
+            int len;
+            const int s = parent_of(p, i, &len);
+            p.len[i] = len;
+            if (p.status) p.status[i] = s == -2 ? HOS_ST_INVALID : 0;
+            list.add(RowWork{i, 0, pages_of(p, len), s});
         }
-    });
-    cluster_sync();
-    for_each_piece(p, seqs, [&](int s, int first, int last) {
-        const int more = __ldcg(p.children + s) - 1, len = p.len_in[s];
-        if (more == 0 || !is_length(p, len)) return;
-        for (int j = first + lane_id(); j < min(last, pages_of(p, len)); j += 32) {
-            const int page = p.table_in[(long long)s * p.in_stride + j];
-            if (is_page(p, page)) atomicAdd(p.refs + page, more);
+        all_pieces(list, first_piece(list, row_of_parent), row_of_parent, [&](const RowWork& r, int j, const Piece& x) {
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) bad |= 32 * k < r.last - j - lane_id() && !is_page(p, x.e[k]);
+            if (bad) flag(p, r.seq);
+            store_piece(p.table + (long long)r.seq * p.out_stride, j, p.max_pages, x);
+        });
+        if (i0 + THREADS < outs.last) __syncthreads();
+    }
+    // the counts: every block looks through all parents for its own sequences' children
+    for (int s0 = seqs.first; s0 == seqs.first || s0 < seqs.last; s0 += THREADS) {
+        if (s0 > seqs.first) __syncthreads();
+        children[tid] = 0;
+        held.begin(1);
+        for (int i0 = tid; i0 < p.n_out; i0 += AHEAD * THREADS) {
+            int s[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) s[k] = i0 + k * THREADS < p.n_out ? p.change[i0 + k * THREADS] : -1;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (s[k] >= s0 && s[k] < min(s0 + THREADS, seqs.last)) atomicAdd(children + s[k] - s0, 1);
         }
-    });
+        const int len = s0 + tid < seqs.last ? p.len_in[s0 + tid] : -1;
+        __syncthreads();
+        const int more = children[tid] - 1;
+        if (is_length(p, len) && len > 0 && more != 0) held.add(RowWork{s0 + tid, 0, pages_of(p, len), more});
+        const Cursor at = first_piece(held, row);
+        if (s0 == seqs.first) cluster_or_block_sync();         // the counts have been copied
+        all_pieces(held, at, row, [&](const RowWork& r, int, const Piece& x) {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (is_page(p, x.e[k])) atomicAdd(p.refs + x.e[k], r.from);
+        });
+    }
 }
 
 // ---- compact -----------------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant__ PagesView p) {
-    __shared__ unsigned long long mine[3], warp_live[WARPS], warp_late[WARPS], warp_hole[WARPS];
+    __shared__ int4 live, others;
+    __shared__ Shares board[2];
+    __shared__ int of_warp[3][WARPS];
+    __shared__ RowList list;
     pdl_launch_dependents();
     pdl_wait();
     const Range seqs = block_part(p.n_seq), pages = block_part(p.n_pages);
-    const Range part = warp_part(pages);
     const int tid = (int)threadIdx.x;
-    unsigned n = 0;
-    for (int i0 = part.first; i0 < part.last; i0 += 32) {
-        const int i = i0 + lane_id();
-        n += __popc(__ballot_sync(FULL, i < part.last && p.refs_in[i] != 0));
-    }
-    if (lane_id() == 0) warp_live[warp_id()] = n;
-    __syncthreads();
-    if (warp_id() == 0) {
-        const unsigned long long all = warp_sum_u64(warp_live[lane_id()]);
-        if (lane_id() == 0) mine[0] = all;
-    }
-    cluster_sync();
-    const int n_live = (int)shares_of(mine).all;
-    // pages in use behind the first n_live, and free ones among those: as many of the one as of the other
-    unsigned late = 0, hole = 0;
-    for (int i0 = part.first; i0 < part.last; i0 += 32) {
-        const int i = i0 + lane_id();
-        const bool there = i < part.last, live = there && p.refs_in[i] != 0;
-        late += __popc(__ballot_sync(FULL, live && i >= n_live));
-        hole += __popc(__ballot_sync(FULL, there && !live && i < n_live));
-    }
-    if (lane_id() == 0) warp_late[warp_id()] = late, warp_hole[warp_id()] = hole;
-    __syncthreads();
-    if (warp_id() == 0) {
-        const unsigned long long a = warp_sum_u64(warp_late[lane_id()]), b = warp_sum_u64(warp_hole[lane_id()]);
-        if (lane_id() == 0) mine[1] = a, mine[2] = b;
-    }
-    cluster_sync();
-    const Shares lates = shares_of(mine + 1), holes = shares_of(mine + 2);
-    int late_at = (int)(lates.before + warp_sum_u64(lane_id() < warp_id() ? warp_late[lane_id()] : 0));
-    int hole_at = (int)(holes.before + warp_sum_u64(lane_id() < warp_id() ? warp_hole[lane_id()] : 0));
-    const int count = (int)lates.all;
-    for (int i0 = part.first; i0 < part.last; i0 += 32) {
-        const int i = i0 + lane_id();
-        const bool there = i < part.last;
-        const int refs = there ? p.refs_in[i] : 0;
-        const bool is_late = refs != 0 && i >= n_live, is_hole = there && refs == 0 && i < n_live;
-        const unsigned a = __ballot_sync(FULL, is_late), b = __ballot_sync(FULL, is_hole);
-        if (is_late) p.src[late_at + __popc(a & lanes_before())] = i;
-        if (is_hole) p.dst[hole_at + __popc(b & lanes_before())] = i;
-        if (there && i >= n_live) p.growers[i] = is_late ? late_at + __popc(a & lanes_before()) : -1;
-        if (there && i >= count) p.src[i] = p.dst[i] = -1;
-        if (there && p.refs != p.refs_in) p.refs[i] = refs;
-        late_at += __popc(a);
-        hole_at += __popc(b);
-    }
-    if (tid == 0 && cluster_rank() == 0) *p.count = count;
+    const bool in_place = p.table == p.table_in;
+    auto row = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.seq * p.in_stride, j, r.last); };
+    auto list_row = [&](int s, int len) {
+        const bool valid = is_length(p, len);
+        if (valid || !in_place) list.add(RowWork{s, 0, valid ? pages_of(p, len) : p.max_pages, valid});
+    };
+    FreeMasks masks{warp_part(pages), 0};
+    int n = 0;
+    masks.first_pass(p.refs_in, [&](int i0, unsigned m) {
+        if (i0 < masks.part.last) n += __popc(masks.there(i0) & ~m);
+    });
+    if (lane_id() == 0) of_warp[0][warp_id()] = n;
+    copy_counts(p, pages);
     for (int s = seqs.first + tid; s < seqs.last; s += THREADS)
         if (p.status) p.status[s] = is_length(p, p.len_in[s]) ? 0 : HOS_ST_INVALID;
-    cluster_sync();
-    for (int k = cluster_rank() * THREADS + tid; k < count; k += cluster_size() * THREADS) {
-        const int a = __ldcg(p.src + k), b = __ldcg(p.dst + k);
-        const int refs = p.refs_in[a];
-        p.refs[b] = refs;
-        p.refs[a] = 0;
+    __syncthreads();
+    if (warp_id() == 0) {
+        const int all = sum_of_warp(of_warp[0][lane_id()]);
+        if (lane_id() == 0) live = make_int4(0, 0, 0, all);
     }
-    const bool in_place = p.table == p.table_in;
-    for_each_piece(p, seqs, [&](int s, int first, int last) {
-        const int len = p.len_in[s];
-        const bool valid = is_length(p, len);
-        const int have = valid ? pages_of(p, len) : p.max_pages;
-        for (int j = first + lane_id(); j < (in_place ? min(last, have) : last); j += 32) {
-            int e = -1;
-            if (j < have) {
-                e = p.table_in[(long long)s * p.in_stride + j];
-                if (valid) {
-                    const bool ok = is_page(p, e);
-                    const int k = ok && e >= n_live ? __ldcg(p.growers + e) : -1;
-                    if (!ok || (e >= n_live && k < 0)) flag(p, s);
-                    if (k >= 0) e = __ldcg(p.dst + k);
-                }
-            }
-            p.table[(long long)s * p.out_stride + j] = e;
-        }
+    cluster_or_block_sync();
+    const int n_live = shares_of(&live, &board[0]).all.w;
+    // pages in use behind the first n_live, and free ones among those: as many of the one as of the other
+    auto behind = [&](int i0) { return i0 >= n_live ? FULL : n_live - i0 >= 32 ? 0u : FULL << (n_live - i0); };
+    int late = 0, hole = 0;
+    masks.again(p.refs_in, [&](int i0, unsigned m) {
+        late += __popc(masks.there(i0) & ~m & behind(i0));
+        hole += __popc(m & ~behind(i0));
+        return true;
     });
+    if (lane_id() == 0) of_warp[1][warp_id()] = late, of_warp[2][warp_id()] = hole;
+    __syncthreads();
+    const int late_of_lane = of_warp[1][lane_id()], hole_of_lane = of_warp[2][lane_id()];
+    if (warp_id() == 0) {
+        const int a = sum_of_warp(late_of_lane), b = sum_of_warp(hole_of_lane);
+        if (lane_id() == 0) others = make_int4(0, a, b, 0);
+    }
+    cluster_or_block_sync();
+    const Shares shares = shares_of(&others, &board[1]);
+    const bool b = lane_id() < warp_id();
+    int late_at = shares.before.y + sum_of_warp(b ? late_of_lane : 0), hole_at = shares.before.z + sum_of_warp(b ? hole_of_lane : 0);
+    const int count = shares.all.y;
+    masks.again(p.refs_in, [&](int i0, unsigned m) {
+        const int i = i0 + lane_id();
+        const unsigned a = masks.there(i0) & ~m & behind(i0), h = m & ~behind(i0), me = 1u << lane_id();
+        const int k = late_at + __popc(a & lanes_before());
+        if (a & me) p.src[k] = i;
+        if (h & me) p.dst[hole_at + __popc(h & lanes_before())] = i;
+        if (a & me) {                                  // its count goes with it, by way of the workspace: the pools may be the same
+            p.queue[k] = p.refs_in[i];
+            p.refs[i] = 0;
+        }
+        if (i >= n_live && i < masks.part.last) p.growers[i] = a & me ? k : -1;
+        late_at += __popc(a);
+        hole_at += __popc(h);
+        return true;
+    });
+    for (int i = max(count, pages.first) + tid; i < pages.last; i += THREADS) p.src[i] = p.dst[i] = -1;
+    if (tid == 0 && cluster_rank() == 0) *p.count = count;
+    list.begin(in_place ? 1 : (p.max_pages + PIECE - 1) / PIECE);
+    if (seqs.first + tid < seqs.last) list_row(seqs.first + tid, p.len_in[seqs.first + tid]);
+    Cursor at = first_piece(list, row);
+    cluster_or_block_sync();
+    for (int k = cluster_rank() * THREADS + tid; k < count; k += cluster_size() * THREADS) p.refs[__ldcg(p.dst + k)] = __ldcg(p.queue + k);
+    for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
+        if (s0 > seqs.first) {
+            __syncthreads();
+            list.begin(in_place ? 1 : (p.max_pages + PIECE - 1) / PIECE);
+            if (s0 + tid < seqs.last) list_row(s0 + tid, p.len_in[s0 + tid]);
+            at = first_piece(list, row);
+        }
+        all_pieces(list, at, row, [&](const RowWork& r, int j, Piece x) {
+            int to[EACH];
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const bool there = r.from && 32 * k < r.last - j - lane_id(), page = is_page(p, x.e[k]), moves = there && page && x.e[k] >= n_live;
+                to[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
+                bad |= there && (!page || (moves && to[k] < 0));
+            }
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (to[k] >= 0) x.e[k] = __ldcg(p.dst + to[k]);
+            if (bad) flag(p, r.seq);
+            store_piece(p.table + (long long)r.seq * p.out_stride, j, in_place ? r.last : p.max_pages, x);
+        });
+    }
 }
 
 // ---- copy --------------------------------------------------------------------------------------------------------------
@@ -392,30 +569,31 @@ __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_pages(const __grid_con
     }
 }
 
-template <typename K> cudaError_t launch_cluster(const char* name, K kernel, int blocks, const PagesView& p, cudaStream_t st) {
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)blocks;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    launch_hook(name, 0, st);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
-    launch_hook(name, 1, st);
-    return e;
+// A small state by one block, whose own barrier is enough; any other by a cluster of 16, the most there are (its barriers take 0.5-1 us
+// each, one block 0.1-0.2 us for a thousand entries).  One block, 2, 4, 8, 16, us: 16 sequences of 33 entries 5.7, 7.3, 7.4, 7.6, 7.8 (resize);
+// 128 of 519, 11,612 pages 19, 16, 15, 13, 13 (resize); 128 of 1,031, twice 38, 24, 15, 10, 8 (fork), 256 of those 137, 74, 40, 24, 16 (compact).
+constexpr long long SMALL_STATE = 8192;
+constexpr int MOST_BLOCKS = 16;
+template <void (*KERNEL)(PagesView)> cudaError_t launch_tables(const char* name, const PagesView& p, cudaStream_t st) {
+    const long long rows = p.n_seq > p.n_out ? p.n_seq : p.n_out;
+    const int blocks = p.n_pages + rows * p.max_pages <= SMALL_STATE ? 1 : MOST_BLOCKS;
+    if (blocks > 8) {                                  // has to be asked for, once a device
+        static std::atomic<unsigned long long> asked{0};
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess && (dev >= 64 || !(asked.load() >> dev & 1)))
+            e = cudaFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) asked.fetch_or(1ull << dev);
+    }
+    return launch_clusters(name, KERNEL, blocks, blocks, THREADS, st, p);
 }
 
 }  // namespace
 
-cudaError_t launch_kv_resize(const PagesView& p, cudaStream_t st) { return launch_cluster("k_kv_resize", k_kv_resize, 1, p, st); }
-cudaError_t launch_kv_fork(const PagesView& p, cudaStream_t st) { return launch_cluster("k_kv_fork", k_kv_fork, 1, p, st); }
-cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st) { return launch_cluster("k_kv_compact", k_kv_compact, 1, p, st); }
+cudaError_t launch_kv_resize(const PagesView& p, cudaStream_t st) { return launch_tables<k_kv_resize>("k_kv_resize", p, st); }
+cudaError_t launch_kv_fork(const PagesView& p, cudaStream_t st) { return launch_tables<k_kv_fork>("k_kv_fork", p, st); }
+cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st) { return launch_tables<k_kv_compact>("k_kv_compact", p, st); }
 
 cudaError_t launch_kv_copy_pages(const CopyView& c, cudaStream_t st) {
     const long long per = 2 * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT + (c.scale_bytes + COPY_UNIT - 1) / COPY_UNIT);

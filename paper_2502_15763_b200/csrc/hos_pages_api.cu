@@ -37,21 +37,20 @@ bool tables_agree(const hos_kv_pages* a, const hos_kv_pages* b) {
 }
 int check_moves(const hos_kv_moves* m) { return m && m->src && m->dst && m->count ? HOS_OK : HOS_E_INVALID; }
 
-size_t carve(PagesView& v, bool resize, bool fork, bool compact, void* ws) {
+size_t carve(PagesView& v, bool resize, void* ws) {
     unsigned char* base = static_cast<unsigned char*>(ws);
     size_t off = 0;
-    auto take = [&](bool wanted, size_t bytes) -> void* {
-        if (!wanted) return nullptr;
+    auto take = [&](size_t bytes) -> void* {
         void* p = base + off;
         off += (bytes + 255) & ~(size_t)255;
         return p;
     };
     const size_t pages = (size_t)v.n_pages * 4;
-    v.growers = static_cast<int32_t*>(take(resize || compact, pages));
-    v.latest = static_cast<int32_t*>(take(resize, pages));
-    v.queue = static_cast<int32_t*>(take(resize, pages));
-    v.plan = static_cast<ResizePlan*>(take(resize, (size_t)v.n_seq * sizeof(ResizePlan)));
-    v.children = static_cast<int32_t*>(take(fork, (size_t)v.n_seq * 4));
+    v.growers = static_cast<int32_t*>(take(pages));
+    v.queue = static_cast<int32_t*>(take(pages));
+    if (!resize) return off;
+    v.latest = static_cast<int32_t*>(take(pages));
+    v.plan = static_cast<ResizePlan*>(take((size_t)v.n_seq * sizeof(ResizePlan)));
     return off;
 }
 
@@ -73,16 +72,14 @@ PagesView view(const hos_kv_pages* in, const hos_kv_pages* out) {
     return v;
 }
 
-size_t workspace(const hos_kv_pages* in, bool resize, bool fork, bool compact) {
+size_t workspace(const hos_kv_pages* in, bool resize) {
     if (check_sizes(in)) return 0;
     PagesView v = {};
     v.n_pages = in->n_pages;
     v.n_seq = in->n_seq;
-    return carve(v, resize, fork, compact, nullptr);
+    return carve(v, resize, nullptr);
 }
-bool fits(size_t need, const void* ws, size_t ws_bytes) {
-    return need == 0 || (ws && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255) == 0);
-}
+bool fits(size_t need, const void* ws, size_t ws_bytes) { return ws && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255) == 0; }
 
 // Caches that pages can be copied between as they are, and the bytes of a page.
 int check_layer(const hos_kv_cache* c) {
@@ -107,9 +104,8 @@ int check_layer(const hos_kv_cache* c) {
 
 extern "C" {
 
-size_t hos_kv_resize_workspace_bytes(const hos_kv_pages* in) { return workspace(in, true, false, false); }
-size_t hos_kv_fork_workspace_bytes(const hos_kv_pages* in) { return workspace(in, false, true, false); }
-size_t hos_kv_compact_workspace_bytes(const hos_kv_pages* in) { return workspace(in, false, false, true); }
+size_t hos_kv_resize_workspace_bytes(const hos_kv_pages* in) { return workspace(in, true); }
+size_t hos_kv_compact_workspace_bytes(const hos_kv_pages* in) { return workspace(in, false); }
 
 int hos_kv_resize(const hos_kv_pages* in, const int32_t* new_len, const hos_kv_pages* out, const hos_kv_moves* moves, int32_t* status, void* ws,
                   size_t ws_bytes, void* stream) {
@@ -118,7 +114,7 @@ int hos_kv_resize(const hos_kv_pages* in, const int32_t* new_len, const hos_kv_p
     if (!same_shape(in, out) || in->n_seq != out->n_seq || !tables_agree(in, out)) return HOS_E_INVALID;
     if ((in->n_seq > 0 && !new_len) || check_moves(moves)) return HOS_E_INVALID;
     PagesView v = view(in, out);
-    if (!fits(carve(v, true, false, false, ws), ws, ws_bytes)) return HOS_E_WORKSPACE;
+    if (!fits(carve(v, true, ws), ws, ws_bytes)) return HOS_E_WORKSPACE;
     v.change = new_len;
     v.src = moves->src;
     v.dst = moves->dst;
@@ -127,13 +123,12 @@ int hos_kv_resize(const hos_kv_pages* in, const int32_t* new_len, const hos_kv_p
     return cuda_rc(launch_kv_resize(v, static_cast<cudaStream_t>(stream)));
 }
 
-int hos_kv_fork(const hos_kv_pages* in, const int32_t* parent, const hos_kv_pages* out, int32_t* status, void* ws, size_t ws_bytes, void* stream) {
+int hos_kv_fork(const hos_kv_pages* in, const int32_t* parent, const hos_kv_pages* out, int32_t* status, void* stream) {
     int rc = check_pages(in, true);
     if (rc || (rc = check_pages(out, true))) return rc;
     if (!same_shape(in, out) || (out->n_seq > 0 && !parent)) return HOS_E_INVALID;
     if (in->n_seq > 0 && out->n_seq > 0 && (in->kv_len == out->kv_len || (in->max_pages > 0 && in->page_table == out->page_table))) return HOS_E_INVALID;
     PagesView v = view(in, out);
-    if (!fits(carve(v, false, true, false, ws), ws, ws_bytes)) return HOS_E_WORKSPACE;
     v.change = parent;
     v.status = status;
     return cuda_rc(launch_kv_fork(v, static_cast<cudaStream_t>(stream)));
@@ -145,7 +140,7 @@ int hos_kv_compact(const hos_kv_pages* in, const hos_kv_pages* out, const hos_kv
     if (rc || (rc = check_pages(out, false))) return rc;
     if (!same_shape(in, out) || in->n_seq != out->n_seq || !tables_agree(in, out) || check_moves(moves)) return HOS_E_INVALID;
     PagesView v = view(in, out);
-    if (!fits(carve(v, false, false, true, ws), ws, ws_bytes)) return HOS_E_WORKSPACE;
+    if (!fits(carve(v, false, ws), ws, ws_bytes)) return HOS_E_WORKSPACE;
     v.src = moves->src;
     v.dst = moves->dst;
     v.count = moves->count;

@@ -5,13 +5,30 @@
 
 namespace hos {
 
-// What a sequence of hos_kv_resize goes through, worked out once.  `takes` counts the pages taken before it by the
-// sequences of the same block, `splits` the pages among them that replace shared ones; the two top bits of splits say
-// whether it grows and whether it is one of those itself.
-struct ResizePlan {
-    int32_t have, need;
-    unsigned long long before;
-};
+// `blocks` blocks in clusters of `cluster`, early (see launch_early).
+template <typename... Params, typename... Args>
+cudaError_t launch_clusters(const char* name, void (*kernel)(Params...), int blocks, int cluster, int threads, cudaStream_t st, const Args&... args) {
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    launch_hook(name, 0, st);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    launch_hook(name, 1, st);
+    return e;
+}
+
+// What a sequence of hos_kv_resize takes (with flags: whether it grows, whether one of the pages replaces a shared one), and what those
+// before it in its block take and replace.
+struct ResizePlan { int32_t takes, before, splits_before; };
 
 // hos_kv_pages in and out, with their workspace; passed to kernels by value.
 struct PagesView {
@@ -24,7 +41,6 @@ struct PagesView {
     // workspace
     int32_t *growers, *latest, *queue;     // [n_pages]; queue: the free pages in order; hos_kv_compact: growers is a page's place among the moves
     ResizePlan* plan;                      // [n_seq]
-    int32_t* children;                     // [n_seq]
 };
 
 cudaError_t launch_kv_resize(const PagesView& p, cudaStream_t st);

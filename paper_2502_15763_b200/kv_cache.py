@@ -35,7 +35,7 @@ def binding():
         spec.loader.exec_module(m)
         m.init(*(C.cast(getattr(L, n), C.c_void_p).value for n in (
             "hos_kv_append", "hos_kv_read", "hos_paged_attention", "hos_paged_attention_workspace_bytes", "hos_kv_resize",
-            "hos_kv_resize_workspace_bytes", "hos_kv_fork", "hos_kv_fork_workspace_bytes", "hos_kv_compact",
+            "hos_kv_resize_workspace_bytes", "hos_kv_fork", "hos_kv_compact",
             "hos_kv_compact_workspace_bytes", "hos_kv_copy_pages", "hos_verify_drafts")))
         _binding, _append, _read, _attention = m, m.append, m.read, m.attention
     return _binding

@@ -25,13 +25,10 @@ def _compiled():
     return kv_cache._binding or kv_cache.binding()
 
 
-def _state(r, where):
-    if r[0]:
-        raise HosError(r[0], where)
-    out = {"refs": r[1], "page_table": r[2], "kv_len": r[3], "status": r[4]}
-    if len(r) > 5:
-        out.update(src=r[5], dst=r[6], count=r[7])
-    return out
+def _checked(r, where):
+    if type(r) is int:
+        raise HosError(r, where)
+    return r
 
 
 def hos_kv_resize(refs, page_table, kv_len, new_len, page_size: int, out=None):
@@ -41,21 +38,21 @@ def hos_kv_resize(refs, page_table, kv_len, new_len, page_size: int, out=None):
     Returns the new state {'refs', 'page_table', 'kv_len'}, the page copies to be made before the next append
     {'src', 'dst': int32 [n_seq], 'count': int32 [1]} and 'status' [n_seq] (HOS_ST_PAGES: too few free pages, the
     sequence and all growing ones after it keep their lengths; HOS_ST_INVALID)."""
-    return _state(_compiled().resize(refs, page_table, kv_len, new_len, page_size, out), "hos_kv_resize")
+    return _checked(_compiled().resize(refs, page_table, kv_len, new_len, page_size, out), "hos_kv_resize")
 
 
 def hos_kv_fork(refs, page_table, kv_len, parent, page_size: int, out=None):
     """Sequence i of the new state holds what sequence parent[i] of the old one holds (-1: nothing); any number of them.
 
     Returns {'refs', 'page_table', 'kv_len', 'status' [len(parent)]}; in `out` only refs may be the old tensor."""
-    return _state(_compiled().fork(refs, page_table, kv_len, parent, page_size, out), "hos_kv_fork")
+    return _checked(_compiled().fork(refs, page_table, kv_len, parent, page_size, out), "hos_kv_fork")
 
 
 def hos_kv_compact(refs, page_table, kv_len, page_size: int, out=None):
     """Moves the pages in use to the front of the pool.
 
     Returns {'refs', 'page_table', 'kv_len' (as it was), 'src', 'dst': int32 [n_pages], 'count': int32 [1], 'status' [n_seq]}."""
-    return _state(_compiled().compact(refs, page_table, kv_len, None, page_size, out), "hos_kv_compact")
+    return _checked(_compiled().compact(refs, page_table, kv_len, None, page_size, out), "hos_kv_compact")
 
 
 def hos_kv_copy_pages(caches, src, dst, count=None, source=None):
@@ -87,7 +84,4 @@ def hos_verify_drafts(tokens, target, draft, tok_off, u_accept, u_sample, kv_len
 
     Returns int32 {'accepted' [n_seq], 'next' [n_seq], 'tokens' [n_tokens]: the accepted drafts, next, then -1 (rows of no
     sequence are not written), 'new_len' [n_seq]: kv_len without the drafts that were not accepted, or None, 'status' [n_seq]}."""
-    rc, accepted, nxt, out, new_len, status = _compiled().verify(tokens, target, draft, tok_off, u_accept, u_sample, kv_len)
-    if rc:
-        raise HosError(rc, "hos_verify_drafts")
-    return {"accepted": accepted, "next": nxt, "tokens": out, "new_len": new_len, "status": status}
+    return _checked(_compiled().verify(tokens, target, draft, tok_off, u_accept, u_sample, kv_len), "hos_verify_drafts")

@@ -114,6 +114,9 @@ def verify(tokens, target, draft, off, u_accept, u_sample, vocab):
     def counted(row):
         return torch.where((row > 0) & (row < math.inf), row, torch.zeros_like(row))
 
+    def of_draft(row):
+        return torch.where(row > 0, row, torch.zeros_like(row))
+
     n_tok, n_seq = len(tokens), len(off) - 1
     accepted, nxt, out, status, owners = [0] * n_seq, [-1] * n_seq, [None] * n_tok, [0] * n_seq, [0] * n_tok
     for s in range(n_seq):
@@ -130,7 +133,7 @@ def verify(tokens, target, draft, off, u_accept, u_sample, vocab):
                 status[s] = INVALID
                 break
             p = float(counted(target[a + j, d:d + 1])[0])
-            q = 1.0 if draft is None else float(counted(draft[a + j, d:d + 1])[0])
+            q = 1.0 if draft is None else float(of_draft(draft[a + j, d:d + 1])[0])
             if not u_accept[a + j] * q < p:
                 break
             j += 1
@@ -138,7 +141,7 @@ def verify(tokens, target, draft, off, u_accept, u_sample, vocab):
         w = p.clone()
         if j < k:
             if draft is not None:
-                w = (p - counted(draft[a + j])).clamp_min(0.0)
+                w = (p - of_draft(draft[a + j])).clamp_min(0.0)
             elif 0 <= tokens[a + j + 1] < vocab:
                 w[tokens[a + j + 1]] = 0.0
             if not bool((w > 0).any()):
