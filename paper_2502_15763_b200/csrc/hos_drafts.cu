@@ -54,6 +54,24 @@ template <typename T> struct Weights {
         if (!q) return v == banned ? 0.0 : x;
         return fmax(x - (double)draft_of(as_float(__ldg(q + v))), 0.0);
     }
+    // K weights from `a` on, as far as [a, b) goes.
+    template <int K> __device__ __forceinline__ void run(int a, int b, bool wide, double (&x)[K]) const {
+        constexpr int N = Vec<T>::N;
+        if (K >= N && wide && b - a >= K && ((reinterpret_cast<uintptr_t>(p + a)) & 15) == 0) {
+            Vec<T> u[(K + N - 1) / N], v[(K + N - 1) / N];
+#pragma unroll
+            for (int k = 0; k < K / N; ++k) {
+                u[k].w = __ldg(reinterpret_cast<const uint4*>(p + a) + k);
+                v[k].w = q ? __ldg(reinterpret_cast<const uint4*>(q + a) + k) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                x[k] = a + k == banned ? 0.0 : fmax((double)target_of(u[k / N].at(k % N)) - (double)draft_of(v[k / N].at(k % N)), 0.0);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) x[k] = a + k < b ? at(a + k) : 0.0;
+    }
     // Sum over [a, b) by one warp; where they can be read 16 bytes at a time from `a` on, in both rows.  A difference x - y > 0 is
     // d + e exactly, d rounded to 32 bits and e = (x - d) - y (Dekker, 1971).  The d are added up in 64 bits; the e, below 2^-24 of
     // them, 16 or 32 in 32 bits first, which leaves 2^-43 of the sum.  So a conversion and a 64-bit sum are left of two and three
@@ -167,6 +185,42 @@ template <typename T> __device__ __forceinline__ Verdict judge(const hos_drafts&
     return r;
 }
 
+// The first entry of [a, b) up to which the weights add up to more than `left` (or the last one that has any) is the next token.  By a
+// whole block, RUN neighbours a thread, all loads at once (32 neighbours a warp at a time would take a scan for each 32: 3 us more).
+template <int RUN, typename T>
+__device__ __forceinline__ void search(const hos_drafts& d, int s, long long row, const Weights<T>& w, int a, int b, bool wide, double left, double* sums) {
+    for (int i0 = a; i0 < b; i0 += THREADS * RUN) {
+        const int first = i0 + (int)threadIdx.x * RUN;
+        double x[RUN], mine = 0.0;
+        w.template run<RUN>(first, b, wide, x);
+#pragma unroll
+        for (int k = 0; k < RUN; ++k) mine += x[k];
+        const double upto_lane = warp_sum_upto(mine);
+        __syncthreads();
+        if (lane_id() == 31) sums[warp_id()] = upto_lane;
+        __syncthreads();
+        const double own = lane_id() < WARPS ? sums[lane_id()] : 0.0, upto = warp_sum_upto(own), all = __shfl_sync(FULL, upto, 31);
+        const int in = first_beyond(upto, own, left);
+        if (in == warp_id()) {                         // should `left` lie behind all of this, the last one so far
+            double rest = left - __shfl_sync(FULL, upto - own, in);
+            if (first_beyond(upto_lane, mine, rest) == lane_id()) {
+                rest -= upto_lane - mine;
+                int pick = -1;
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < RUN; ++k) {
+                    if (x[k] > 0.0 && !found) pick = first + k;
+                    found |= x[k] > rest;
+                    rest -= x[k];
+                }
+                d.next[s] = d.out_tokens[row] = pick;
+            }
+        }
+        if (all > left) return;
+        left -= all;
+    }
+}
+
 template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_drafts(const __grid_constant__ hos_drafts d) {
     __shared__ Verdict verdict;
     __shared__ double sums[WARPS], total;
@@ -238,36 +292,10 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
             double left = t - __shfl_sync(FULL, upto_block - of_block, block);
             const int warp = first_beyond(upto, own, left);
             left -= __shfl_sync(FULL, upto - own, warp);
-            // the segment of that warp, by the whole block: a run of neighbours each
-            const int i = rank * WARPS + warp, first = edge(i), last = edge(i + 1);
-            const int run = (last - first + THREADS - 1) / THREADS, c = min(first + (int)threadIdx.x * run, last), e = min(c + run, last);
-            double mine = 0.0;
-            for (int x = c; x < e; ++x) mine += w.at(x);
-            __syncthreads();
-            const double upto_lane = warp_sum_upto(mine);
-            if (lane_id() == 31) sums[warp_id()] = upto_lane;
-            __syncthreads();
-            own = lane_id() < WARPS ? sums[lane_id()] : 0.0;
-            upto = warp_sum_upto(own);
-            const int in = first_beyond(upto, own, left);
-            if (warp_id() == in) {
-                left -= __shfl_sync(FULL, upto - own, in);
-                const int lane = first_beyond(upto_lane, mine, left);
-                if (lane_id() == lane) {
-                    left -= upto_lane - mine;
-                    int pick = -1;
-                    double sofar = 0.0;
-                    for (int x = c; x < e; ++x) {
-                        const double y = w.at(x);
-                        sofar += y;
-                        if (y > 0.0) {
-                            pick = x;
-                            if (sofar > left) break;
-                        }
-                    }
-                    d.next[s] = d.out_tokens[row] = pick;
-                }
-            }
+            const int from = edge(rank * WARPS + warp), to = edge(rank * WARPS + warp + 1);
+            // one neighbour a thread where that is enough: 32,000 entries by 8 blocks 5.3 us, with 8 neighbours 6.2
+            if (to - from <= THREADS) search<1>(d, s, row, w, from, to, wide, left, sums);
+            else search<8>(d, s, row, w, from, to, wide, left, sums);
         }
         if (blocks > 1) cluster_wait();
         return;
@@ -275,8 +303,8 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
 }
 
 // As many blocks a sequence as there are room for at once (two of 512 threads an SM, and as good as all SMs even), up to 8, with
-// 2,048 entries each at least.  One, 2, 4, 8, 16, us: one sequence of 32,000 32-bit entries 8.6, 6.6, 5.6, 5.6, 5.8; 33 of 50,257
-// bf16 ones 12.7, 10.7, 8.9, 10.1, 20.6; 128 of 128,000 32-bit ones 44, 30, 33, 41, 73.
+// 2,048 entries each at least.  One, 2, 4, 8, 16, us: one sequence of 32,000 32-bit entries 7.5, 6.8, 5.3, 5.3, 5.8; 33 of 50,257
+// bf16 ones 11.5, 10.6, 9.0, 10.1, 20.6; 128 of 128,000 32-bit ones 36, 27, 32, 41, 73.
 template <typename T> cudaError_t verify(const hos_drafts& d, cudaStream_t st) {
     int blocks = 8;
     while (blocks > 1 && ((long long)d.n_seq * blocks > 256 || d.vocab < 2048 * blocks)) blocks >>= 1;

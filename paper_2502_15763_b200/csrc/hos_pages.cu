@@ -533,39 +533,46 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
 }
 
 // ---- copy --------------------------------------------------------------------------------------------------------------
+// A unit is 16 KB of a page's keys or values, with the scales of the 8-bit ones (1/16 or 1/32 of that); a thread has four
+// accesses of 16 bytes on the way.  Units are counted on by a block's stride in three digits (unit of a page, move, layer), without divisions.
 constexpr int COPY_THREADS = 256, COPY_UNIT = COPY_THREADS * 64;
 
 __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_pages(const __grid_constant__ CopyView c) {
     pdl_launch_dependents();
     pdl_wait();
     const int n = c.count ? max(0, min(c.n_moves, __ldg(c.count))) : c.n_moves;
-    // a page of k or v is so many units, its scales one each as far as they go
-    const int units = (c.bytes + COPY_UNIT - 1) / COPY_UNIT, scale_units = (c.scale_bytes + COPY_UNIT - 1) / COPY_UNIT, per = 2 * (units + scale_units);
-    const long long total = (long long)n * c.n_layers * per;
-    for (long long u = blockIdx.x; u < total; u += gridDim.x) {
-        const int which = (int)(u % per), move = (int)(u / per % n), layer = (int)(u / per / n);
+    if (n == 0) return;
+    const int units = 2 * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT);
+    const int step = (int)gridDim.x % units, step_moves = (int)gridDim.x / units % n, step_layers = (int)gridDim.x / units / n;
+    int unit = (int)blockIdx.x % units, move = (int)blockIdx.x / units % n, layer = (int)blockIdx.x / units / n;
+    const int scale_at = (int)threadIdx.x * 16;
+    while (layer < c.n_layers) {
         const int from = __ldg(c.src + move), to = __ldg(c.dst + move);
-        if ((unsigned)from >= (unsigned)c.from_pages || (unsigned)to >= (unsigned)c.to_pages) {
-            if (threadIdx.x == 0 && which == 0 && layer == 0 && c.status) atomicOr(c.status + move, HOS_ST_INVALID);
-            continue;
-        }
-        const bool scales = which >= 2 * units;
-        const int w = scales ? which - 2 * units : which, each = scales ? scale_units : units;
-        const int array = (scales ? 2 : 0) + w / each, at = w % each * COPY_UNIT, end = min(scales ? c.scale_bytes : c.bytes, at + COPY_UNIT);
         const CopyLayer& l = c.layer[layer];
-        const unsigned char* a = l.from[array] + from * l.from_stride[scales];
-        unsigned char* b = l.to[array] + to * l.to_stride[scales];
-        uint4 x[4];
+        if ((unsigned)from < (unsigned)c.from_pages && (unsigned)to < (unsigned)c.to_pages) {
+            const int v = unit & 1, at = (unit >> 1) * COPY_UNIT;              // keys and values in turn
+            const int left = c.bytes - at - (int)threadIdx.x * 16;
+            const unsigned char* a = l.from[v] + from * l.from_stride[0] + (at + (int)threadIdx.x * 16);
+            unsigned char* b = l.to[v] + to * l.to_stride[0] + (at + (int)threadIdx.x * 16);
+            uint4 x[4], s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int o = at + (i * COPY_THREADS + (int)threadIdx.x) * 16;
-            if (o < end) x[i] = *reinterpret_cast<const uint4*>(a + o);
-        }
+            for (int i = 0; i < 4; ++i)
+                if (i * COPY_THREADS * 16 < left) x[i] = __ldg(reinterpret_cast<const uint4*>(a + i * COPY_THREADS * 16));
+            const int scale_first = at >> c.scale_shift, scale_last = min(c.scale_bytes, (at + COPY_UNIT) >> c.scale_shift);
+            const bool scale = scale_first + scale_at < scale_last;
+            if (scale) s = __ldg(reinterpret_cast<const uint4*>(l.from[2 + v] + from * l.from_stride[1] + scale_first + scale_at));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int o = at + (i * COPY_THREADS + (int)threadIdx.x) * 16;
-            if (o < end) *reinterpret_cast<uint4*>(b + o) = x[i];
+            for (int i = 0; i < 4; ++i)
+                if (i * COPY_THREADS * 16 < left) *reinterpret_cast<uint4*>(b + i * COPY_THREADS * 16) = x[i];
+            if (scale) *reinterpret_cast<uint4*>(l.to[2 + v] + to * l.to_stride[1] + scale_first + scale_at) = s;
+        } else if (threadIdx.x == 0 && unit == 0 && layer == 0 && c.status) {
+            atomicOr(c.status + move, HOS_ST_INVALID);
         }
+        unit += step;
+        move += step_moves;
+        layer += step_layers;
+        if (unit >= units) unit -= units, ++move;
+        if (move >= n) move -= n, ++layer;
     }
 }
 
@@ -595,9 +602,12 @@ cudaError_t launch_kv_resize(const PagesView& p, cudaStream_t st) { return launc
 cudaError_t launch_kv_fork(const PagesView& p, cudaStream_t st) { return launch_tables<k_kv_fork>("k_kv_fork", p, st); }
 cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st) { return launch_tables<k_kv_compact>("k_kv_compact", p, st); }
 
+// A block a unit, as far as 256 an SM go, where all moves are there (16 moves of 80 layers, 1.34 GB, with 8, 32 and 256 blocks an SM: 224, 208
+// and 200 us, 6.7 TB/s).  Where their number is on the device it is mostly small or nothing, and blocks without work cost more
+// than that (none of 128 moves: 1.9, 5.5 and 40 us; one: 9.8, 10.5, 45): 8 an SM then.
 cudaError_t launch_kv_copy_pages(const CopyView& c, cudaStream_t st) {
-    const long long per = 2 * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT + (c.scale_bytes + COPY_UNIT - 1) / COPY_UNIT);
-    const long long blocks = std::min<long long>(per * c.n_moves * c.n_layers, 148 * 8);
+    const long long units = 2ll * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT);
+    const long long blocks = std::min<long long>(units * c.n_moves * c.n_layers, ATTN_SMS * (c.count ? 8 : 256));
     launch_hook("k_kv_copy_pages", 0, st);
     const cudaError_t e = launch_early(k_kv_copy_pages, dim3((unsigned)blocks), COPY_THREADS, 0, st, c);
     launch_hook("k_kv_copy_pages", 1, st);

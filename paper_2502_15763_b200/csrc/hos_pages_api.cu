@@ -173,6 +173,7 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
     v.to_pages = to->n_pages;
     v.bytes = (int)(rows * to->head_dim * size);
     v.scale_bytes = coded ? (int)(rows * 4) : 0;
+    v.scale_shift = to->head_dim == 64 ? 4 : 5;
     for (int first = 0; first < n_layers; first += COPY_LAYERS) {
         v.n_layers = n_layers - first < COPY_LAYERS ? n_layers - first : COPY_LAYERS;
         for (int l = 0; l < v.n_layers; ++l) {

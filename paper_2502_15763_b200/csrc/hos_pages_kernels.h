@@ -59,6 +59,7 @@ struct CopyView {
     int32_t* status;
     int n_moves, n_layers, from_pages, to_pages;
     int bytes, scale_bytes;                // of a page's k or v, of its scales (0: none)
+    int scale_shift;                       // log2 of the one over the other
     CopyLayer layer[COPY_LAYERS];
 };
 cudaError_t launch_kv_copy_pages(const CopyView& c, cudaStream_t st);
