@@ -441,7 +441,7 @@ PyObject* pages(int kind, PyObject* const* a) {
     Results r;
     r.add(n.refs, given ? Py_NewRef(o[0]) : w.tensor(refs, {in.n_pages}));
     r.add(n.page_table, given ? Py_NewRef(o[1]) : w.tensor(table, {n_out, in.max_pages}));
-    r.add(n.kv_len, given ? Py_NewRef(o[2]) : kind == COMPACT ? Py_NewRef(a[2]) : w.tensor(len, {n_out}));
+    r.add(n.kv_len, kind == COMPACT ? Py_NewRef(a[2]) : given ? Py_NewRef(o[2]) : w.tensor(len, {n_out}));
     r.add(n.status, w.tensor(status, {n_out}));
     if (kind != FORK) {
         r.add(n.src, w.tensor(src, {n_moves}));

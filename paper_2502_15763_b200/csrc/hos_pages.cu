@@ -537,7 +537,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
 // accesses of 16 bytes on the way.  Units are counted on by a block's stride in three digits (unit of a page, move, layer), without divisions.
 constexpr int COPY_THREADS = 256, COPY_UNIT = COPY_THREADS * 64;
 
-__global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_pages(const __grid_constant__ CopyView c) {
+// The layers come as kernel parameters.  Room for 128 of them, 12 KB, costs a call 2.5 us on the host more than for 4.
+template <int LAYERS> struct CopyView {
+    CopyCall call;
+    CopyLayer layer[LAYERS];
+};
+
+template <int LAYERS> __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_pages(const __grid_constant__ CopyView<LAYERS> view) {
+    const CopyCall& c = view.call;
     pdl_launch_dependents();
     pdl_wait();
     const int n = c.count ? max(0, min(c.n_moves, __ldg(c.count))) : c.n_moves;
@@ -548,7 +555,7 @@ __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_pages(const __grid_con
     const int scale_at = (int)threadIdx.x * 16;
     while (layer < c.n_layers) {
         const int from = __ldg(c.src + move), to = __ldg(c.dst + move);
-        const CopyLayer& l = c.layer[layer];
+        const CopyLayer& l = view.layer[layer];
         if ((unsigned)from < (unsigned)c.from_pages && (unsigned)to < (unsigned)c.to_pages) {
             const int v = unit & 1, at = (unit >> 1) * COPY_UNIT;              // keys and values in turn
             const int left = c.bytes - at - (int)threadIdx.x * 16;
@@ -605,13 +612,19 @@ cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st) { return laun
 // A block a unit, as far as 256 an SM go, where all moves are there (16 moves of 80 layers, 1.34 GB, with 8, 32 and 256 blocks an SM: 224, 208
 // and 200 us, 6.7 TB/s).  Where their number is on the device it is mostly small or nothing, and blocks without work cost more
 // than that (none of 128 moves: 1.9, 5.5 and 40 us; one: 9.8, 10.5, 45): 8 an SM then.
-cudaError_t launch_kv_copy_pages(const CopyView& c, cudaStream_t st) {
+cudaError_t launch_kv_copy_pages(const CopyCall& c, const CopyLayer* layers, cudaStream_t st) {
     const long long units = 2ll * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT);
     const long long blocks = std::min<long long>(units * c.n_moves * c.n_layers, ATTN_SMS * (c.count ? 8 : 256));
-    launch_hook("k_kv_copy_pages", 0, st);
-    const cudaError_t e = launch_early(k_kv_copy_pages, dim3((unsigned)blocks), COPY_THREADS, 0, st, c);
-    launch_hook("k_kv_copy_pages", 1, st);
-    return e;
+    auto launch = [&](auto most) {
+        CopyView<decltype(most)::value> view;
+        view.call = c;
+        std::copy(layers, layers + c.n_layers, view.layer);
+        launch_hook("k_kv_copy_pages", 0, st);
+        const cudaError_t e = launch_early(k_kv_copy_pages<decltype(most)::value>, dim3((unsigned)blocks), COPY_THREADS, 0, st, view);
+        launch_hook("k_kv_copy_pages", 1, st);
+        return e;
+    };
+    return c.n_layers <= 4 ? launch(IntTag<4>{}) : c.n_layers <= 32 ? launch(IntTag<32>{}) : launch(IntTag<COPY_LAYERS>{});
 }
 
 }  // namespace hos

@@ -163,7 +163,8 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
     if (!src_page || !dst_page) return HOS_E_INVALID;
     const bool coded = to->format != HOS_KV_SAME;
     const long long rows = (long long)to->n_kv_heads * to->page_size, size = coded ? 1 : 2;
-    CopyView v;
+    CopyCall v;
+    CopyLayer layers[COPY_LAYERS];
     v.src = src_page;
     v.dst = dst_page;
     v.count = count;
@@ -178,7 +179,7 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
         v.n_layers = n_layers - first < COPY_LAYERS ? n_layers - first : COPY_LAYERS;
         for (int l = 0; l < v.n_layers; ++l) {
             const hos_kv_cache &a = from[first + l], &b = to[first + l];
-            CopyLayer& w = v.layer[l];
+            CopyLayer& w = layers[l];
             void* const as[4] = {a.k, a.v, a.k_scale, a.v_scale};
             void* const bs[4] = {b.k, b.v, b.k_scale, b.v_scale};
             for (int i = 0; i < 4; ++i) {
@@ -190,7 +191,7 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
             w.from_stride[1] = a.scale_page_stride ? a.scale_page_stride * 4 : v.scale_bytes;
             w.to_stride[1] = b.scale_page_stride ? b.scale_page_stride * 4 : v.scale_bytes;
         }
-        const int rc = cuda_rc(launch_kv_copy_pages(v, static_cast<cudaStream_t>(stream)));
+        const int rc = cuda_rc(launch_kv_copy_pages(v, layers, static_cast<cudaStream_t>(stream)));
         if (rc) return rc;
     }
     return HOS_OK;

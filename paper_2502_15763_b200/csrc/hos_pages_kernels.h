@@ -47,22 +47,20 @@ cudaError_t launch_kv_resize(const PagesView& p, cudaStream_t st);
 cudaError_t launch_kv_fork(const PagesView& p, cudaStream_t st);
 cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st);
 
-// Layers of a hos_kv_copy_pages call that one launch takes; kernel parameters may have 32,764 bytes.
-constexpr int COPY_LAYERS = 128;
 struct CopyLayer {
     const unsigned char* from[4];          // k, v, k_scale, v_scale
     unsigned char* to[4];
     long long from_stride[2], to_stride[2];        // bytes from page to page: of k and v, of their scales
 };
-struct CopyView {
+struct CopyCall {
     const int32_t *src, *dst, *count;
     int32_t* status;
     int n_moves, n_layers, from_pages, to_pages;
     int bytes, scale_bytes;                // of a page's k or v, of its scales (0: none)
     int scale_shift;                       // log2 of the one over the other
-    CopyLayer layer[COPY_LAYERS];
 };
-cudaError_t launch_kv_copy_pages(const CopyView& c, cudaStream_t st);
+constexpr int COPY_LAYERS = 128;           // that one launch takes
+cudaError_t launch_kv_copy_pages(const CopyCall& c, const CopyLayer* layers, cudaStream_t st);
 
 cudaError_t launch_verify_drafts(const hos_drafts& d, cudaStream_t st);
 

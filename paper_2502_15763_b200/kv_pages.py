@@ -51,7 +51,7 @@ def hos_kv_fork(refs, page_table, kv_len, parent, page_size: int, out=None):
 def hos_kv_compact(refs, page_table, kv_len, page_size: int, out=None):
     """Moves the pages in use to the front of the pool.
 
-    Returns {'refs', 'page_table', 'kv_len' (as it was), 'src', 'dst': int32 [n_pages], 'count': int32 [1], 'status' [n_seq]}."""
+    Returns {'refs', 'page_table', 'kv_len' (the tensor that was given), 'src', 'dst': int32 [n_pages], 'count': int32 [1], 'status' [n_seq]}."""
     return _checked(_compiled().compact(refs, page_table, kv_len, None, page_size, out), "hos_kv_compact")
 
 
@@ -63,7 +63,10 @@ def hos_kv_copy_pages(caches, src, dst, count=None, source=None):
     for each i (HOS_ST_INVALID: a page number out of range)."""
     caches = [caches] if isinstance(caches, KvCache) else list(caches)
     source = caches if source is None else [source] if isinstance(source, KvCache) else list(source)
-    to, of = [c._h for c in caches], [c._h for c in source]
+    try:
+        to, of = [c._h for c in caches], [c._h for c in source]
+    except AttributeError:
+        raise TypeError("caches, source: expected handles made by hos_kv_cache") from None
     call = _compiled().copy_pages
     rc = call(to, of, src, dst, count)
     if rc == STATUS_TOO_SHORT:

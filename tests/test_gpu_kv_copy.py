@@ -181,6 +181,9 @@ def test_refusals():
                                   (one, one, one.float(), TypeError), ([0], one, None, TypeError), (dev([[0]]), dev([[0]]), None, ValueError)):
         with pytest.raises(kind):
             h.hos_kv_copy_pages(a, src, dst, count)
+    for bad in ([a.k], [None], [a, 3]):
+        with pytest.raises(TypeError):
+            h.hos_kv_copy_pages(bad, one, one)
     for bad, src in (([], None), ([a], [a, a])):
         with pytest.raises(ValueError):
             h.hos_kv_copy_pages(bad, one, one, source=src)

@@ -246,6 +246,34 @@ def test_compact_with_bad_data():
     check_compact(empty)
 
 
+@pytest.mark.parametrize("n_seq,shared", [(2000, 0.0), (1100, 0.3), (40000, 0.2)])
+def test_more_sequences_than_threads(n_seq, shared):
+    """One block with several sequences a thread; sixteen of them."""
+    pool = Pool(n_seq, n_seq, 4, 4, 700 if n_seq < 6000 else 9000, shared=shared, entries=2 if shared == 0.0 else None)
+    new = pool.targets(1, True)
+    for in_place in (False, True):
+        check_resize(pool, new, in_place)
+        check_compact(pool, in_place)
+    r = random.Random(n_seq)
+    check_fork(pool, [r.randrange(n_seq) for _ in range(n_seq)])
+    check_fork(pool, [r.randrange(-1, n_seq) for _ in range(3 * n_seq // 2)], refs_in_place=True)
+
+
+def test_compacting_a_million_pages_in_place():
+    pool = Pool(4, 30, 1, 60000, 0, shared=0.0)
+    more = 1_100_000 - pool.n_pages
+    r = random.Random(1)
+    at = sorted(r.sample(range(1_100_000), pool.n_pages))
+    pool.rows = [[at[p] if p >= 0 else -1 for p in row] for row in pool.rows]
+    pool.refs, pool.n_pages = [0] * 1_100_000, pool.n_pages + more
+    for row in pool.rows:
+        for p in row:
+            if p >= 0:
+                pool.refs[p] += 1
+    check_compact(pool, True)
+    check_compact(pool, False)
+
+
 def test_a_million_pages():
     """Numbers beyond 16 bits, rows of many pieces; a sequence that takes nearly everything."""
     h = hos()

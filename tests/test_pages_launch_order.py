@@ -35,4 +35,4 @@ def test_the_kernels_are_found():
 def test_a_kernel_waits_before_anything_else(kernel):
     before, found, after = ALL[kernel].partition("\n    pdl_wait();\n")
     assert found and "pdl_wait" not in after
-    assert not re.search(r"p\.|c\.|d\.|\breturn\b|cp_async|atomic|__ldg|cluster_sync", before)
+    assert not re.search(r"p\.|\bc\.|\bd\.|\breturn\b|cp_async|atomic|__ldg|cluster_sync", before)
