@@ -189,21 +189,17 @@ constexpr int GROWS = 1 << 30, SPLITS = 1 << 29, TAKES = SPLITS - 1;
 struct Change {
     int old, now;
     bool valid;
-    int page;                  // that the sequence grows from the inside of; -1: none, -2: none that exists
+    bool inside;               // it grows from the inside of `page`, as the table has it (looked at late: it is still on its way)
+    int page;
 };
 __device__ __forceinline__ Change change_of(const PagesView& p, int s) {
     Change c;
     c.old = p.len_in[s];
     c.now = p.change[s];
     c.valid = is_length(p, c.old) && is_length(p, c.now);
-    c.page = -1;
-    if (c.valid && c.now > c.old) {
-        const unsigned at = (unsigned)c.old / (unsigned)p.page_size;
-        if (at * (unsigned)p.page_size != (unsigned)c.old) {
-            c.page = p.table_in[(long long)s * p.in_stride + at];
-            if (!is_page(p, c.page)) c.page = -2;
-        }
-    }
+    const unsigned at = (unsigned)c.old / (unsigned)p.page_size;
+    c.inside = c.valid && c.now > c.old && at * (unsigned)p.page_size != (unsigned)c.old;
+    c.page = c.inside ? p.table_in[(long long)s * p.in_stride + at] : -1;
     return c;
 }
 
@@ -235,23 +231,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
     };
     // the new counts begin as the old ones; what is known of shared pages that are grown from, as nothing; rows of tables apart are copied
     // as far as they stay
-    Change first = {};                                 // of this thread's first sequence
+    Change first = {0, 0, false, false, -1};           // of this thread's first sequence
     if (seqs.first + tid < seqs.last) first = change_of(p, seqs.first + tid);
     copy_counts(p, pages);
     go.begin(1);
     for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
         stay.begin((p.max_pages + PIECE - 1) / PIECE);
         const int s = s0 + tid;
-        const Change c = s0 == seqs.first ? first : s < seqs.last ? change_of(p, s) : Change{};
+        Change c = first;
+        if (s0 > seqs.first) c = s < seqs.last ? change_of(p, s) : Change{0, 0, false, false, -1};
         if (s < seqs.last) {
             if (!in_place) stay.add(RowWork{s, 0, c.valid ? pages_of(p, min(c.old, c.now)) : p.max_pages, 0});
             if (s0 == seqs.first) list_of_gone(c, s);
             p.src[s] = p.dst[s] = -1;
         }
-        if (!in_place) all_pieces(stay, first_piece(stay, old_row), old_row, keep);
+        Cursor kept;
+        if (!in_place) kept = first_piece(stay, old_row);
+        const int holders = is_page(p, c.page) && s < seqs.last ? p.refs_in[c.page] : 0;
+        if (!in_place) all_pieces(stay, kept, old_row, keep);
         if (s < seqs.last) {
-            if (p.status) p.status[s] = c.valid && c.page != -2 ? 0 : HOS_ST_INVALID;
-            if (c.page >= 0 && p.refs_in[c.page] > 1) p.growers[c.page] = 0, p.latest[c.page] = -1;
+            if (p.status) p.status[s] = c.valid && (!c.inside || is_page(p, c.page)) ? 0 : HOS_ST_INVALID;
+            if (holders > 1) p.growers[c.page] = 0, p.latest[c.page] = -1;
         }
         if (s0 + THREADS < seqs.last) __syncthreads();
     }
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
         }
         if (s < seqs.last) {
             const Change c = s0 == seqs.first ? first : change_of(p, s);
-            if (c.page >= 0 && __ldcg(p.refs_in + c.page) > 1) {
+            if (is_page(p, c.page) && __ldcg(p.refs_in + c.page) > 1) {
                 atomicAdd(p.growers + c.page, 1);
                 atomicMax(p.latest + c.page, s);
             }
@@ -277,6 +277,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
     }
     cluster_or_block_sync();
     // how many pages are free; what each sequence takes, with sums in order
+    int holders = 0, growers = 0, latest = 0;          // of the page that this thread's first sequence grows from
+    if (is_page(p, first.page)) {
+        holders = __ldcg(p.refs + first.page);
+        growers = __ldcg(p.growers + first.page);      // nothing, where there is but one holder: not looked at then
+        latest = __ldcg(p.latest + first.page);
+    }
     FreeMasks masks{warp_part(pages), 0};
     int n_free = 0;
     masks.first_pass(p.refs, [&](int, unsigned m) { n_free += __popc(m); });
@@ -290,10 +296,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
             const Change c = s0 == seqs.first ? first : change_of(p, s);
             if (c.valid && c.now > c.old) {
                 plan.takes = GROWS | min(pages_of(p, c.now) - pages_of(p, c.old), PLENTY - 1);
-                if (c.page >= 0) {
-                    const int refs = __ldcg(p.refs + c.page);
-                    if (refs > 1 && !(__ldcg(p.growers + c.page) == refs && __ldcg(p.latest + c.page) == s)) plan.takes = (plan.takes + 1) | SPLITS;
+                if (s0 > seqs.first && is_page(p, c.page)) {
+                    holders = __ldcg(p.refs + c.page);
+                    growers = __ldcg(p.growers + c.page);
+                    latest = __ldcg(p.latest + c.page);
                 }
+                if (is_page(p, c.page) && holders > 1 && !(growers == holders && latest == s)) plan.takes = (plan.takes + 1) | SPLITS;
             }
         }
         const unsigned split = __ballot_sync(FULL, plan.takes & SPLITS);
@@ -491,10 +499,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
         const int k = late_at + __popc(a & lanes_before());
         if (a & me) p.src[k] = i;
         if (h & me) p.dst[hole_at + __popc(h & lanes_before())] = i;
-        if (a & me) {                                  // its count goes with it, by way of the workspace: the pools may be the same
-            p.queue[k] = p.refs_in[i];
-            p.refs[i] = 0;
-        }
         if (i >= n_live && i < masks.part.last) p.growers[i] = a & me ? k : -1;
         late_at += __popc(a);
         hole_at += __popc(h);
@@ -506,7 +510,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     if (seqs.first + tid < seqs.last) list_row(seqs.first + tid, p.len_in[seqs.first + tid]);
     Cursor at = first_piece(list, row);
     cluster_or_block_sync();
-    for (int k = cluster_rank() * THREADS + tid; k < count; k += cluster_size() * THREADS) p.refs[__ldcg(p.dst + k)] = __ldcg(p.queue + k);
+    int k = cluster_rank() * THREADS + tid, from = 0, to = 0;      // a move whose count goes along; its numbers come while the rows are worked on
+    if (k < count) from = __ldcg(p.src + k), to = __ldcg(p.dst + k);
     for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
         if (s0 > seqs.first) {
             __syncthreads();
@@ -515,20 +520,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
             at = first_piece(list, row);
         }
         all_pieces(list, at, row, [&](const RowWork& r, int j, Piece x) {
-            int to[EACH];
+            int place[EACH];                           // among the moves
             bool bad = false;
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 const bool there = r.from && 32 * k < r.last - j - lane_id(), page = is_page(p, x.e[k]), moves = there && page && x.e[k] >= n_live;
-                to[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
-                bad |= there && (!page || (moves && to[k] < 0));
+                place[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
+                bad |= there && (!page || (moves && place[k] < 0));
             }
 #pragma unroll
             for (int k = 0; k < EACH; ++k)
-                if (to[k] >= 0) x.e[k] = __ldcg(p.dst + to[k]);
+                if (place[k] >= 0) x.e[k] = __ldcg(p.dst + place[k]);
             if (bad) flag(p, r.seq);
             store_piece(p.table + (long long)r.seq * p.out_stride, j, in_place ? r.last : p.max_pages, x);
         });
+    }
+    while (k < count) {
+        const int refs = p.refs_in[from];
+        p.refs[to] = refs;
+        p.refs[from] = 0;
+        k += cluster_size() * THREADS;
+        if (k < count) from = __ldcg(p.src + k), to = __ldcg(p.dst + k);
     }
 }
 

@@ -47,9 +47,9 @@ size_t carve(PagesView& v, bool resize, void* ws) {
     };
     const size_t pages = (size_t)v.n_pages * 4;
     v.growers = static_cast<int32_t*>(take(pages));
-    v.queue = static_cast<int32_t*>(take(pages));
     if (!resize) return off;
     v.latest = static_cast<int32_t*>(take(pages));
+    v.queue = static_cast<int32_t*>(take(pages));
     v.plan = static_cast<ResizePlan*>(take((size_t)v.n_seq * sizeof(ResizePlan)));
     return off;
 }
