@@ -2,9 +2,13 @@
 //
 // Of all the rows only one a sequence is read whole: that of the first draft which is not accepted, or the last one.  A cluster
 // of blocks takes a sequence.  Each block finds that row for itself (two scattered reads a draft, 32 drafts at once), then each of
-// its warps adds up the weights of a contiguous segment of the vocabulary in 64 bits; the segments' sums are exchanged through
-// shared memory, and the one that the random number falls into is gone through once more, in order.
-// Bound: HBM where there are many sequences, latency of four dependent reads where there are few.
+// its warps adds up the weights of a contiguous segment of the vocabulary in 64 bits; the blocks' sums are exchanged through
+// shared memory, and the one that the random number falls into goes once more through the segment that it falls into, in order.
+// Sums are kept in 64 bits because the token is found by comparing them: with 128,000 shares of 10^-5 an error of 10^-7
+// would move their ends by a hundredth.
+// Bound: latency where there are few sequences (six dependent steps: offsets, drafts, their probabilities, the row, the blocks' sums,
+// the segment), HBM where there are many.  One B200: one sequence of 32,000 32-bit entries 5.3 us, 33 of 50,257 bf16 ones 9.0; 128 of
+// 128,000 32-bit ones (129 MB) 27 us, 4.8 TB/s: a single wave of blocks, whose first and last steps are not hidden behind the reads.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -305,12 +305,14 @@ def test_a_million_pages():
         assert [to.get(p, p) for p in r2["page_table"][s, :k].tolist()] == r3["page_table"][s, :k].tolist()
 
 
-def test_captured_and_on_other_streams():
-    """In place, replayed: every replay is one more round.  Two calls at once on two streams have workspaces of their own."""
+@pytest.mark.parametrize("more", [20, 700])
+def test_captured_and_on_other_streams(more):
+    """In place, replayed: every replay is one more round.  Two calls at once on two streams have workspaces of their own.  By one block
+    and by sixteen."""
     h = hos()
     pool = Pool(9, 16, 16, 200, 300)
-    pool.entries += 20
-    pool.rows = [row + [-1] * 20 for row in pool.rows]
+    pool.entries += more
+    pool.rows = [row + [-1] * more for row in pool.rows]
     refs, table, lens = pool.device()
     one = torch.ones_like(lens)
     new = torch.empty_like(lens)
@@ -329,7 +331,7 @@ def test_captured_and_on_other_streams():
         state = want[:3]
         assert refs.tolist() == state[0] and table.tolist() == state[1] and lens.tolist() == state[2]
         assert r["count"].tolist() == [len(want[3])] and r["status"].tolist() == want[5]
-    pools = [Pool(50 + i, 64, 16, 400, 50) for i in range(2)]
+    pools = [Pool(50 + i, 64, 16, 400, 50, entries=more + 60) for i in range(2)]
     given = [(p.device(), dev(p.targets(i, True)), p.targets(i, True)) for i, p in enumerate(pools)]
     streams, got = [torch.cuda.Stream() for _ in pools], []
     torch.cuda.synchronize()
@@ -342,6 +344,41 @@ def test_captured_and_on_other_streams():
         p = pools[i % 2]
         want = P.resize(p.refs, p.rows, p.lens, given[i % 2][2], 16, p.entries)
         assert r["refs"].tolist() == want[0] and r["page_table"].tolist() == want[1]
+
+
+@pytest.mark.parametrize("entries", [40, 600])
+def test_a_chain_of_calls_in_one_graph(entries):
+    """Resize, fork, compact and resize again, each on what the one before left, replayed on other states."""
+    h = hos()
+    pools = [Pool(70 + i, 40, 16, 300, 60, entries=entries) for i in range(4)]
+    r = random.Random(3)
+    parent = [r.randrange(-1, 40) for _ in range(50)]
+    news = [(p.targets(1, False), [r.choice([0, 3, 20]) for _ in range(50)]) for p in pools]
+    n = max(p.n_pages for p in pools)
+    for p in pools:
+        p.refs += [0] * (n - p.n_pages)
+        p.n_pages = n
+    refs, table, lens = pools[0].device()
+    new, add, par = dev(news[0][0]), dev(news[0][1]), dev(parent)
+    h.hos_kv_fork(refs, table, lens, par, 16)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a = h.hos_kv_resize(refs, table, lens, new, 16)
+        b = h.hos_kv_fork(a["refs"], a["page_table"], a["kv_len"], par, 16)
+        c = h.hos_kv_compact(b["refs"], b["page_table"], b["kv_len"], 16)
+        d = h.hos_kv_resize(c["refs"], c["page_table"], c["kv_len"], c["kv_len"] + add, 16)
+    for i in (0, 2, 1, 3, 3, 0):
+        p = pools[i]
+        for x, y in zip((refs, table, lens, new, add), (*p.device(), dev(news[i][0]), dev(news[i][1]))):
+            x.copy_(y)
+        graph.replay()
+        w = P.resize(p.refs, p.rows, p.lens, news[i][0], 16, entries)
+        w = P.fork(*w[:3], parent, 16, entries)
+        k = P.compact(*w[:3], 16, entries)
+        w = P.resize(k[0], k[1], w[2], [x + y for x, y in zip(w[2], news[i][1])], 16, entries)
+        assert d["refs"].tolist() == w[0] and d["page_table"].tolist() == w[1] and d["kv_len"].tolist() == w[2]
+        assert d["src"].tolist()[:len(w[3])] == w[3] and d["status"].tolist() == w[5]
 
 
 def test_refusals():
