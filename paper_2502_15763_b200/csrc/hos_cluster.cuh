@@ -1,4 +1,4 @@
-// Blocks of a cluster: who is who, their barrier, and reading one another's shared memory.
+// Blocks of a cluster: who is who, their barrier, and writing to one another's shared memory.
 #pragma once
 
 #include <stdint.h>
@@ -24,25 +24,22 @@ __device__ __forceinline__ void cluster_or_block_sync() {
     if (cluster_size() == 1) __syncthreads();
     else cluster_sync();
 }
-// The same in two halves: what this block has read of others' shared memory is behind it when they pass the second one.
+// The same in two halves, with work of one's own in between.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// The words of another block's shared memory that lie where *mine does in this one's.
+// Writes to another block's shared memory, where *mine is in this one's.  That block must have begun (a barrier of the cluster before)
+// and sees it after the next barrier.
 __device__ __forceinline__ uint32_t address_in_block(const void* mine, int block) {
     uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
     asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(a) : "r"(block));
     return a;
 }
-__device__ __forceinline__ double read_of_block(const double* mine, int block) {
-    double v;
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(address_in_block(mine, block)) : "memory");
-    return v;
+__device__ __forceinline__ void write_to_block(double* mine, int block, double v) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(address_in_block(mine, block)), "d"(v) : "memory");
 }
-__device__ __forceinline__ int4 read_of_block(const int4* mine, int block) {
-    int4 v;
-    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "r"(address_in_block(mine, block)) : "memory");
-    return v;
+__device__ __forceinline__ void write_to_block(int4* mine, int block, const int4& v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(address_in_block(mine, block)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
 }
 
 }  // namespace hos

@@ -20,7 +20,7 @@
 namespace hos {
 namespace {
 
-constexpr int THREADS = 512, WARPS = THREADS / 32;
+constexpr int THREADS = 512, WARPS = THREADS / 32, MOST_BLOCKS = 8;
 
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
@@ -227,10 +227,11 @@ __device__ __forceinline__ void search(const hos_drafts& d, int s, long long row
 
 template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_drafts(const __grid_constant__ hos_drafts d) {
     __shared__ Verdict verdict;
-    __shared__ double sums[WARPS], total;
+    __shared__ double sums[WARPS], board[2][MOST_BLOCKS];  // of this block's warps; of all blocks, in each pass
     pdl_launch_dependents();
     pdl_wait();
     const int blocks = cluster_size(), rank = cluster_rank(), s = (int)blockIdx.x / blocks;
+    if (blocks > 1) cluster_arrive();                  // all blocks have begun when everybody has passed the second half
     if (warp_id() == 0) {
         const Verdict v = judge<T>(d, s);
         if (lane_id() == 0) verdict = v;
@@ -248,6 +249,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
             if (d.status) d.status[s] = v.flags;
         }
     }
+    if (blocks > 1) cluster_wait();
     if (v.n == 0) return;                              // the whole cluster
     const bool rejected = v.accepted < k;
     const long long row = v.off + v.accepted;
@@ -270,15 +272,13 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
         if (lane_id() == 0) sums[warp_id()] = sum;
         __syncthreads();
         double own = lane_id() < WARPS ? sums[lane_id()] : 0.0, upto = warp_sum_upto(own);
-        if (threadIdx.x == 31) total = upto;
+        const double mine = __shfl_sync(FULL, upto, 31);
+        if ((int)threadIdx.x < blocks) write_to_block(&board[pass][rank], (int)threadIdx.x, mine);
         cluster_or_block_sync();
-        const double of_block = lane_id() < blocks ? read_of_block(&total, lane_id()) : 0.0;
+        const double of_block = lane_id() < blocks ? board[pass][lane_id()] : 0.0;
         const double upto_block = warp_sum_upto(of_block);
-        if (blocks > 1) cluster_arrive();
         const double all = __shfl_sync(FULL, upto_block, 31);
         if (!(all > 0.0)) {
-            if (blocks > 1) cluster_wait();
-            else __syncthreads();
             if (rejected && pass == 0) {
                 w.q = nullptr;
                 w.banned = -1;
@@ -301,7 +301,6 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
             if (to - from <= THREADS) search<1>(d, s, row, w, from, to, wide, left, sums);
             else search<8>(d, s, row, w, from, to, wide, left, sums);
         }
-        if (blocks > 1) cluster_wait();
         return;
     }
 }
@@ -310,7 +309,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
 // 2,048 entries each at least.  One, 2, 4, 8, 16, us: one sequence of 32,000 32-bit entries 7.5, 6.8, 5.3, 5.3, 5.8; 33 of 50,257
 // bf16 ones 11.5, 10.6, 9.0, 10.1, 20.6; 128 of 128,000 32-bit ones 36, 27, 32, 41, 73.
 template <typename T> cudaError_t verify(const hos_drafts& d, cudaStream_t st) {
-    int blocks = 8;
+    int blocks = MOST_BLOCKS;
     while (blocks > 1 && ((long long)d.n_seq * blocks > 256 || d.vocab < 2048 * blocks)) blocks >>= 1;
     return launch_clusters("k_verify_drafts", k_verify_drafts<T>, d.n_seq * blocks, blocks, THREADS, st, d);
 }

@@ -49,22 +49,22 @@ __device__ __forceinline__ int sum_before_lane(int v) {
     return lane_id() == 0 ? 0 : s;
 }
 
-// What the blocks tell one another: each writes `mine`, in shared memory, by one thread before a barrier of the cluster.  One warp of a
-// block reads what the others have written (all 32 of all 16 blocks at once took 2 us).
+// What the blocks tell one another: one warp of each writes its sums to all the others' boards before a barrier of the cluster (read from
+// theirs after it, by all warps of all blocks at once, took 2 us).
+constexpr int MOST_BLOCKS = 16;
 struct Shares { int4 before, all; };
-__device__ __forceinline__ Shares shares_of(const int4* mine, Shares* board) {
+__device__ __forceinline__ void tell(int4* board, const int4& mine) {
+    if (lane_id() < cluster_size()) write_to_block(board + cluster_rank(), lane_id(), mine);
+}
+__device__ __forceinline__ Shares heard(const int4* board) {
     const int rank = cluster_rank(), n = cluster_size();
-    if (n == 1) return Shares{make_int4(0, 0, 0, 0), *mine};
-    if (warp_id() == 0) {
-        Shares s;
-        const int4 v = lane_id() < n ? read_of_block(mine, lane_id()) : make_int4(0, 0, 0, 0);
-        const bool b = lane_id() < rank;
-        s.all = make_int4(min(sum_of_warp(v.x), PLENTY), sum_of_warp(v.y), sum_of_warp(v.z), sum_of_warp(v.w));
-        s.before = make_int4(min(sum_of_warp(b ? v.x : 0), PLENTY), sum_of_warp(b ? v.y : 0), sum_of_warp(b ? v.z : 0), sum_of_warp(b ? v.w : 0));
-        if (lane_id() == 0) *board = s;
-    }
-    __syncthreads();
-    return *board;
+    const int4 v = lane_id() < n ? board[lane_id()] : make_int4(0, 0, 0, 0);
+    if (n == 1) return Shares{make_int4(0, 0, 0, 0), board[0]};
+    Shares s;
+    const bool b = lane_id() < rank;
+    s.all = make_int4(min(sum_of_warp(v.x), PLENTY), sum_of_warp(v.y), sum_of_warp(v.z), sum_of_warp(v.w));
+    s.before = make_int4(min(sum_of_warp(b ? v.x : 0), PLENTY), sum_of_warp(b ? v.y : 0), sum_of_warp(b ? v.z : 0), sum_of_warp(b ? v.w : 0));
+    return s;
 }
 
 __device__ __forceinline__ bool is_page(const PagesView& p, int page) { return (unsigned)page < (unsigned)p.n_pages; }
@@ -74,36 +74,45 @@ __device__ __forceinline__ void flag(const PagesView& p, int s) {
     if (p.status) atomicOr(p.status + s, HOS_ST_INVALID);
 }
 
-// A warp's pages, 32 at a time, as masks of those whose count is zero.  The loads of AHEAD groups are on their way at once; the masks
-// of the first 32 groups stay with the lanes for a second pass (a pool of up to 32,768 pages a block is read once).
+// A warp's pages in groups of 32, as masks of those whose count is zero.  The loads of AHEAD groups are on their way at once; the masks
+// of the first 32 groups stay with the lanes, lane g has group g: a pool of up to 32,768 pages a block is read once, and what is
+// counted in it takes one step instead of one a group (a group is some 50 instructions of 32 warps, 0.2 us).
 constexpr int AHEAD = 8;
 struct FreeMasks {
     Range part;
     unsigned kept;                                     // of group lane_id()
-    template <typename F> __device__ __forceinline__ void first_pass(const int32_t* refs, F&& f) {
+    __device__ __forceinline__ int group_first(int g) const { return part.first + 32 * g; }
+    __device__ __forceinline__ unsigned load(const int32_t* refs, int g) const {
+        const int i = group_first(g) + lane_id();
+        return __ballot_sync(FULL, i < part.last && __ldcg(refs + i) == 0);
+    }
+    __device__ __forceinline__ void read(const int32_t* refs) {
         kept = 0;
-        for (int g0 = 0; part.first + 32 * g0 < part.last; g0 += AHEAD) {
+        for (int g0 = 0; g0 < 32 && group_first(g0) < part.last; g0 += AHEAD) {
             int r[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int i = part.first + 32 * (g0 + k) + lane_id();
+                const int i = group_first(g0 + k) + lane_id();
                 r[k] = i < part.last ? __ldcg(refs + i) : 1;
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const unsigned m = __ballot_sync(FULL, r[k] == 0);
                 if (g0 + k == lane_id()) kept = m;
-                f(part.first + 32 * (g0 + k), m);
             }
         }
     }
-    // f(first page of the group, mask) until it returns false
-    template <typename F> __device__ __forceinline__ void again(const int32_t* refs, F&& f) const {
-        for (int g = 0; part.first + 32 * g < part.last; ++g) {
-            const int i0 = part.first + 32 * g, i = i0 + lane_id();
-            const unsigned m = g < 32 ? __shfl_sync(FULL, kept, g) : __ballot_sync(FULL, i < part.last && __ldcg(refs + i) == 0);
-            if (!f(i0, m)) return;
-        }
+    // Sum over the groups of f(first page, mask).
+    template <typename F> __device__ __forceinline__ int sum(const int32_t* refs, F&& f) const {
+        const int mine = group_first(lane_id());
+        int n = sum_of_warp(mine < part.last ? f(mine, kept) : 0);
+        for (int g = 32; group_first(g) < part.last; ++g) n += f(group_first(g), load(refs, g));
+        return n;
+    }
+    // f(first page, mask) by the whole warp, group by group, until it returns false
+    template <typename F> __device__ __forceinline__ void each(const int32_t* refs, F&& f) const {
+        for (int g = 0; group_first(g) < part.last; ++g)
+            if (!f(group_first(g), g < 32 ? __shfl_sync(FULL, kept, g) : load(refs, g))) return;
     }
     __device__ __forceinline__ unsigned there(int i0) const { return part.last - i0 >= 32 ? FULL : (1u << (part.last - i0)) - 1u; }
 };
@@ -126,6 +135,11 @@ constexpr int EACH = 8, PIECE = 32 * EACH;
 struct Piece { int e[EACH]; };
 __device__ __forceinline__ Piece load_piece(const int32_t* row, int first, int last) {
     Piece x;
+    if (first >= last) {                               // behind what a row holds: most pieces of a wide table
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) x.e[k] = -1;
+        return x;
+    }
     const int left = last - first - lane_id();
     const int32_t* at = row + (first + lane_id());
 #pragma unroll
@@ -217,8 +231,7 @@ __device__ __forceinline__ Change change_of(const PagesView& p, int s) {
 // holds it (two atomics a holder: how many, and the last); then sums over the sequences give each its place among the free pages, taken
 // by number, and the first that is short is the first whose sum is beyond them, as all sums after it are.
 __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant__ PagesView p) {
-    __shared__ int4 mine;
-    __shared__ Shares board;
+    __shared__ int4 board[MOST_BLOCKS];
     __shared__ int of_warp[3][WARPS];
     __shared__ RowList stay, go;
     pdl_launch_dependents();
@@ -229,10 +242,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
     auto old_row = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.seq * p.in_stride, j, r.last); };
     auto keep = [&](const RowWork& r, int j, const Piece& x) { store_piece(p.table + (long long)r.seq * p.out_stride, j, p.max_pages, x); };
     auto give_up = [&](const RowWork& r, int j, const Piece& x) {
+        int was[EACH];                                 // all on their way before the first is looked at
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) was[k] = is_page(p, x.e[k]) ? atomicSub(p.refs + x.e[k], 1) : 32 * k < r.last - j - lane_id() ? 0 : 1;
         bool bad = false;
 #pragma unroll
-        for (int k = 0; k < EACH; ++k)
-            if (32 * k < r.last - j - lane_id()) bad |= !is_page(p, x.e[k]) || atomicSub(p.refs + x.e[k], 1) <= 0;
+        for (int k = 0; k < EACH; ++k) bad |= was[k] <= 0;
         if (bad) flag(p, r.seq);
         if (in_place) store_piece(p.table + (long long)r.seq * p.out_stride, j, r.last, Piece{{-1, -1, -1, -1, -1, -1, -1, -1}});
     };
@@ -297,8 +312,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
         latest = __ldcg(p.latest + first.page);
     }
     FreeMasks masks{warp_part(pages), 0};
-    int n_free = 0;
-    masks.first_pass(p.refs, [&](int, unsigned m) { n_free += __popc(m); });
+    masks.read(p.refs);
+    const int n_free = masks.sum(p.refs, [&](int, unsigned m) { return __popc(m); });
     if (lane_id() == 0) of_warp[2][warp_id()] = n_free;
     int sum_takes = 0, sum_splits = 0;
     ResizePlan of_first = {0, 0, 0};
@@ -335,16 +350,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
     const int free_of_lane = of_warp[2][lane_id()];
     if (warp_id() == 0) {
         const int all = sum_of_warp(free_of_lane);
-        if (lane_id() == 0) mine = make_int4(sum_takes, sum_splits, all, 0);
+        tell(board, make_int4(sum_takes, sum_splits, all, 0));
     }
     cluster_or_block_sync();
-    const Shares shares = shares_of(&mine, &board);
+    const Shares shares = heard(board);
     const int wanted = shares.all.x, free = shares.all.z;
     if (tid == 0 && cluster_rank() == 0 && wanted <= free) *p.count = shares.all.y;
     // the free pages in order, as many as are taken
     int at = shares.before.z + sum_of_warp(lane_id() < warp_id() ? free_of_lane : 0);
     if (at < wanted)
-        masks.again(p.refs, [&](int i0, unsigned m) {
+        masks.each(p.refs, [&](int i0, unsigned m) {
             const int k = at + __popc(m & lanes_before());
             if ((m >> lane_id() & 1u) && k < wanted) p.queue[k] = i0 + lane_id();
             at += __popc(m);
@@ -459,12 +474,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_fork(const __grid_constant__ 
 // With n pages in use there are as many of them from n on as there are free ones below n; both are numbered in order, and the k-th goes to the
 // k-th.  A table entry finds its new page by two reads: its place among the moves, and where that one goes.
 __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant__ PagesView p) {
-    __shared__ int4 live, others;
-    __shared__ Shares board[2];
+    __shared__ int4 live[MOST_BLOCKS], others[MOST_BLOCKS];
     __shared__ int of_warp[3][WARPS];
     __shared__ RowList list;
     pdl_launch_dependents();
     pdl_wait();
+    if (cluster_size() > 1) cluster_arrive();          // all blocks have begun when everybody has passed the second half
     const Range seqs = block_part(p.n_seq), pages = block_part(p.n_pages);
     const int tid = (int)threadIdx.x;
     const bool in_place = p.table == p.table_in;
@@ -474,42 +489,38 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
         if (valid || !in_place) list.add(RowWork{s, 0, valid ? pages_of(p, len) : p.max_pages, valid});
     };
     FreeMasks masks{warp_part(pages), 0};
-    int n = 0;
-    masks.first_pass(p.refs_in, [&](int i0, unsigned m) {
-        if (i0 < masks.part.last) n += __popc(masks.there(i0) & ~m);
-    });
+    masks.read(p.refs_in);
+    const int n = masks.sum(p.refs_in, [&](int i0, unsigned m) { return __popc(masks.there(i0) & ~m); });
     if (lane_id() == 0) of_warp[0][warp_id()] = n;
     copy_counts(p, pages);
+    const int first_len = seqs.first + tid < seqs.last ? p.len_in[seqs.first + tid] : 0;
     for (int s = seqs.first + tid; s < seqs.last; s += THREADS)
-        if (p.status) p.status[s] = is_length(p, p.len_in[s]) ? 0 : HOS_ST_INVALID;
+        if (p.status) p.status[s] = is_length(p, s == seqs.first + tid ? first_len : p.len_in[s]) ? 0 : HOS_ST_INVALID;
+    if (cluster_size() > 1) cluster_wait();
     __syncthreads();
     if (warp_id() == 0) {
         const int all = sum_of_warp(of_warp[0][lane_id()]);
-        if (lane_id() == 0) live = make_int4(0, 0, 0, all);
+        tell(live, make_int4(0, 0, 0, all));
     }
     cluster_or_block_sync();
-    const int n_live = shares_of(&live, &board[0]).all.w;
+    const int n_live = heard(live).all.w;
     // pages in use behind the first n_live, and free ones among those: as many of the one as of the other
     auto behind = [&](int i0) { return i0 >= n_live ? FULL : n_live - i0 >= 32 ? 0u : FULL << (n_live - i0); };
-    int late = 0, hole = 0;
-    masks.again(p.refs_in, [&](int i0, unsigned m) {
-        late += __popc(masks.there(i0) & ~m & behind(i0));
-        hole += __popc(m & ~behind(i0));
-        return true;
-    });
+    const int late = masks.sum(p.refs_in, [&](int i0, unsigned m) { return __popc(masks.there(i0) & ~m & behind(i0)); });
+    const int hole = masks.sum(p.refs_in, [&](int i0, unsigned m) { return __popc(m & ~behind(i0)); });
     if (lane_id() == 0) of_warp[1][warp_id()] = late, of_warp[2][warp_id()] = hole;
     __syncthreads();
     const int late_of_lane = of_warp[1][lane_id()], hole_of_lane = of_warp[2][lane_id()];
     if (warp_id() == 0) {
         const int a = sum_of_warp(late_of_lane), b = sum_of_warp(hole_of_lane);
-        if (lane_id() == 0) others = make_int4(0, a, b, 0);
+        tell(others, make_int4(0, a, b, 0));
     }
     cluster_or_block_sync();
-    const Shares shares = shares_of(&others, &board[1]);
+    const Shares shares = heard(others);
     const bool b = lane_id() < warp_id();
     int late_at = shares.before.y + sum_of_warp(b ? late_of_lane : 0), hole_at = shares.before.z + sum_of_warp(b ? hole_of_lane : 0);
     const int count = shares.all.y;
-    masks.again(p.refs_in, [&](int i0, unsigned m) {
+    masks.each(p.refs_in, [&](int i0, unsigned m) {
         const int i = i0 + lane_id();
         const unsigned a = masks.there(i0) & ~m & behind(i0), h = m & ~behind(i0), me = 1u << lane_id();
         const int k = late_at + __popc(a & lanes_before());
@@ -523,11 +534,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     for (int i = max(count, pages.first) + tid; i < pages.last; i += THREADS) p.src[i] = p.dst[i] = -1;
     if (tid == 0 && cluster_rank() == 0) *p.count = count;
     list.begin(in_place ? 1 : (p.max_pages + PIECE - 1) / PIECE);
-    if (seqs.first + tid < seqs.last) list_row(seqs.first + tid, p.len_in[seqs.first + tid]);
+    if (seqs.first + tid < seqs.last) list_row(seqs.first + tid, first_len);
     Cursor at = first_piece(list, row);
     cluster_or_block_sync();
-    int k = cluster_rank() * THREADS + tid, from = 0, to = 0;      // a move whose count goes along; its numbers come while the rows are worked on
-    if (k < count) from = __ldcg(p.src + k), to = __ldcg(p.dst + k);
+    // a move, whose count goes along: its numbers come while the rows are worked on
+    const int step = cluster_size() * THREADS, move = cluster_rank() * THREADS + tid;
+    int from = 0, to = 0;
+    if (move < count) from = __ldcg(p.src + move), to = __ldcg(p.dst + move);
     for (int s0 = seqs.first; s0 < seqs.last; s0 += THREADS) {
         if (s0 > seqs.first) {
             __syncthreads();
@@ -536,27 +549,28 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
             at = first_piece(list, row);
         }
         all_pieces(list, at, row, [&](const RowWork& r, int j, Piece x) {
-            int place[EACH];                           // among the moves
-            bool bad = false;
+            if (r.from && j < r.last) {
+                int place[EACH];                       // among the moves
+                bool bad = false;
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                const bool there = r.from && 32 * k < r.last - j - lane_id(), page = is_page(p, x.e[k]), moves = there && page && x.e[k] >= n_live;
-                place[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
-                bad |= there && (!page || (moves && place[k] < 0));
+                for (int k = 0; k < EACH; ++k) {
+                    const bool there = 32 * k < r.last - j - lane_id(), page = is_page(p, x.e[k]), moves = there && page && x.e[k] >= n_live;
+                    place[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
+                    bad |= there && (!page || (moves && place[k] < 0));
+                }
+#pragma unroll
+                for (int k = 0; k < EACH; ++k)
+                    if (place[k] >= 0) x.e[k] = __ldcg(p.dst + place[k]);
+                if (bad) flag(p, r.seq);
             }
-#pragma unroll
-            for (int k = 0; k < EACH; ++k)
-                if (place[k] >= 0) x.e[k] = __ldcg(p.dst + place[k]);
-            if (bad) flag(p, r.seq);
             store_piece(p.table + (long long)r.seq * p.out_stride, j, in_place ? r.last : p.max_pages, x);
         });
     }
-    while (k < count) {
+    for (int k = move; k < count; k += step) {
+        if (k > move) from = __ldcg(p.src + k), to = __ldcg(p.dst + k);
         const int refs = p.refs_in[from];
         p.refs[to] = refs;
         p.refs[from] = 0;
-        k += cluster_size() * THREADS;
-        if (k < count) from = __ldcg(p.src + k), to = __ldcg(p.dst + k);
     }
 }
 
@@ -617,7 +631,6 @@ template <int LAYERS> __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_
 // each, one block 0.1-0.2 us for a thousand entries).  One block, 2, 4, 8, 16, us: 16 sequences of 33 entries 5.7, 7.3, 7.4, 7.6, 7.8 (resize);
 // 128 of 519, 11,612 pages 19, 16, 15, 13, 13 (resize); 128 of 1,031, twice 38, 24, 15, 10, 8 (fork), 256 of those 137, 74, 40, 24, 16 (compact).
 constexpr long long SMALL_STATE = 8192;
-constexpr int MOST_BLOCKS = 16;
 template <void (*KERNEL)(PagesView)> cudaError_t launch_tables(const char* name, const PagesView& p, cudaStream_t st) {
     const long long rows = p.n_seq > p.n_out ? p.n_seq : p.n_out;
     const int blocks = p.n_pages + rows * p.max_pages <= SMALL_STATE ? 1 : MOST_BLOCKS;
