@@ -441,7 +441,8 @@ typedef struct hos_kv_moves {    /* HOST struct */
  *      from those that are free after 1.  The first sequence whose pages are not there, and every
  *      growing one after it, keeps its length and pages (HOS_ST_PAGES).
  * A length outside [0, max_pages * page_size], old or new: the sequence stays as it is, with its whole row
- * (HOS_ST_INVALID).  A page that is given up more often than it is held: HOS_ST_INVALID.
+ * (HOS_ST_INVALID).  A page that is given up more often than refs says it is held has a count below zero then and is
+ * not free (HOS_ST_INVALID).
  * `out` may be `in`, as a whole or array by array.  The copies have to be made before the new tokens are
  * appended, and before the next call of these.
  */
@@ -496,7 +497,7 @@ int hos_kv_copy_pages(const hos_kv_cache* to, const hos_kv_cache* from, int n_la
  *   kv_len, new_len [n_seq], both or neither: new_len = kv_len - k + accepted (the length to cut the cache to)
  *   status [n_seq], nullable, written: HOS_ST_INVALID where offsets are out of range (accepted 0, next -1, nothing
  *     else), the first draft that is not accepted is outside [0, vocab), or w is zero everywhere (next -1)
- * A sequence without tokens: accepted 0, next -1.
+ * A sequence without tokens: accepted 0, next -1.  n_seq <= 262,144, vocab <= 2^30; results are other memory than inputs.
  */
 typedef struct hos_drafts {      /* HOST struct; DEVICE arrays */
     int32_t n_seq, n_tokens, vocab, type;
