@@ -98,6 +98,7 @@ template <typename T> struct Weights {
             float small = 0.0f;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
+                if (i0 - lane_id() * N + k * 32 * N >= whole) break;       // the end of the warp's
                 const int out = banned - (i0 + k * 32 * N);        // which of these is the banned one
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
@@ -231,7 +232,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
     pdl_launch_dependents();
     pdl_wait();
     const int blocks = cluster_size(), rank = cluster_rank(), s = (int)blockIdx.x / blocks;
-    if (blocks > 1) cluster_arrive();                  // all blocks have begun when everybody has passed the second half
+    cluster_begun_arrive();
     if (warp_id() == 0) {
         const Verdict v = judge<T>(d, s);
         if (lane_id() == 0) verdict = v;
@@ -249,7 +250,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
             if (d.status) d.status[s] = v.flags;
         }
     }
-    if (blocks > 1) cluster_wait();
+    cluster_begun_wait();
     if (v.n == 0) return;                              // the whole cluster
     const bool rejected = v.accepted < k;
     const long long row = v.off + v.accepted;

@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     __shared__ RowList list;
     pdl_launch_dependents();
     pdl_wait();
-    if (cluster_size() > 1) cluster_arrive();          // all blocks have begun when everybody has passed the second half
+    cluster_begun_arrive();
     const Range seqs = block_part(p.n_seq), pages = block_part(p.n_pages);
     const int tid = (int)threadIdx.x;
     const bool in_place = p.table == p.table_in;
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     const int first_len = seqs.first + tid < seqs.last ? p.len_in[seqs.first + tid] : 0;
     for (int s = seqs.first + tid; s < seqs.last; s += THREADS)
         if (p.status) p.status[s] = is_length(p, s == seqs.first + tid ? first_len : p.len_in[s]) ? 0 : HOS_ST_INVALID;
-    if (cluster_size() > 1) cluster_wait();
+    cluster_begun_wait();
     __syncthreads();
     if (warp_id() == 0) {
         const int all = sum_of_warp(of_warp[0][lane_id()]);
