@@ -7,8 +7,9 @@
 // Sums are kept in 64 bits because the token is found by comparing them: with 128,000 shares of 10^-5 an error of 10^-7
 // would move their ends by a hundredth.
 // Bound: latency where there are few sequences (six dependent steps: offsets, drafts, their probabilities, the row, the blocks' sums,
-// the segment), HBM where there are many.  One B200: one sequence of 32,000 32-bit entries 5.3 us, 33 of 50,257 bf16 ones 9.0; 128 of
-// 128,000 32-bit ones (129 MB) 27 us, 4.8 TB/s: a single wave of blocks, whose first and last steps are not hidden behind the reads.
+// the segment); where there are many, HBM for 32-bit entries, instructions for 16-bit ones (ten a pair).  One B200: one sequence of 32,000
+// 32-bit entries 5.0 us, 33 of 50,257 bf16 ones 7.7; 128 of 128,000 32-bit ones (129 MB) 27 us, 4.8 TB/s: a single wave of blocks, not even
+// over the SMs, whose first and last steps are not hidden behind the reads; 800 of them 6.8 TB/s, of bf16 ones 5.0.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -77,9 +78,10 @@ template <typename T> struct Weights {
         for (int k = 0; k < K; ++k) x[k] = a + k < b ? at(a + k) : 0.0;
     }
     // Sum over [a, b) by one warp; where they can be read 16 bytes at a time from `a` on, in both rows.  A difference x - y > 0 is
-    // d + e exactly, d rounded to 32 bits and e = (x - d) - y (Dekker, 1971).  The d are added up in 64 bits; the e, below 2^-24 of
-    // them, 16 or 32 in 32 bits first, which leaves 2^-43 of the sum.  So a conversion and a 64-bit sum are left of two and three
-    // (they go at a fraction of the others' rate).
+    // d + e exactly, d rounded to 32 bits and e = (x - d) - y (Dekker, 1971); with the larger of x and y in the place of x both are
+    // zero where nothing is left.  The d are added up in 64 bits; the e, below 2^-24 of them, 16 or 32 in 32 bits first, which leaves 2^-43 of the
+    // sum.  So a conversion and a 64-bit sum are left of two and three (they go at a fraction of the others' rate).  An infinity or a NaN that
+    // does not fall out by itself makes the sum one: the caller looks.
     template <bool Q> __device__ __forceinline__ double sum_wide(int a, int b) const {
         constexpr int N = Vec<T>::N, AHEAD = 4;
         double s[2] = {0.0, 0.0};
@@ -102,16 +104,15 @@ template <typename T> struct Weights {
                 const int out = banned - (i0 + k * 32 * N);        // which of these is the banned one
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const float v = x[k].at(j);
                     if (Q) {
-                        const float u = draft_of(y[k].at(j)), d = v - u, e = (v - d) - u;
-                        const bool some = counts(d);
-                        s[j & 1] += (double)(some ? d : 0.0f);
-                        small += some ? e : 0.0f;
+                        const float u = draft_of(y[k].at(j)), v = fmaxf(x[k].at(j), u), d = v - u;
+                        s[j & 1] += (double)d;
+                        small += (v - d) - u;
                     } else {
-                        s[j & 1] += (double)(counts(v) && j != out ? v : 0.0f);
+                        s[j & 1] += (double)fmaxf(x[k].at(j), 0.0f);
                     }
                 }
+                if (!Q && (unsigned)out < (unsigned)N) return __longlong_as_double(0x7FF8000000000000ll);      // not by this way
             }
             if (Q) s[0] += (double)small;
         }
@@ -119,11 +120,16 @@ template <typename T> struct Weights {
         if (i < b) s[0] += at(i);
         return s[0] + s[1];
     }
-    __device__ __forceinline__ double sum(int a, int b, bool wide) const {
-        if (wide) return q ? sum_wide<true>(a, b) : sum_wide<false>(a, b);
+    __device__ __forceinline__ double sum_plain(int a, int b) const {
         double s = 0.0;
 #pragma unroll 8
         for (int i = a + lane_id(); i < b; i += 32) s += at(i);
+        return s;
+    }
+    // Of the whole warp.
+    __device__ __forceinline__ double sum(int a, int b, bool wide) const {
+        double s = !wide ? sum_plain(a, b) : q ? sum_wide<true>(a, b) : sum_wide<false>(a, b);
+        if (wide && __any_sync(FULL, !(s < __longlong_as_double(0x7FF0000000000000ll)))) s = sum_plain(a, b);
         return s;
     }
 };
@@ -306,12 +312,12 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
     }
 }
 
-// As many blocks a sequence as there are room for at once (two of 512 threads an SM, and as good as all SMs even), up to 8, with
-// 2,048 entries each at least.  One, 2, 4, 8, 16, us: one sequence of 32,000 32-bit entries 7.5, 6.8, 5.3, 5.3, 5.8; 33 of 50,257
-// bf16 ones 11.5, 10.6, 9.0, 10.1, 20.6; 128 of 128,000 32-bit ones 36, 27, 32, 41, 73.
+// As many blocks a sequence as there is room for at once (two of 512 threads an SM), up to 8, with 2,048 entries each at least.  One, 2, 4,
+// 8, us, p and q in 32 bits: one sequence of 32,000 entries 8.3, 7.4, 5.8, 5.7; of 128,000 17, 11, 8.7, 7.4; 64 of those 20, 16, 12, 16; 100 of
+// them 25, 19, 21, 27; 296 of them 47 (6.4 TB/s), 51, 60, 73.
 template <typename T> cudaError_t verify(const hos_drafts& d, cudaStream_t st) {
     int blocks = MOST_BLOCKS;
-    while (blocks > 1 && ((long long)d.n_seq * blocks > 256 || d.vocab < 2048 * blocks)) blocks >>= 1;
+    while (blocks > 1 && ((long long)d.n_seq * blocks > 2 * ATTN_SMS || d.vocab < 2048 * blocks)) blocks >>= 1;
     return launch_clusters("k_verify_drafts", k_verify_drafts<T>, d.n_seq * blocks, blocks, THREADS, st, d);
 }
 

@@ -150,6 +150,18 @@ def test_one_token_has_everything(dt):
     check(sure, None, tokens, off, ua, us)
 
 
+@pytest.mark.parametrize("dt,vocab,share", [("f32", 90, 0.05), ("f32", 20000, 0.0002), ("bf16", 20000, 0.0002), ("f16", 4099, 0.001)])
+def test_strange_entries(dt, vocab, share):
+    """A few of them in large rows, anywhere."""
+    for seed in range(4):
+        target, draft, tokens, off, ua, us = make([4, 1, 0, 6, 2], vocab, dt, 40 + seed)
+        g = torch.Generator().manual_seed(seed)
+        for t, more in ((target, (math.inf, -math.inf, math.nan, -2.0, 0.0)), (draft, (math.inf, -math.inf, math.nan, -2.0, 0.0))):
+            for x in more:
+                t[torch.rand(t.shape, generator=g) < share] = x
+        check(target, draft if seed % 2 else None, tokens, off, ua, us)
+
+
 def test_strange_probabilities():
     """Zeros, negative entries, infinities and NaN count as nothing, in the target, the draft and at the draft's place."""
     for seed in range(6):
