@@ -89,6 +89,12 @@ def test_many_sequences(n_seq):
     check(*make([s % 4 for s in range(n_seq)], 2000, "f32", n_seq))
 
 
+@pytest.mark.parametrize("n_seq,vocab,dt", [(20, 20011, "f32"), (64, 9000, "bf16"), (140, 4100, "f32"), (310, 4500, "f16")])
+def test_one_to_eight_blocks_a_sequence(n_seq, vocab, dt):
+    check(*make([s % 3 for s in range(n_seq)], vocab, dt, n_seq))
+    check(*make([s % 2 for s in range(n_seq)], vocab, dt, n_seq + 1, lookup=True))
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16"])
 @pytest.mark.parametrize("pad,shift", [((1, 1), (0, 0)), ((3, 0), (1, 0)), ((0, 5), (0, 3)), ((8, 8), (4, 4)), ((7, 2), (5, 6))])
 @pytest.mark.parametrize("vocab", [5, 1003, 8000])
