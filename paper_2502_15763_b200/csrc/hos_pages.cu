@@ -5,8 +5,8 @@
 // of 16 whose barrier is in hardware and whose blocks exchange their sums through shared memory; a barrier through global memory or a
 // launch a phase would cost 1-2 us each.  What bounds them: for small states the reads, block barriers and counters of a
 // phase (0.6-1.2 us each); for large ones the 16 SMs' own rate (a row's entries 32 at a time, instructions as much as bytes).
-// One B200, device time: 16 sequences of 33 entries resized 5.7 us, 128 of 519 with 11,612 pages 12.2, 4 forked into 16 4.0, 128 rows of
-// 1,031 reordered 8.1, 136 pages compacted 5.1, 79,796 pages under 256 rows of 1,031 15.7.
+// One B200, device time: 16 sequences of 33 entries resized 4.8 us, 128 of 519 with 11,612 pages 9.7, 4 forked into 16 3.4, 128 rows of
+// 1,031 reordered 7.4, 136 pages compacted 4.6, 79,796 pages under 256 rows of 1,031 14.2.
 // The contents are a matter of bandwidth: each byte once in and once out, 6.6-6.7 TB/s (see k_kv_copy_pages).
 #include <algorithm>
 #include <atomic>
@@ -19,7 +19,9 @@
 namespace hos {
 namespace {
 
-constexpr int THREADS = 1024, WARPS = THREADS / 32;
+// 256, 512 and 1,024 threads, us: 16 sequences resized 4.8, 5.1, 5.8; 128 9.3, 9.9, 11.2; 4 forked 3.3, 3.4, 4.0; 128 7.5, 7.5, 8.0; 136 pages
+// compacted 4.9, 4.7, 5.4; 79,796 16.6, 14.3, 14.2.  (A barrier of 1,024 threads takes 100-160 cycles, and what all warps do alike adds up.)
+constexpr int THREADS = 512, WARPS = THREADS / 32;
 
 struct Range { int first, last; };
 // The part of n things that falls to this block.
@@ -32,6 +34,8 @@ __device__ __forceinline__ Range warp_part(Range block) {
     const int each = ((block.last - block.first + WARPS - 1) / WARPS + 31) & ~31, a = min(block.first + warp_id() * each, block.last);
     return Range{a, min(a + each, block.last)};
 }
+// Of a block's warps, the one of this lane's number.
+__device__ __forceinline__ int of_lane(const int* of_warps) { return lane_id() < WARPS ? of_warps[lane_id()] : 0; }
 __device__ __forceinline__ unsigned lanes_before() { return (1u << lane_id()) - 1u; }
 
 // Numbers of pages are added up in 32 bits.  What sequences ask for may be more than that holds; every sum stops at PLENTY, which no pool has
@@ -75,8 +79,8 @@ __device__ __forceinline__ void flag(const PagesView& p, int s) {
 }
 
 // A warp's pages in groups of 32, as masks of those whose count is zero.  The loads of AHEAD groups are on their way at once; the masks
-// of the first 32 groups stay with the lanes, lane g has group g: a pool of up to 32,768 pages a block is read once, and what is
-// counted in it takes one step instead of one a group (a group is some 50 instructions of 32 warps, 0.2 us).
+// of the first 32 groups stay with the lanes, lane g has group g: a pool of up to 16,384 pages a block is read once, and what is
+// counted in it takes one step instead of one a group (a group is some 50 instructions of all warps).
 constexpr int AHEAD = 8;
 struct FreeMasks {
     Range part;
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
         const int before = sum_before_lane(plan.takes & TAKES), all = min(before + (plan.takes & TAKES), PLENTY);
         if (lane_id() == 31) of_warp[0][warp_id()] = all, of_warp[1][warp_id()] = __popc(split);
         __syncthreads();
-        const int t = of_warp[0][lane_id()], u = of_warp[1][lane_id()];
+        const int t = of_lane(of_warp[0]), u = of_lane(of_warp[1]);
         const bool b = lane_id() < warp_id();
         plan.before = min(sum_takes + min(sum_of_warp(b ? t : 0), PLENTY) + before, PLENTY);
         plan.splits_before = sum_splits + sum_of_warp(b ? u : 0) + __popc(split & lanes_before());
@@ -347,7 +351,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_resize(const __grid_constant_
         if (s0 + THREADS < seqs.last) __syncthreads();
     }
     __syncthreads();
-    const int free_of_lane = of_warp[2][lane_id()];
+    const int free_of_lane = of_lane(of_warp[2]);
     if (warp_id() == 0) {
         const int all = sum_of_warp(free_of_lane);
         tell(board, make_int4(sum_takes, sum_splits, all, 0));
@@ -499,7 +503,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     cluster_begun_wait();
     __syncthreads();
     if (warp_id() == 0) {
-        const int all = sum_of_warp(of_warp[0][lane_id()]);
+        const int all = sum_of_warp(of_lane(of_warp[0]));
         tell(live, make_int4(0, 0, 0, all));
     }
     cluster_or_block_sync();
@@ -510,7 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     const int hole = masks.sum(p.refs_in, [&](int i0, unsigned m) { return __popc(m & ~behind(i0)); });
     if (lane_id() == 0) of_warp[1][warp_id()] = late, of_warp[2][warp_id()] = hole;
     __syncthreads();
-    const int late_of_lane = of_warp[1][lane_id()], hole_of_lane = of_warp[2][lane_id()];
+    const int late_of_lane = of_lane(of_warp[1]), hole_of_lane = of_lane(of_warp[2]);
     if (warp_id() == 0) {
         const int a = sum_of_warp(late_of_lane), b = sum_of_warp(hole_of_lane);
         tell(others, make_int4(0, a, b, 0));
@@ -628,8 +632,9 @@ template <int LAYERS> __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_
 }
 
 // A small state by one block, whose own barrier is enough; any other by a cluster of 16, the most there are (its barriers take 0.5-1 us
-// each, one block 0.1-0.2 us for a thousand entries).  One block, 2, 4, 8, 16, us: 16 sequences of 33 entries 5.7, 7.3, 7.4, 7.6, 7.8 (resize);
-// 128 of 519, 11,612 pages 19, 16, 15, 13, 13 (resize); 128 of 1,031, twice 38, 24, 15, 10, 8 (fork), 256 of those 137, 74, 40, 24, 16 (compact).
+// each, one block 0.1-0.15 us for a thousand entries).  One block, 2, 4, 8, 16, us (with 1,024 threads each): 16 sequences of 33 entries 5.8, 7.4,
+// 7.4, 7.5, 7.7 (resize); 128 of 519, 11,612 pages 17, 14, 12, 11, 11 (resize); 128 of 1,031, twice 39, 24, 15, 10, 8 (fork); 256 of those 129, 65,
+// 34, 21, 14 (compact).
 constexpr long long SMALL_STATE = 8192;
 template <void (*KERNEL)(PagesView)> cudaError_t launch_tables(const char* name, const PagesView& p, cudaStream_t st) {
     const long long rows = p.n_seq > p.n_out ? p.n_seq : p.n_out;
