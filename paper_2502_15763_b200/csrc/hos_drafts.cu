@@ -8,8 +8,8 @@
 // would move their ends by a hundredth.
 // Bound: latency where there are few sequences (six dependent steps: offsets, drafts, their probabilities, the row, the blocks' sums,
 // the segment); where there are many, HBM for 32-bit entries, instructions for 16-bit ones (ten a pair).  One B200: one sequence of 32,000
-// 32-bit entries 5.0 us, 33 of 50,257 bf16 ones 7.7; 128 of 128,000 32-bit ones (129 MB) 27 us, 4.8 TB/s: a single wave of blocks, not even
-// over the SMs, whose first and last steps are not hidden behind the reads; 800 of them 6.8 TB/s, of bf16 ones 5.0.
+// 32-bit entries 4.6 us, 33 of 50,257 bf16 ones 6.8; 128 of 128,000 32-bit ones (129 MB) 28 us, 4.6 TB/s: a single wave of blocks, not even
+// over the SMs, whose first and last steps are not hidden behind the reads; 800 of them 6.8 TB/s, of bf16 ones 4.9.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -21,7 +21,7 @@
 namespace hos {
 namespace {
 
-constexpr int THREADS = 512, WARPS = THREADS / 32, MOST_BLOCKS = 8;
+constexpr int THREADS = 256, WARPS = THREADS / 32, BLOCKS_PER_SM = 4, MOST_BLOCKS = 16;
 
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
@@ -232,7 +232,7 @@ __device__ __forceinline__ void search(const hos_drafts& d, int s, long long row
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_drafts(const __grid_constant__ hos_drafts d) {
+template <typename T> __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) k_verify_drafts(const __grid_constant__ hos_drafts d) {
     __shared__ Verdict verdict;
     __shared__ double sums[WARPS], board[2][MOST_BLOCKS];  // of this block's warps; of all blocks, in each pass
     pdl_launch_dependents();
@@ -304,7 +304,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
             const int warp = first_beyond(upto, own, left);
             left -= __shfl_sync(FULL, upto - own, warp);
             const int from = edge(rank * WARPS + warp), to = edge(rank * WARPS + warp + 1);
-            // one neighbour a thread where that is enough: 32,000 entries by 8 blocks 5.3 us, with 8 neighbours 6.2 (before the last steps)
+            // one neighbour a thread where that is enough (32,000 entries by 8 blocks of 512 threads: 5.3 us, with 8 neighbours 6.2)
             if (to - from <= THREADS) search<1>(d, s, row, w, from, to, wide, left, sums);
             else search<8>(d, s, row, w, from, to, wide, left, sums);
         }
@@ -312,12 +312,20 @@ template <typename T> __global__ void __launch_bounds__(THREADS, 2) k_verify_dra
     }
 }
 
-// As many blocks a sequence as there is room for at once (two of 512 threads an SM), up to 8, with 2,048 entries each at least.  One, 2, 4,
-// 8, us, p and q in 32 bits: one sequence of 32,000 entries 8.3, 7.4, 5.8, 5.7; of 128,000 17, 11, 8.7, 7.4; 64 of those 20, 16, 12, 16; 100 of
-// them 25, 19, 21, 27; 296 of them 47 (6.4 TB/s), 51, 60, 73.
+// As many blocks a sequence as there is room for at once, with 1,000 entries each at least and, room or not, 64,000 at most; up to 16, but
+// those only where two an SM are enough (clusters of 16 do not fill the groups of SMs that they have to stay in).  One, 2, 4, 8, 16, us, p and q in
+// 32 bits: one sequence of 32,000 entries 9.7, 7.7, 6.3, 6.1, 5.1; of 128,000 21, 15, 9.4, 7.7, 6.6; 40 of those 28, 17, 13, 12, 13; 100 of them
+// 40, 25, 19, 20, 27; 296 of them 59, 50 (6.1 TB/s), 56, 57, 76; 800 134, 121 (6.8 TB/s), 120, 129, 186.  With 512 threads, two blocks an SM and up
+// to 8 a sequence: 5.7, 7.4, 12, 19, 47 and 120.
 template <typename T> cudaError_t verify(const hos_drafts& d, cudaStream_t st) {
     int blocks = MOST_BLOCKS;
-    while (blocks > 1 && ((long long)d.n_seq * blocks > 2 * ATTN_SMS || d.vocab < 2048 * blocks)) blocks >>= 1;
+    auto room = [&] { return (long long)d.n_seq * blocks <= ATTN_SMS * (blocks > 8 ? 2 : BLOCKS_PER_SM); };
+    while (blocks > 1 && (d.vocab < 1000 * blocks || (!room() && d.vocab <= 64000 * (blocks / 2)))) blocks >>= 1;
+    static std::atomic<unsigned long long> asked{0};
+    if (blocks > 8) {
+        const cudaError_t e = ask_for_large_clusters(reinterpret_cast<const void*>(&k_verify_drafts<T>), asked);
+        if (e != cudaSuccess) return e;
+    }
     return launch_clusters("k_verify_drafts", k_verify_drafts<T>, d.n_seq * blocks, blocks, THREADS, st, d);
 }
 

@@ -9,7 +9,6 @@
 // 1,031 reordered 7.4, 136 pages compacted 4.6, 79,796 pages under 256 rows of 1,031 14.2.
 // The contents are a matter of bandwidth: each byte once in and once out, 6.6-6.7 TB/s (see k_kv_copy_pages).
 #include <algorithm>
-#include <atomic>
 
 #include "hos_cluster.cuh"
 #include "hos_kv_kernels.h"
@@ -639,14 +638,10 @@ constexpr long long SMALL_STATE = 8192;
 template <void (*KERNEL)(PagesView)> cudaError_t launch_tables(const char* name, const PagesView& p, cudaStream_t st) {
     const long long rows = p.n_seq > p.n_out ? p.n_seq : p.n_out;
     const int blocks = p.n_pages + rows * p.max_pages <= SMALL_STATE ? 1 : MOST_BLOCKS;
-    if (blocks > 8) {                                  // has to be asked for, once a device
-        static std::atomic<unsigned long long> asked{0};
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
-        if (e == cudaSuccess && (dev >= 64 || !(asked.load() >> dev & 1)))
-            e = cudaFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static std::atomic<unsigned long long> asked{0};
+    if (blocks > 8) {
+        const cudaError_t e = ask_for_large_clusters(reinterpret_cast<const void*>(KERNEL), asked);
         if (e != cudaSuccess) return e;
-        if (dev < 64) asked.fetch_or(1ull << dev);
     }
     return launch_clusters(name, KERNEL, blocks, blocks, THREADS, st, p);
 }

@@ -1,9 +1,20 @@
 // Internal launch interface of the kernels on a cache's pages and on drafted tokens.
 #pragma once
 
+#include <atomic>
+
 #include "hos_kernels.h"
 
 namespace hos {
+
+// Clusters of more than 8 blocks have to be asked for, once a kernel and device; `asked` is the kernel's own.
+inline cudaError_t ask_for_large_clusters(const void* kernel, std::atomic<unsigned long long>& asked) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !(asked.load() >> dev & 1))) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && dev < 64) asked.fetch_or(1ull << dev);
+    return e;
+}
 
 // `blocks` blocks in clusters of `cluster`, early (see launch_early).
 template <typename... Params, typename... Args>
