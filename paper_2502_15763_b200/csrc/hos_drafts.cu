@@ -220,8 +220,10 @@ __device__ __forceinline__ void search(const hos_drafts& d, int s, long long row
                 bool found = false;
 #pragma unroll
                 for (int k = 0; k < RUN; ++k) {
-                    if (x[k] > 0.0 && !found) pick = first + k;
-                    found |= x[k] > rest;
+                    if (x[k] > 0.0 && !found) {        // only weights decide: rounded sums may have left a rest below zero
+                        pick = first + k;
+                        found = x[k] > rest;
+                    }
                     rest -= x[k];
                 }
                 d.next[s] = d.out_tokens[row] = pick;
