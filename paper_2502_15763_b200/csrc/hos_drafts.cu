@@ -299,7 +299,8 @@ template <typename T> __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) 
             }
             return;
         }
-        const double t = u > 0.0f ? (double)u * all : 0.0;
+        // from 1 on beyond all sums, however they are rounded: the last token that has anything
+        const double t = u >= 1.0f ? __longlong_as_double(0x7FF0000000000000ll) : u > 0.0f ? (double)u * all : 0.0;
         const int block = first_beyond(upto_block, of_block, t);
         if (block == rank) {
             double left = t - __shfl_sync(FULL, upto_block - of_block, block);

@@ -63,3 +63,24 @@ def test_a_number_at_the_end_of_a_share_behind_zeros(dt, vocab, n, with_draft):
     got = draw(target, [0.5] * n, draft)
     for s in range(n):
         assert fits(weights(target[s].double(), None if draft is None else draft[s].double()), 0.5, got[s]), (s, got[s])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,n", [(700, 40), (2000, 60), (9000, 30), (40000, 9), (128000, 4)])
+@pytest.mark.parametrize("u", [1.0, 1.5, math.inf])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_from_one_on_the_last_token_that_has_any(dt, vocab, n, u, with_draft):
+    """However little the last one has."""
+    g = torch.Generator().manual_seed(vocab)
+    target = (torch.rand((n, vocab), generator=g) * (torch.rand((n, vocab), generator=g) < 0.5)).to(DT[dt])
+    last = [vocab - 1 - 3 * s for s in range(n)]
+    for s in range(n):
+        target[s, last[s]:] = 0.0
+        target[s, last[s]] = (1e-14, 1e-20, 3e-16, 1.0)[s % 4]
+    draft = None
+    if with_draft:
+        draft = torch.full_like(target, 0.125)
+        draft[target > 0] *= 0.5
+        for s in range(n):
+            draft[s, last[s]] = 0.0
+    assert draw(target, [u] * n, draft) == last
