@@ -28,6 +28,11 @@ __device__ __forceinline__ Range block_part(int n) {
     const int each = (n + cluster_size() - 1) / cluster_size(), a = min(cluster_rank() * each, n);
     return Range{a, min(a + each, n)};
 }
+// The same in whole groups of 32: the k-th group of the pool is one warp's.
+__device__ __forceinline__ Range block_part_of_groups(int n) {
+    const Range g = block_part((n + 31) / 32);
+    return Range{min(32 * g.first, n), min(32 * g.last, n)};
+}
 // A warp's part of the block's pages: whole groups of 32 but for the last one.
 __device__ __forceinline__ Range warp_part(Range block) {
     const int each = ((block.last - block.first + WARPS - 1) / WARPS + 31) & ~31, a = min(block.first + warp_id() * each, block.last);
@@ -475,7 +480,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_fork(const __grid_constant__ 
 
 // ---- compact -----------------------------------------------------------------------------------------------------------
 // With n pages in use there are as many of them from n on as there are free ones below n; both are numbered in order, and the k-th goes to the
-// k-th.  A table entry finds its new page by two reads: its place among the moves, and where that one goes.
+// k-th.  A table entry finds its new page by two reads: its place among the moves, and where that one goes.  Where it stays, the first read is of
+// its group's mask of free pages instead: whether the page is in use has to be known of every entry, and the counts change under a call in place.
 __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant__ PagesView p) {
     __shared__ int4 live[MOST_BLOCKS], others[MOST_BLOCKS];
     __shared__ int of_warp[3][WARPS];
@@ -483,7 +489,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
     pdl_launch_dependents();
     pdl_wait();
     cluster_begun_arrive();
-    const Range seqs = block_part(p.n_seq), pages = block_part(p.n_pages);
+    const Range seqs = block_part(p.n_seq), pages = block_part_of_groups(p.n_pages);
     const int tid = (int)threadIdx.x;
     const bool in_place = p.table == p.table_in;
     auto row = [&](const RowWork& r, int j) { return load_piece(p.table_in + (long long)r.seq * p.in_stride, j, r.last); };
@@ -530,6 +536,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
         if (a & me) p.src[k] = i;
         if (h & me) p.dst[hole_at + __popc(h & lanes_before())] = i;
         if (i >= n_live && i < masks.part.last) p.growers[i] = a & me ? k : -1;
+        if (i0 < n_live && lane_id() == 0) p.growers[i0 >> 5] = (int)m;        // below the places: i0 / 32 < n_live
         late_at += __popc(a);
         hole_at += __popc(h);
         return true;
@@ -553,17 +560,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv_compact(const __grid_constant
         }
         all_pieces(list, at, row, [&](const RowWork& r, int j, Piece x) {
             if (r.from && j < r.last) {
-                int place[EACH];                       // among the moves
+                int word[EACH];                        // its place among the moves (-1: free), or which pages of its group are free
                 bool bad = false;
 #pragma unroll
-                for (int k = 0; k < EACH; ++k) {
-                    const bool there = 32 * k < r.last - j - lane_id(), page = is_page(p, x.e[k]), moves = there && page && x.e[k] >= n_live;
-                    place[k] = moves ? __ldcg(p.growers + x.e[k]) : -1;
-                    bad |= there && (!page || (moves && place[k] < 0));
-                }
+                for (int k = 0; k < EACH; ++k) word[k] = is_page(p, x.e[k]) ? p.growers[x.e[k] < n_live ? x.e[k] >> 5 : x.e[k]] : -1;
 #pragma unroll
-                for (int k = 0; k < EACH; ++k)
-                    if (place[k] >= 0) x.e[k] = __ldcg(p.dst + place[k]);
+                for (int k = 0; k < EACH; ++k) {
+                    const bool stays = x.e[k] < n_live, wrong = stays ? word[k] >> (x.e[k] & 31) & 1 : word[k] < 0;
+                    bad |= wrong && 32 * k < r.last - j - lane_id();
+                    if (!stays && word[k] >= 0) x.e[k] = __ldcg(p.dst + word[k]);
+                }
                 if (bad) flag(p, r.seq);
             }
             store_piece(p.table + (long long)r.seq * p.out_stride, j, in_place ? r.last : p.max_pages, x);

@@ -50,7 +50,8 @@ struct PagesView {
     int32_t *src, *dst, *count, *status;
     int n_pages, page_size, n_seq, n_out, max_pages;
     // workspace
-    int32_t *growers, *latest, *queue;     // [n_pages]; queue: the free pages in order; hos_kv_compact: growers is a page's place among the moves
+    int32_t *growers, *latest, *queue;     // [n_pages]; queue: the free pages in order; hos_kv_compact: growers is a page's place among the moves,
+                                           // and before those the masks of free pages, 32 each
     ResizePlan* plan;                      // [n_seq]
 };
 
