@@ -442,7 +442,7 @@ typedef struct hos_kv_moves {    /* HOST struct */
  *      growing one after it, keeps its length and pages (HOS_ST_PAGES).
  * A length outside [0, max_pages * page_size], old or new: the sequence stays as it is, with its whole row
  * (HOS_ST_INVALID).  A page that is given up more often than refs says it is held has a count below zero then and is
- * not free (HOS_ST_INVALID).
+ * not free (HOS_ST_INVALID, for every sequence that gives it up).
  * `out` may be `in`, as a whole or array by array.  The copies have to be made before the new tokens are
  * appended, and before the next call of these.
  */
