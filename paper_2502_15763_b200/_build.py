@@ -29,7 +29,7 @@ def _deps():
 def source_hash() -> str:
     """SHA-256 over the scheduling kernels' sources (names and contents, in name order), the headers that the
     KV-cache kernels share with them included: what a set of profiler counters of theirs was taken on.  Only
-    the KV-cache kernels' own files do not count."""
+    the own files of the calls on the cache, on its pages and on drafts do not count."""
     import hashlib
     h = hashlib.sha256()
     for path in sorted(_deps()):
