@@ -7,9 +7,13 @@
 // Sums are kept in 64 bits because the token is found by comparing them: with 128,000 shares of 10^-5 an error of 10^-7
 // would move their ends by a hundredth.
 // Bound: latency where there are few sequences (six dependent steps: offsets, drafts, their probabilities, the row, the blocks' sums,
-// the segment); where there are many, HBM for 32-bit entries, instructions for 16-bit ones (ten a pair).  One B200: one sequence of 32,000
-// 32-bit entries 4.6 us, 33 of 50,257 bf16 ones 6.8; 128 of 128,000 32-bit ones (129 MB) 28 us, 4.6 TB/s: a single wave of blocks, not even
-// over the SMs, whose first and last steps are not hidden behind the reads; 800 of them 6.8 TB/s, of bf16 ones 4.9.
+// the segment); where there are many, HBM for 32-bit entries, instructions for 16-bit ones (ten a pair; the bf16 form spills 16 bytes at its 64
+// registers).  One B200: one sequence of 32,000 32-bit entries 4.6 us, 33 of 50,257 bf16 ones 6.8; 128 of 128,000 32-bit ones, four drafts (129 MB),
+// 27 us, 4.8 TB/s: a single wave of blocks, not even over the SMs, whose first and last steps are not hidden behind the reads; 800 of them
+// with one draft 122 us, 6.7 TB/s, of bf16 ones 81, 5.0, of fp16 ones 78, 5.2.
+// Two forms go entry by entry.  Where a looked-up draft is not accepted, the warp whose segment holds it adds that up again: 128 of 128,000 bf16
+// entries 18.6 us against 14.2 for an accepted one, 800 84 against 61, in 32 bits 126 against 85.  Rows of p and q that are not aligned alike:
+// 128 of 128,000 31 us in 32 bits (23 where they are), 26 in bf16 (18), 800 134 (122) and 113 (81).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -307,7 +311,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) 
             const int warp = first_beyond(upto, own, left);
             left -= __shfl_sync(FULL, upto - own, warp);
             const int from = edge(rank * WARPS + warp), to = edge(rank * WARPS + warp + 1);
-            // one neighbour a thread where that is enough (32,000 entries by 8 blocks of 512 threads: 5.3 us, with 8 neighbours 6.2)
+            // one neighbour a thread where that is enough (one sequence of 32,000 entries: 4.6 us, with 8 neighbours 5.6)
             if (to - from <= THREADS) search<1>(d, s, row, w, from, to, wide, left, sums);
             else search<8>(d, s, row, w, from, to, wide, left, sums);
         }

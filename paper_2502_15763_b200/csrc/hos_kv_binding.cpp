@@ -349,7 +349,7 @@ bool state_of(PyObject* refs_o, PyObject* table_o, PyObject* len_o, long long pa
 }
 
 // The int32 results of a call and its workspace, cut from one allocation: with eight of their own the allocations took longer than
-// the kernel.  (Whoever keeps one of the results keeps the workspace: 12 bytes a page at most.)
+// the kernel.  (Whoever keeps one of the results keeps all of them, the table too, and a workspace of up to 12 bytes a page and 12 a sequence.)
 class Words {
   public:
     explicit Words(int device) : device_(device) {}

@@ -5,8 +5,8 @@
 // of 16 whose barrier is in hardware and whose blocks exchange their sums through shared memory; a barrier through global memory or a
 // launch a phase would cost 1-2 us each.  What bounds them: for small states the reads, block barriers and counters of a
 // phase (0.6-1.2 us each); for large ones the 16 SMs' own rate (a row's entries 32 at a time, instructions as much as bytes).
-// One B200, device time: 16 sequences of 33 entries resized 4.8 us, 128 of 519 with 11,612 pages 9.7, 4 forked into 16 3.4, 128 rows of
-// 1,031 reordered 7.4, 136 pages compacted 4.6, 79,796 pages under 256 rows of 1,031 14.2.
+// One B200, device time: 16 sequences of 33 entries resized 5.0 us, 128 of 519 with 11,612 pages 9.9, 4 forked into 16 3.4, 128 rows of
+// 1,031 reordered 7.4, 136 pages compacted 4.6, 79,796 pages under 256 rows of 1,031 13.8.
 // The contents are a matter of bandwidth: each byte once in and once out, 6.6-6.7 TB/s (see k_kv_copy_pages).
 #include <algorithm>
 
@@ -18,8 +18,9 @@
 namespace hos {
 namespace {
 
-// 256, 512 and 1,024 threads, us: 16 sequences resized 4.8, 5.1, 5.8; 128 9.3, 9.9, 11.2; 4 forked 3.3, 3.4, 4.0; 128 7.5, 7.5, 8.0; 136 pages
-// compacted 4.9, 4.7, 5.4; 79,796 16.6, 14.3, 14.2.  (A barrier of 1,024 threads takes 100-160 cycles, and what all warps do alike adds up.)
+// 256, 512 and 1,024 threads, us: 16 sequences resized 4.9, 5.2, 6.1; 128 9.6, 9.9, 11.2; 4 forked 3.3, 3.4, 3.9; 128 7.5, 7.5, 8.0; 136 pages
+// compacted 4.5, 4.6, 5.4; 79,796 15.8, 13.8, 13.8; 256 rows of 1,000 entries grown in place 26, 11, 10.  (A barrier of 1,024 threads takes
+// 100-160 cycles, and what all warps do alike adds up.)
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 
 struct Range { int first, last; };
@@ -663,9 +664,10 @@ template <int LAYERS> __global__ void __launch_bounds__(COPY_THREADS) k_kv_copy_
 }
 
 // A small state by one block, whose own barrier is enough; any other by a cluster of 16, the most there are (its barriers take 0.5-1 us
-// each, one block 0.1-0.15 us for a thousand entries).  One block, 2, 4, 8, 16, us (with 1,024 threads each): 16 sequences of 33 entries 5.8, 7.4,
-// 7.4, 7.5, 7.7 (resize); 128 of 519, 11,612 pages 17, 14, 12, 11, 11 (resize); 128 of 1,031, twice 39, 24, 15, 10, 8 (fork); 256 of those 129, 65,
-// 34, 21, 14 (compact).
+// each, one block 0.1-0.15 us for a thousand entries).  One block, 2, 4, 8, 16, us: 16 sequences of 33 entries 5.0, 6.4, 6.5, 6.6, 6.8, of 1,024
+// (16,384 entries, mostly empty) 6.0, 7.1, 6.9, 6.6, 6.8 (resize); 128 of 519, 11,612 pages 18, 15, 11, 10, 9.9 (resize); 4 forked into 16 3.4, 3.8, 3.7,
+// 3.7, 3.8, 128 of 1,031 38, 23, 14, 9.8, 7.4 (fork); 136 pages 4.6, 5.6, 5.6, 5.7, 5.8, 79,796 172, 82, 38, 20, 14 (compact).  A resize in
+// place does not go through the entries that stay, but is counted by them all the same: 16 rows of 1,024 take 6.5 us in place, of 33 4.8.
 constexpr long long SMALL_STATE = 8192;
 template <void (*KERNEL)(PagesView)> cudaError_t launch_tables(const char* name, const PagesView& p, cudaStream_t st) {
     const long long rows = p.n_seq > p.n_out ? p.n_seq : p.n_out;
@@ -686,7 +688,8 @@ cudaError_t launch_kv_compact(const PagesView& p, cudaStream_t st) { return laun
 
 // A block a unit, as far as 256 an SM go, where all moves are there (16 moves of 80 layers, 1.34 GB, with 8, 32 and 256 blocks an SM: 224, 208
 // and 200 us, 6.7 TB/s).  Where their number is on the device it is mostly small or nothing, and blocks without work cost more
-// than that (none of 128 moves: 1.9, 5.5 and 40 us; one: 9.8, 10.5, 45): 8 an SM then.
+// than that (none of 128 moves: 1.9, 5.5 and 40 us; one: 9.8, 10.5, 45): 8 an SM then, which takes 225 us for the 1.34 GB and 113 instead of 101 for
+// the 676 MB above.
 cudaError_t launch_kv_copy_pages(const CopyCall& c, const CopyLayer* layers, cudaStream_t st) {
     const long long units = 2ll * ((c.bytes + COPY_UNIT - 1) / COPY_UNIT);
     const long long blocks = std::min<long long>(units * c.n_moves * c.n_layers, ATTN_SMS * (c.count ? 8 : 256));

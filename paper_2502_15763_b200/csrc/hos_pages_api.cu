@@ -7,7 +7,8 @@ namespace {
 
 using namespace hos;
 
-constexpr int MOST_SEQS = 1 << 18, MOST_PAGES = 1 << 24;             // their products with a page's number fit the kernels' sums
+// Numbers of sequences and of pages add up in 32 bits (what is asked for may be more: its sums stop at 2^25, which no pool has).
+constexpr int MOST_SEQS = 1 << 18, MOST_PAGES = 1 << 24;
 
 inline int cuda_rc(cudaError_t e) {
     if (e == cudaSuccess) return HOS_OK;
@@ -15,7 +16,7 @@ inline int cuda_rc(cudaError_t e) {
     return HOS_E_CUDA;
 }
 
-// The sizes of a state, and that what they ask for is there.  `part`: without refs and table, for workspace sizes.
+// The sizes of a state (enough for a workspace's size); and that what they ask for is there, lengths only where `length` says so.
 int check_sizes(const hos_kv_pages* p) {
     if (!p || p->n_pages < 1 || p->page_size < 1 || p->n_seq < 0 || p->max_pages < 0) return HOS_E_INVALID;
     if (p->n_pages > MOST_PAGES || p->n_seq > MOST_SEQS || (long long)p->max_pages * p->page_size >= (1ll << 31) - 256) return HOS_E_UNSUPPORTED;

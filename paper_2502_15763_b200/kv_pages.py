@@ -12,7 +12,9 @@ for hos_kv_resize and hos_kv_compact may be the old ones (and must not overlap w
     r = hos_kv_resize(r["refs"], r["page_table"], r["kv_len"], v["new_len"], page_size)
 
 Everything stays on the device, so a round can be captured into a graph.  Like the other calls of the cache these are plain
-functions without a backward pass.
+functions without a backward pass.  The results of a call lie in one allocation: whoever keeps one of them (the status, say) keeps
+the memory of all, the table and a workspace of up to 12 bytes a page and 12 a sequence included, and torch.save writes all of it;
+clone what is kept for long.
 """
 from __future__ import annotations
 
@@ -37,7 +39,8 @@ def hos_kv_resize(refs, page_table, kv_len, new_len, page_size: int, out=None):
 
     Returns the new state {'refs', 'page_table', 'kv_len'}, the page copies to be made before the next append
     {'src', 'dst': int32 [n_seq], 'count': int32 [1]} and 'status' [n_seq] (HOS_ST_PAGES: too few free pages, the
-    sequence and all growing ones after it keep their lengths; HOS_ST_INVALID)."""
+    sequence and all growing ones after it keep their lengths; HOS_ST_INVALID: a length or a page number out of range, or a
+    page given up whose count comes out below zero)."""
     return _checked(_compiled().resize(refs, page_table, kv_len, new_len, page_size, out), "hos_kv_resize")
 
 
@@ -51,7 +54,8 @@ def hos_kv_fork(refs, page_table, kv_len, parent, page_size: int, out=None):
 def hos_kv_compact(refs, page_table, kv_len, page_size: int, out=None):
     """Moves the pages in use to the front of the pool.
 
-    Returns {'refs', 'page_table', 'kv_len' (the tensor that was given), 'src', 'dst': int32 [n_pages], 'count': int32 [1], 'status' [n_seq]}."""
+    Returns {'refs', 'page_table', 'kv_len' (the tensor that was given), 'src', 'dst': int32 [n_pages], 'count': int32 [1], 'status' [n_seq]}
+    (HOS_ST_INVALID: a length out of range, or the sequence holds a page that refs says is free)."""
     return _checked(_compiled().compact(refs, page_table, kv_len, None, page_size, out), "hos_kv_compact")
 
 
@@ -83,7 +87,8 @@ def hos_verify_drafts(tokens, target, draft, tok_off, u_accept, u_sample, kv_len
     tokens: int32 [n_tokens], packed by tok_off [n_seq + 1] as in the round's attention call: of every sequence the token it
     had, then its drafts.  target, draft: probabilities [n_tokens][vocab] (float32, bfloat16 or float16; rows may be strided):
     row r of target is the distribution after token r, row r of draft the one that tokens[r + 1] was drawn from; draft None: the
-    drafts were not drawn.  u_accept [n_tokens], u_sample [n_seq]: float32 in [0, 1).
+    drafts were not drawn.  u_accept [n_tokens], u_sample [n_seq]: float32 in [0, 1).  Rows of target and draft whose addresses
+    differ modulo 16 bytes are read more slowly (by a tenth to a half).
 
     Returns int32 {'accepted' [n_seq], 'next' [n_seq], 'tokens' [n_tokens]: the accepted drafts, next, then -1 (rows of no
     sequence are not written), 'new_len' [n_seq]: kv_len without the drafts that were not accepted, or None, 'status' [n_seq]}."""
