@@ -1,4 +1,4 @@
-"""What the smoke pass needs of the test tree, and that it runs the kernels on pages and drafts."""
+"""What the smoke pass takes from the tests, and that it runs the kernels on pages and drafts."""
 import ast
 import os
 
@@ -8,7 +8,7 @@ ENTRY = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def test_smoke_takes_no_expected_values_of_pages_and_drafts_from_the_tests():
-    """It is run with test trees that lack the newer files; the two that it has always taken are the harness and the attention formulas."""
+    """The entry states them itself; all that it takes is the harness and the attention formulas."""
     taken = set()
     for node in ast.walk(ast.parse(open(ENTRY).read())):
         if isinstance(node, ast.ImportFrom) and (node.module or "").split(".")[0] == "tests":
